@@ -23,27 +23,18 @@
 // at position pos_base[b] + pos_offset + j.  The round never moves cache data:
 // removing the rejected part of a block only moves pos_base, and the entries
 // past it are overwritten before any row can attend to them.
-#include <cmath>
-
+#include "sq_attn.hpp"
 #include "sq_device.hpp"
 #include "sq_internal.hpp"
+#include "sq_rope.hpp"
 
 namespace sq {
 namespace {
 
-constexpr int kHd = 128;    // head dimension of the family
 constexpr int kChunk = 64;  // cache positions per attention wavefront
 
 // device status bits (the SQ_DEV_* values of the C header)
 constexpr int32_t kBadToken = 1, kBadPos = 2, kOverflow = 4, kNoDist = 8;
-
-typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ void flag(int32_t* status, int32_t bit) {
-  if (status) atomicOr(status, bit);
-}
-
-constexpr uint16_t kNanF16 = 0x7E00;
 
 // ------------------------------------------------------------------ embed
 __global__ __launch_bounds__(256) void embed_kernel(const uint16_t* __restrict__ table, int64_t vocab, int hidden,
@@ -132,67 +123,7 @@ __global__ __launch_bounds__(256) void add_rmsnorm_kernel(float* __restrict__ h,
 }
 
 // ------------------------------------------------- bias + RoPE + cache write
-// The rotation shared by rope_kv_kernel and the attention that rotates its own
-// query rows and new cache entries (the same bits): pair (t, t + 64) of a head
-// turns by pos * theta^(-2t/128), the angle and its cosine and sine in fp64,
-// the turn itself in fp32 with every product rounded on its own.
-// Both functions are short series here: the library's pow and sincos, with their
-// branches for every argument, are code that a launch fetches to run once
-// (with the items' shorter code a rotating attention of 4 x 9 rows over 64
-// positions took 12.1 us, 14.1 before; the attention alone 8.0).
-struct RopeBase {  // ln theta = hi + lo
-  double hi, lo;
-};
-
-// theta^(-2t/128) = exp(-(t / 64) ln theta), the exponent in two parts, the exponential by its Taylor series to
-// degree 13 on |r| <= ln 2 / 2 (next term 4e-18).
-__device__ __forceinline__ double rope_freq(int t, RopeBase base) {
-  const double s = (double)t * (-1.0 / 64.0);
-  const double x = s * base.hi, xl = __builtin_fma(s, base.hi, -x) + s * base.lo;
-  const double n = rint(x * 0x1.71547652b82fep+0);
-  double r = __builtin_fma(n, -0x1.62e42fefa39efp-1, x);
-  r = __builtin_fma(n, -0x1.abc9e3b39803fp-56, r) + xl;
-  double p = 1.0 / 6227020800.0;
-  const double c[] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0,
-                      1.0 / 5040.0,      1.0 / 720.0,      1.0 / 120.0,     1.0 / 24.0,     1.0 / 6.0,
-                      0.5,               1.0,              1.0};
-#pragma unroll
-  for (int i = 0; i < 13; ++i) p = __builtin_fma(p, r, c[i]);
-  return ldexp(p, (int)n);
-}
-
-// Cosine and sine of pos * freq: the angle less n pi / 2 by fused steps with pi / 2 in three parts (the first is
-// exact below 2^31), what the second rounds off carried along, and the Taylor series to degrees 16 and 17 on
-// |r| <= pi / 4 (next terms below 5e-17); 2.3e-16 of the values at most over angles up to 1e6.
-__device__ __forceinline__ float2 rope_cos_sin(int64_t pos, double freq) {
-  const double x = (double)pos * freq;
-  const double n = rint(x * 0x1.45f306dc9c883p-1);
-  const double r1 = __builtin_fma(-n, 0x1.921fb54442d18p+0, x);
-  const double r = __builtin_fma(-n, 0x1.1a62633145c07p-54, r1);
-  const double tail = __builtin_fma(-n, -0x1.f1976b7ed8fbcp-110, __builtin_fma(-n, 0x1.1a62633145c07p-54, r1 - r));
-  const double z = r * r;
-  double ps = 1.0 / 355687428096000.0, pc = 1.0 / 20922789888000.0;
-  const double cs[] = {-1.0 / 1307674368000.0, 1.0 / 6227020800.0, -1.0 / 39916800.0, 1.0 / 362880.0,
-                       -1.0 / 5040.0,          1.0 / 120.0,        -1.0 / 6.0};
-  const double cc[] = {-1.0 / 87178291200.0, 1.0 / 479001600.0, -1.0 / 3628800.0, 1.0 / 40320.0, -1.0 / 720.0,
-                       1.0 / 24.0};
-#pragma unroll
-  for (int i = 0; i < 7; ++i) ps = __builtin_fma(ps, z, cs[i]);
-#pragma unroll
-  for (int i = 0; i < 6; ++i) pc = __builtin_fma(pc, z, cc[i]);
-  const double sn = r + __builtin_fma(r * z, ps, tail);
-  const double co = __builtin_fma(-0.5, z, 1.0) + __builtin_fma(z * z, pc, -r * tail);
-  const int q = (int)(int64_t)n & 3;
-  const double a = q & 1 ? sn : co, b = q & 1 ? co : sn;  // |cosine|, |sine| of the angle
-  return make_float2((float)((q + 1) & 2 ? -a : a), (float)(q & 2 ? -b : b));
-}
-
-__device__ __forceinline__ void rope_turn(float a, float e, float2 cs, float& ra, float& re) {
-#pragma clang fp contract(off)
-  ra = a * cs.x - e * cs.y;
-  re = e * cs.x + a * cs.y;
-}
-
+// The arithmetic is sq_rope.hpp's.
 // One wavefront per (row, head); lane t handles the pair (t, t + 64).
 __global__ __launch_bounds__(64) void rope_kv_kernel(const float* __restrict__ qkv, const uint16_t* __restrict__ bias,
                                                      int hq, int hkv, int rps, const int32_t* __restrict__ pos_base,
@@ -328,27 +259,6 @@ __device__ __forceinline__ void attn_mask_v(int64_t key0, int64_t pmax, int lg, 
       vf[t2][dt] = f;
     }
   }
-}
-
-// v_exp_f32 alone: exp2f's extra steps only serve results below 2^-126.
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// max / sum over the four lanes li + 16 (0..3) that share a query row
-template <class OP>
-__device__ __forceinline__ float quad_fold(float v, OP op) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, v);
-  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const uint32_t p0 = p[0], p1 = p[1];
-  const uint32_t w = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1)));
-  const auto r = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-  const uint32_t r0 = r[0], r1 = r[1];
-  return op(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
-}
-__device__ __forceinline__ float quad_max(float v) {
-  return quad_fold(v, [](float x, float y) { return fmaxf(x, y); });
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  return quad_fold(v, [](float x, float y) { return x + y; });
 }
 
 // One chunk (keys key0 .. key0 + 63) into tile qt's running (m, l, O); the
@@ -1195,14 +1105,6 @@ hipError_t launch_add_rmsnorm(float* h, const float* delta, int64_t m, int hidde
     hipLaunchKernelGGL(add_rmsnorm_kernel<16>, grid, block, 0, stream, h, delta, hidden, w, eps, group, x);
   return hipGetLastError();
 }
-
-namespace {
-RopeBase rope_base(double theta) {
-  const long double ln = std::log((long double)theta);
-  const double hi = (double)ln;
-  return {hi, (double)(ln - (long double)hi)};
-}
-}  // namespace
 
 hipError_t launch_rope_kv(const float* qkv, const uint16_t* bias, int m, int hq, int hkv, int rps,
                           const int32_t* pos_base, int pos_offset, int64_t len_bound, int64_t capacity, double theta,
