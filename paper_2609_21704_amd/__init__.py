@@ -19,6 +19,11 @@ from ._lib import (  # noqa: F401
     sq_attention_f16,
     sq_embed_block_f16,
     sq_kv_adopt_f16,
+    sq_packed_attention_f16,
+    sq_packed_attention_q4,
+    sq_packed_kv_read_q4,
+    sq_packed_rope_kv_f16,
+    sq_packed_rope_kv_q4,
     sq_qgemv_w4a16,
     sq_qgemv_w4a16_acc,
     sq_qgemv_w4a16_rmsnorm,

@@ -74,6 +74,13 @@ def load() -> ctypes.CDLL:
             "sq_prefill_rope_kv_f16": ([P, P, I32, I32, I32, I32, P, I32, I64, I64, ctypes.c_double, P, P, P, P, P],
                                        S),
             "sq_prefill_attention_f16": ([P, P, P, I32, I32, I32, I32, P, I32, I64, I64, P, P], S),
+            "sq_packed_rope_kv_f16": ([P, P, P, I32, I64, I64, I32, I32, P, I32, I64, I64, ctypes.c_double, P, P, P, P,
+                                       P], S),
+            "sq_packed_rope_kv_q4": ([P, P, P, I32, I64, I64, I32, I32, P, I32, I64, I64, ctypes.c_double, P, P, P, P,
+                                      P, P, P], S),
+            "sq_packed_kv_read_q4": ([P, P, P, P, P, I32, I64, I64, I32, P, I32, I64, I64, P, P, P], S),
+            "sq_packed_attention_f16": ([P, P, P, P, I32, I64, I64, I32, I32, P, I32, I64, I64, P, P], S),
+            "sq_packed_attention_q4": ([P, P, P, P, P, P, I32, I64, I64, I32, I32, P, I32, I64, I64, P, P], S),
             "sq_kv_adopt_f16": ([P, P, I32, I32, I32, I32, I64, P, P, P, I32, I32, P], S),
             "sq_spec_commit_multi": ([P, P, P, P, I32, I32, I32, P, P, P, P, I64, P, P, P], S),
         }
@@ -95,6 +102,7 @@ EXPORTED = ("sq_abi_version", "sq_status_str", "sq_quantize_int4_g128", "sq_quan
 
 # device status bits (SQ_DEV_* of include/specquant.h)
 DEV_BAD_TOKEN, DEV_BAD_POS, DEV_OVERFLOW, DEV_NO_DIST = 1, 2, 4, 8
+DEV_BAD_ROWS = 16  # of include/specquant_packed.h
 
 
 def _ptr(t):
@@ -671,3 +679,122 @@ def sq_prefill_attention_f16(q, k_cache, v_cache, pos_base, pos_offset: int, row
     """sq_attention_f16 for blocks of any number of rows."""
     return sq_attention_f16(q, k_cache, v_cache, pos_base, pos_offset, rows_per_seq, len_bound, out,
                             _entry="sq_prefill_attention_f16")
+
+
+# ------------------------------------------------- packed rows, 4-bit cache
+# The calls of include/specquant_packed.h.  row_start: int32 [b + 1] on the GPU, or None for max_rows rows of every
+# sequence; max_rows: a bound on one sequence's rows (by default all rows, which suits one sequence or long prompts).
+
+
+def _q4_cache(k_codes, k_scales, v_codes, v_scales):
+    """(b, hkv, capacity) of a 4-bit cache."""
+    b, hkv, cap, _ = k_codes.shape
+    if cap % 64:
+        raise ValueError("the cache capacity must be a multiple of 64")
+    _expect(k_codes, torch.uint8, (b, hkv, cap, HEAD_DIM // 2), "k_codes")
+    _expect(k_scales, torch.float16, (b, hkv, cap, 4), "k_scales")
+    _expect(v_codes, torch.uint8, (b, hkv, cap // 64, 64, 64), "v_codes")
+    _expect(v_scales, torch.float16, (b, hkv, cap // 64, 4, 64), "v_scales")
+    return b, hkv, cap
+
+
+def _packed(b: int, cap: int, rows: int, row_start, pos_base, max_rows, len_bound):
+    if row_start is not None:
+        _expect(row_start, torch.int32, (b + 1,), "row_start")
+        max_rows = max(rows, 1) if max_rows is None else int(max_rows)
+    elif max_rows is None:
+        if rows % b:
+            raise ValueError("without row_start every sequence has the same number of rows")
+        max_rows = max(rows // b, 1)
+    _expect(pos_base, torch.int32, (b,), "pos_base")
+    return int(max_rows), cap if len_bound is None else int(len_bound)
+
+
+def _packed_rope(entry, qkv, bias, row_start, pos_base, hq, cache, dims, max_rows, pos_offset, len_bound, theta, q_out,
+                 status):
+    b, hkv, cap = dims
+    nh = hq + 2 * hkv
+    if qkv.dtype != torch.float32 or qkv.numel() % (nh * HEAD_DIM):
+        raise ValueError("qkv must be float32 [rows][(hq + 2 hkv) * 128]")
+    rows = qkv.numel() // (nh * HEAD_DIM)
+    max_rows, len_bound = _packed(b, cap, rows, row_start, pos_base, max_rows, len_bound)
+    q_out = torch.empty((rows, hq, HEAD_DIM), dtype=torch.float16, device=qkv.device) if q_out is None else q_out
+    dev = _dev(qkv, bias, row_start, pos_base, q_out, *cache, status)
+    _expect(q_out, torch.float16, (rows, hq, HEAD_DIM), "q_out")
+    if bias is not None:
+        _expect(bias, torch.float16, (nh * HEAD_DIM,), "bias")
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise ValueError("status must be int32")
+    with torch.cuda.device(dev):
+        _check(getattr(load(), entry)(_ptr(qkv), _ptr(bias), _ptr(row_start), b, rows, max_rows, hq, hkv,
+                                      _ptr(pos_base), int(pos_offset), len_bound, cap, float(theta), _ptr(q_out),
+                                      *map(_ptr, cache), _ptr(status), _stream(dev)), entry)
+    return q_out
+
+
+def sq_packed_rope_kv_f16(qkv, bias, row_start, pos_base, hq: int, k_cache, v_cache, max_rows: int | None = None,
+                          pos_offset: int = 0, len_bound: int | None = None, theta: float = 1e6, q_out=None,
+                          status=None):
+    """Bias + RoPE of packed q|k|v rows, keys and values into the fp16 cache; returns q_out [rows][hq][128] fp16."""
+    return _packed_rope("sq_packed_rope_kv_f16", qkv, bias, row_start, pos_base, hq, (k_cache, v_cache),
+                        _cache_dims(k_cache, v_cache), max_rows, pos_offset, len_bound, theta, q_out, status)
+
+
+def sq_packed_rope_kv_q4(qkv, bias, row_start, pos_base, hq: int, k_codes, k_scales, v_codes, v_scales,
+                         max_rows: int | None = None, pos_offset: int = 0, len_bound: int | None = None,
+                         theta: float = 1e6, q_out=None, status=None):
+    """sq_packed_rope_kv_f16 into a 4-bit cache (k_codes u8 [b][hkv][capacity][64], k_scales fp16
+    [b][hkv][capacity][4], v_codes u8 [b][hkv][capacity / 64][64][64], v_scales fp16 [b][hkv][capacity / 64][4][64])."""
+    cache = (k_codes, k_scales, v_codes, v_scales)
+    return _packed_rope("sq_packed_rope_kv_q4", qkv, bias, row_start, pos_base, hq, cache, _q4_cache(*cache), max_rows,
+                        pos_offset, len_bound, theta, q_out, status)
+
+
+def sq_packed_kv_read_q4(k_codes, k_scales, v_codes, v_scales, row_start, pos_base, rows: int,
+                         max_rows: int | None = None, pos_offset: int = 0, len_bound: int | None = None, k_out=None,
+                         v_out=None):
+    """(k_out, v_out) [rows][hkv][128] fp16: what the 4-bit entries at the packed rows' positions stand for."""
+    cache = (k_codes, k_scales, v_codes, v_scales)
+    b, hkv, cap = _q4_cache(*cache)
+    max_rows, len_bound = _packed(b, cap, rows, row_start, pos_base, max_rows, len_bound)
+    shape = (rows, hkv, HEAD_DIM)
+    k_out = torch.empty(shape, dtype=torch.float16, device=k_codes.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=torch.float16, device=k_codes.device) if v_out is None else v_out
+    dev = _dev(*cache, row_start, pos_base, k_out, v_out)
+    _expect(k_out, torch.float16, shape, "k_out")
+    _expect(v_out, torch.float16, shape, "v_out")
+    with torch.cuda.device(dev):
+        _check(load().sq_packed_kv_read_q4(*map(_ptr, cache), _ptr(row_start), b, rows, max_rows, hkv, _ptr(pos_base),
+                                           int(pos_offset), len_bound, cap, _ptr(k_out), _ptr(v_out), _stream(dev)),
+               "sq_packed_kv_read_q4")
+    return k_out, v_out
+
+
+def _packed_attention(entry, q, cache, dims, row_start, pos_base, max_rows, pos_offset, len_bound, out):
+    b, hkv, cap = dims
+    if q.dtype != torch.float16 or q.dim() != 3 or q.shape[2] != HEAD_DIM:
+        raise ValueError("q must be float16 [rows][hq][128]")
+    rows, hq, _ = q.shape
+    max_rows, len_bound = _packed(b, cap, rows, row_start, pos_base, max_rows, len_bound)
+    out = torch.empty((rows, hq, HEAD_DIM), dtype=torch.float16, device=q.device) if out is None else out
+    dev = _dev(q, *cache, row_start, pos_base, out)
+    _expect(out, torch.float16, (rows, hq, HEAD_DIM), "out")
+    with torch.cuda.device(dev):
+        _check(getattr(load(), entry)(_ptr(q), *map(_ptr, cache), _ptr(row_start), b, rows, max_rows, hq, hkv,
+                                      _ptr(pos_base), int(pos_offset), len_bound, cap, _ptr(out), _stream(dev)), entry)
+    return out
+
+
+def sq_packed_attention_f16(q, k_cache, v_cache, row_start, pos_base, max_rows: int | None = None, pos_offset: int = 0,
+                            len_bound: int | None = None, out=None):
+    """Causal GQA attention of packed rows over the fp16 cache; returns out [rows][hq][128] fp16."""
+    return _packed_attention("sq_packed_attention_f16", q, (k_cache, v_cache), _cache_dims(k_cache, v_cache), row_start,
+                             pos_base, max_rows, pos_offset, len_bound, out)
+
+
+def sq_packed_attention_q4(q, k_codes, k_scales, v_codes, v_scales, row_start, pos_base, max_rows: int | None = None,
+                           pos_offset: int = 0, len_bound: int | None = None, out=None):
+    """sq_packed_attention_f16 over a 4-bit cache."""
+    cache = (k_codes, k_scales, v_codes, v_scales)
+    return _packed_attention("sq_packed_attention_q4", q, cache, _q4_cache(*cache), row_start, pos_base, max_rows,
+                             pos_offset, len_bound, out)

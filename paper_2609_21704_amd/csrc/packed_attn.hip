@@ -1,0 +1,794 @@
+// Causal grouped-query attention of packed rows over a cache of fp16 or 4-bit entries:
+//   out[r][h] = f16( sum_{t <= p} e_t v_t / sum_{t <= p} e_t ),  e_t = exp(q . k_t / sqrt(128))
+// for row r at position p of its sequence, the softmax kept as a running maximum and sum while the keys pass once.
+// The G = hq / hkv query heads of a kv head read the same keys, so the unit of work is a tile of a sequence's queries
+// qi = j G + gg (row j, head gg of the group): one pass over the keys serves all G heads.
+//   prompt_attn_kernel  many rows: 32 queries a wavefront, keys through LDS; bound by the matrix cores
+//   few_attn_kernel     few rows: every wavefront its own keys; bound by the cache's bytes
+//   packed_merge_kernel joins the parts of the keys where they were split over workgroups
+// Both keep S^T = K Q^T and O^T = V^T P^T, so that a query is a lane's column in every product: the maximum, the sum
+// and the rescaling of O need no exchange but a fold over the lanes of one column.  The keys enter S^T in an order that
+// makes a lane's scores consecutive keys, which is the order that P^T's fragments take: P goes from one product to the
+// next in registers.
+// Scores, maxima, sums and O are fp32.  A weight enters the product with V as one binary16: 2^-11 of itself off, as the
+// output's own rounding is, and independent from key to key.  Weights are kept times 2^7, and the reference maximum is
+// moved only when a row's maximum passes it by 2^8, so they stay below 2^15 and a weight loses bits only
+// below 2^-21 of the row's largest.
+#include "sq_internal.hpp"
+#include "sq_packed.hpp"
+
+namespace sq {
+namespace {
+
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kTile = 64;  // keys per step
+constexpr float kScale = 1.4426950408889634f * 0.08838834764831845f;  // log2(e) / sqrt(128)
+constexpr float kShift = 7.f, kSlack = 8.f;
+constexpr float kNoMax = -1e30f;  // a finite start: exp2(kNoMax - m) = 0 and exp2(-inf - kNoMax) = 0
+
+struct AttnArgs {
+  const uint16_t* q;
+  KvCache c;
+  const int32_t* pos_base;
+  int pos_offset, hq, hkv;
+  int64_t len_bound, capacity;
+  uint16_t* out;
+  float* part_o;    // [item][slot][query][128], null without splitting
+  float2* part_ml;  // [item][slot][query]
+  int nslots;
+};
+
+// max / sum over the two lanes that share a column of a 32 x 32 product
+template <class OP>
+__device__ __forceinline__ float pair_fold(float v, OP op) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t p0 = p[0], p1 = p[1];
+  return op(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1));
+}
+
+__device__ __forceinline__ bool nonfinite_h(half_t v) { return (__builtin_bit_cast(uint16_t, v) & 0x7C00) == 0x7C00; }
+
+// The keys of part `slot` of `n` steps of 64 split evenly over nslots parts, in multiples of `grain` steps.
+__device__ __forceinline__ void slot_steps(int n, int nslots, int slot, int grain, int& lo, int& hi) {
+  int span = (n + nslots - 1) / nslots;
+  span = (span + grain - 1) / grain * grain;
+  lo = slot * span;
+  hi = lo + span < n ? lo + span : n;
+}
+
+// ------------------------------------------------------------------ dequant
+// Sixteen bytes of codes to 16 halves of the low and 16 of the high nibbles: f16((c - z) s), the difference exact.
+template <bool HIGH, class Z, class S>
+__device__ __forceinline__ void dequant16(u32x4 w, Z zero, S scale, half8_t (&o)[2]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    half2_t a, b;
+    code_pairs<HIGH>(w[i], a, b);
+    a = (a - zero(2 * i)) * scale(2 * i);
+    b = (b - zero(2 * i + 1)) * scale(2 * i + 1);
+    o[i >> 1][4 * (i & 1) + 0] = a[0];
+    o[i >> 1][4 * (i & 1) + 1] = a[1];
+    o[i >> 1][4 * (i & 1) + 2] = b[0];
+    o[i >> 1][4 * (i & 1) + 3] = b[1];
+  }
+}
+
+// A key's part: 16 elements of each group, with the key's own scales and zeros.
+__device__ __forceinline__ void dequant_key(u32x4 w, uint2 sz, half8_t (&lo)[2], half8_t (&hi)[2]) {
+  const half2_t s0 = bits_h2((sz.x & 0xFFFF) * 0x10001u), z0 = zero_pair<false>(bits_h2((sz.x >> 16) * 0x10001u));
+  const half2_t s1 = bits_h2((sz.y & 0xFFFF) * 0x10001u), z1 = zero_pair<true>(bits_h2((sz.y >> 16) * 0x10001u));
+  dequant16<false>(w, [&](int) { return z0; }, [&](int) { return s0; }, lo);
+  dequant16<true>(w, [&](int) { return z1; }, [&](int) { return s1; }, hi);
+}
+
+// Scales and zeros of 16 consecutive positions of a block of values: [4][64] halves, 32 bytes of each row.
+struct ValScales {
+  u32x4 p[4][2];
+};
+__device__ __forceinline__ ValScales load_val_scales(const uint16_t* vs) {
+  ValScales r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) r.p[i][h] = *reinterpret_cast<const u32x4*>(vs + 64 * i + 8 * h);
+  return r;
+}
+template <bool HIGH>
+__device__ __forceinline__ void dequant_val(u32x4 w, const ValScales& v, half8_t (&o)[2]) {
+  constexpr int si = HIGH ? 2 : 0;
+  dequant16<HIGH>(
+      w,
+      [&](int i) {
+        const uint32_t z = v.p[si + 1][i >> 2][i & 3];
+        return zero_pair<HIGH>(bits_h2(z));
+      },
+      [&](int i) {
+        const uint32_t s = v.p[si][i >> 2][i & 3];
+        return bits_h2(s);
+      },
+      o);
+}
+
+// Element `dim` of the value at position `key` of (sequence, kv head) sg.
+template <bool Q4>
+__device__ __forceinline__ float value_at(const AttnArgs& a, int64_t sg, int64_t key, int dim) {
+  if constexpr (!Q4) return f16_bits_to_f32(a.c.v[(sg * kHd + dim) * a.capacity + key]);
+  const int64_t blk = sg * a.capacity + (key & ~63);
+  const int j = dim & 63, t = (int)key & 63, hi = dim >> 6;
+  const uint32_t c = a.c.v4[blk * 64 + j * 64 + swap01(t)] >> (4 * hi) & 15;
+  const uint16_t* p = a.c.vs + blk * 4 + 128 * hi + t;
+  return (float)(half_t)(((float)c - f16_bits_to_f32(p[64])) * f16_bits_to_f32(p[0]));
+}
+
+// The elements of a key's value that are not finite (zero for the others), dims lane and 64 + lane: the lanes hand them
+// round, since a lane's own 32 or 64 addresses would be formed ahead of the loop over keys and held in registers.
+struct OddValue {
+  float v[2];
+};
+template <bool Q4>
+__device__ __forceinline__ OddValue odd_value(const AttnArgs& a, int64_t sg, int64_t key) {
+  OddValue r;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float v = value_at<Q4>(a, sg, key, 64 * i + lane);
+    r.v[i] = fabsf(v) <= 65504.f ? 0.f : v;
+  }
+  return r;
+}
+
+// Values in a step of which some row may read only a part of the keys: those after the last key `left` (an index into
+// the fragment) are stale and zeroed; one that is not finite is zeroed too, since a zero weight times it is NaN, and its
+// key noted in `odd`: add_odd gives it to the rows that read it.
+__device__ __forceinline__ half8_t tame(half8_t f, int left, uint32_t& odd) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const bool nf = e <= left && nonfinite_h(f[e]);
+    odd |= nf ? 1u << e : 0u;
+    f[e] = e > left || nf ? (half_t)0 : f[e];
+  }
+  return f;
+}
+
+// ---------------------------------------------------------------- few rows
+// One workgroup per (part of the keys, sequence, kv head); its wavefronts take the part's steps of 64 keys in turn, each
+// for all the queries (NQT tiles of 16), and meet in LDS.  v_mfma_f32_16x16x32_f16: lane l holds row / column li = l %
+// 16 and k = 8 lg .. +8 (lg = l / 16); D[4 lg + i][li].  Row r of the key tile kt is key 16 (r / 4) + 4 kt + r % 4, so a
+// lane ends with the scores of keys 16 lg .. 16 lg + 15 of query li, and takes the values of those keys as they lie.
+constexpr int kFewWaves = 4;
+
+template <bool Q4, int NQT>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(NQT > 2 ? 1 : 2))) void few_attn_kernel(PackedRows pr, AttnArgs a) {
+  __shared__ __align__(16) float ob[kFewWaves][16][kHd + 4];
+  __shared__ float2 ml[kFewWaves][16];
+  const int slot = blockIdx.x, s = blockIdx.y / a.hkv, g = blockIdx.y - s * a.hkv;
+  const int64_t sg = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.hq / a.hkv;
+  const SeqRows sr = seq_rows(pr, s);
+  const int nq = sr.n * G;
+  if (nq == 0) return;
+  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
+  const int64_t pl = p0 + sr.n - 1;
+  const int64_t klast = pl < a.len_bound ? pl : a.len_bound - 1;  // (rows past the bound are not computed)
+  const int nst = klast < 0 ? 0 : (int)(klast / kTile) + 1;
+  int st0, st1;
+  slot_steps(nst, a.nslots, slot, kFewWaves, st0, st1);
+  if (st0 >= st1 && slot > 0) return;  // the part has no keys (part 0 always answers: rows without any key)
+
+  half8_t qf[NQT][4];
+  int lpos[NQT];  // the position of this lane's query, clipped to [-1, 2^31)
+#pragma unroll
+  for (int t = 0; t < NQT; ++t) {
+    const int qi = 16 * t + li, qc = qi < nq ? qi : nq - 1;
+    const int j = qc / G;
+    const uint16_t* qp = a.q + ((int64_t)(sr.first + j) * a.hq + g * G + (qc - j * G)) * kHd;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      qf[t][x] = *reinterpret_cast<const half8_t*>(qp + (Q4 ? (x >> 1) * 64 + 16 * lg + 8 * (x & 1) : 32 * lg + 8 * x));
+    const int64_t p = p0 + j;
+    lpos[t] = p < 0 ? -1 : (p > 0x7FFFFFFF ? 0x7FFFFFFF : (int)p);
+  }
+  float m[NQT], l[NQT];
+  float4_t o[NQT][8];
+#pragma unroll
+  for (int t = 0; t < NQT; ++t) {
+    m[t] = kNoMax;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) o[t][d] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int krow = 16 * (li >> 2) + (li & 3);  // + 4 kt: this lane's key of a tile
+  for (int st = st0 + wave; st < st1; st += kFewWaves) {
+    const int64_t key0 = (int64_t)st * kTile;
+    float4_t sc[NQT][4];
+    u32x4 vw[Q4 ? 4 : 16];  // 4-bit: codes of byte row 16 j + li; fp16: positions 16 lg .. +16 of dim 16 d + li
+    ValScales vs;
+    if constexpr (Q4) {
+      u32x4 kw[4];
+      uint2 ksz[4];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const int64_t e = sg * a.capacity + key0 + krow + 4 * kt;
+        kw[kt] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + lg];
+        ksz[kt] = reinterpret_cast<const uint2*>(a.c.ks)[e];
+      }
+      vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * lg);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        vw[j] = *reinterpret_cast<const u32x4*>(a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 +
+                                                (16 * j + li) * 64 + 16 * lg);
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        half8_t lo[2], hi[2];
+        dequant_key(kw[kt], ksz[kt], lo, hi);
+#pragma unroll
+        for (int t = 0; t < NQT; ++t) {
+          float4_t acc = {0.f, 0.f, 0.f, 0.f};
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[0], qf[t][0], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[1], qf[t][1], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[0], qf[t][2], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[1], qf[t][3], acc, 0, 0, 0);
+          sc[t][kt] = acc;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const uint16_t* kp = a.c.k + (sg * a.capacity + key0 + krow + 4 * kt) * kHd + 32 * lg;
+        half8_t kf[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) kf[x] = *reinterpret_cast<const half8_t*>(kp + 8 * x);
+#pragma unroll
+        for (int t = 0; t < NQT; ++t) {
+          float4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x], qf[t][x], acc, 0, 0, 0);
+          sc[t][kt] = acc;
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const uint16_t* vp = a.c.v + (sg * kHd + 16 * d + li) * a.capacity + key0 + 16 * lg;
+        vw[2 * d] = *reinterpret_cast<const u32x4*>(vp);
+        vw[2 * d + 1] = *reinterpret_cast<const u32x4*>(vp + 8);
+      }
+    }
+    // only a step past the first row's position holds keys that some row may not read
+    const bool tail = key0 + kTile - 1 > p0;  // uniform
+    half8_t pf[NQT][2];
+#pragma unroll
+    for (int t = 0; t < NQT; ++t) {
+      if (tail) {
+        const int lim = (int)(lpos[t] - key0 < kTile ? lpos[t] - key0 : kTile) - 16 * lg;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[t][kt][i] = 4 * kt + i <= lim ? sc[t][kt][i] : -__builtin_inff();
+      }
+      float cm = sc[t][0][0];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cm = fmaxf(cm, sc[t][kt][i]);
+      cm = quad_max(cm) * kScale;
+      if (__any(cm > m[t] + kSlack)) {
+        const float mn = fmaxf(m[t], cm), alpha = exp2_fast(m[t] - mn);
+        m[t] = mn;
+        l[t] *= alpha;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) o[t][d] *= alpha;
+      }
+      const float ref = kShift - m[t];
+      float sum = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = exp2_fast(__builtin_fmaf(sc[t][kt][i], kScale, ref));
+          sum += p;
+          pf[t][kt >> 1][4 * (kt & 1) + i] = (half_t)p;
+        }
+      l[t] += sum;
+    }
+    uint32_t odd = 0;  // of this lane's 16 keys
+    const int left = (int)(klast - key0 < kTile ? klast - key0 : kTile) - 16 * lg;
+    auto product = [&](int d, half8_t v0, half8_t v1) {
+      if (tail) {
+        uint32_t o0 = 0, o1 = 0;
+        v0 = tame(v0, left, o0);
+        v1 = tame(v1, left - 8, o1);
+        odd |= o0 | o1 << 8;
+      }
+#pragma unroll
+      for (int t = 0; t < NQT; ++t) {
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[t][0], o[t][d], 0, 0, 0);
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[t][1], o[t][d], 0, 0, 0);
+      }
+    };
+    if constexpr (Q4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        half8_t x[2];
+        dequant_val<false>(vw[j], vs, x);
+        product(j, x[0], x[1]);
+        dequant_val<true>(vw[j], vs, x);
+        product(4 + j, x[0], x[1]);
+      }
+    } else {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const u32x4 w0 = vw[2 * d], w1 = vw[2 * d + 1];
+        product(d, __builtin_bit_cast(half8_t, w0), __builtin_bit_cast(half8_t, w1));
+      }
+    }
+    if (tail && __any(odd != 0)) {
+#pragma unroll 1
+      for (int key = 0; key < kTile; ++key) {
+        if (!(__ballot((odd >> (key & 15)) & 1) >> (16 * (key >> 4)) & 0xFFFF)) continue;  // uniform
+        const OddValue ov = odd_value<Q4>(a, sg, key0 + key);
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = __shfl(ov.v[d >> 2], 16 * (d & 3) + 4 * lg + i, kWave);
+#pragma unroll
+            for (int t = 0; t < NQT; ++t) o[t][d][i] += key0 + key <= lpos[t] ? v : 0.f;
+          }
+      }
+    }
+  }
+  // the wavefronts' sums meet, a query tile at a time
+  const int nq_pad = 16 * NQT;
+#pragma unroll 1
+  for (int t = 0; t < NQT; ++t) {
+    if (16 * t >= nq) break;  // uniform
+    if (t) __syncthreads();
+    float mt = 0.f, lt = 0.f;
+    float4_t ot[8];
+#pragma unroll
+    for (int x = 0; x < NQT; ++x)
+      if (x == t) {
+        mt = m[x];
+        lt = l[x];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) ot[d] = o[x][d];
+      }
+    lt = quad_sum(lt);
+    if (lg == 0) ml[wave][li] = make_float2(mt, lt);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) *reinterpret_cast<float4_t*>(&ob[wave][li][16 * d + 4 * lg]) = ot[d];
+    __syncthreads();
+    const int qr = tid >> 4, d0 = 8 * (tid & 15), qi = 16 * t + qr;
+    float M = kNoMax, L = 0.f, f[kFewWaves], r[8] = {};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, ml[w][qr].x);
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      f[w] = exp2_fast(ml[w][qr].x - M);
+      L += f[w] * ml[w][qr].y;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) r[x] += f[w] * ob[w][qr][d0 + x];
+    }
+    if (a.part_o) {
+      const int64_t at = (sg * a.nslots + slot) * nq_pad + qi;
+      float4_t* po = reinterpret_cast<float4_t*>(a.part_o + at * kHd + d0);
+      po[0] = float4_t{r[0], r[1], r[2], r[3]};
+      po[1] = float4_t{r[4], r[5], r[6], r[7]};
+      if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
+    } else if (qi < nq) {
+      const int j = qi / G;
+      const int64_t pos = p0 + j;
+      const bool bad = pos < 0 || pos >= a.len_bound;
+      half8_t h;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) h[x] = bad ? __builtin_bit_cast(half_t, kNanF16) : (half_t)(r[x] / L);
+      *reinterpret_cast<half8_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + d0) = h;
+    }
+  }
+}
+
+// -------------------------------------------------------------- many rows
+// One workgroup per (tile of 32 NW queries, kv head, part of the keys): each wavefront 32 queries, the keys in steps of
+// 64 through two LDS buffers (the next step's loads in flight meanwhile, one barrier a step).
+// v_mfma_f32_32x32x16_f16: lane l holds row / column lc = l % 32 and k = 8 h .. +8 (h = l / 32), and of D rows 8 (i / 4) +
+// 4 h + i % 4 of column lc.  Row r of a key tile is the key r with bits 2 and 3 exchanged, so that a lane's 16 scores
+// are keys 16 (i / 8) + 8 h + i % 8: the P^T fragments of two steps of 16 keys.
+// LDS: keys as rows of 16 cells (16 B) with cell c at c ^ (r % 16), values as rows of 8 cells (64 positions of a
+// dimension) with cell c at c ^ (d / 2 % 8): 16 lanes of one fragment read 16 different 16-byte banks.
+__device__ __forceinline__ int swap23(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
+
+template <bool Q4, int NW, bool SPLIT>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
+                                                                                                      AttnArgs a) {
+  constexpr int NT = 64 * NW, TQ = 32 * NW;
+  constexpr int kCells = 1024 / NT;               // fp16: 16-byte cells of keys (and of values) per thread
+  constexpr int kCodes = NW >= 8 ? 1 : 512 / NT;  // 4-bit: 16-byte cells of codes per thread
+  __shared__ __align__(16) u32x4 kb[2][1024], vb[2][1024];
+  __shared__ unsigned long long odd_keys[3];  // keys of a step whose values are not finite
+  const int G = a.hq / a.hkv;
+  const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
+  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int s, t;
+  if (!find_tile(pr.b, item, [&](int i) { return (seq_rows(pr, i).n * G + TQ - 1) / TQ; }, s, t)) return;
+  const SeqRows sr = seq_rows(pr, s);
+  const int nq = sr.n * G;
+  const int qt = (nq + TQ - 1) / TQ - 1 - t;  // the latest rows (the most keys) first
+  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
+  const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
+  const int64_t pmin = p0 + qt * TQ / G, pl = p0 + qlast / G;
+  const int64_t klast64 = pl < a.len_bound ? pl : a.len_bound - 1;
+  const int klast = klast64 < -1 ? -1 : (int)klast64;
+  int st0 = 0, st1 = klast < 0 ? 0 : klast / kTile + 1;
+  if constexpr (SPLIT) {
+    slot_steps(st1, a.nslots, blockIdx.y, 1, st0, st1);
+    if (st0 >= st1 && blockIdx.y > 0) return;
+  }
+  const int64_t sg = (int64_t)s * a.hkv + g;
+  const int wq = qt * TQ + 32 * wave;                       // the wavefront's first query
+  const bool owner = wq < nq;
+  const int qi = wq + lc < nq ? wq + lc : nq - 1, qj = qi / G;
+  auto clip = [](int64_t p) { return p < 0 ? -1 : (p > 0x7FFFFFFF ? 0x7FFFFFFF : (int)p); };
+  const int lpos = clip(p0 + qj);
+  const int wmin = clip(p0 + wq / G);                       // of the wavefront's queries
+  const int wmax = clip(p0 + (wq + 31 < nq ? wq + 31 : nq - 1) / G);
+  const uint16_t* qp = a.q + ((int64_t)(sr.first + qj) * a.hq + g * G + (qi - qj * G)) * kHd + 8 * h;
+  half8_t qf[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) qf[x] = *reinterpret_cast<const half8_t*>(qp + 16 * x);
+
+  u32x4 pre[Q4 ? kCodes : 2 * kCells];
+  uint2 pre_ks[Q4 ? kCodes : 1];
+  ValScales pre_vs;
+  // 4-bit cell c: key c / 4, part c % 4 of it (c < 256), byte (c - 256) / 4 of the block of values, positions 16 (c % 4)
+  // .. +16; which of the two is uniform across a wavefront
+  auto load_step = [&](int st) {
+    const int64_t key0 = (int64_t)st * kTile;
+    if constexpr (Q4) {
+#pragma unroll
+      for (int i = 0; i < kCodes; ++i) {
+        const int c = tid + NT * i;
+        if (c < 256) {
+          const int64_t e = sg * a.capacity + key0 + (c >> 2);
+          pre[i] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + (c & 3)];
+          pre_ks[i] = reinterpret_cast<const uint2*>(a.c.ks)[e];
+        } else {
+          const int c2 = c - 256;
+          pre[i] = *reinterpret_cast<const u32x4*>(a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 + 16 * c2);
+          pre_vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * (c2 & 3));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCells; ++i) {
+        const int c = tid + NT * i;
+        pre[i] = *reinterpret_cast<const u32x4*>(a.c.k + (sg * a.capacity + key0 + (c >> 4)) * kHd + (c & 15) * 8);
+      }
+#pragma unroll
+      for (int i = 0; i < kCells; ++i) {
+        const int c = tid + NT * i;
+        pre[kCells + i] =
+            *reinterpret_cast<const u32x4*>(a.c.v + (sg * kHd + (c >> 3)) * a.capacity + key0 + (c & 7) * 8);
+      }
+    }
+  };
+  // a cell of eight positions of a dimension into the buffer
+  auto put_val = [&](int buf, int st, int d, int part, half8_t v, uint32_t& odd) {
+    if (st * (int64_t)kTile + kTile - 1 > pmin) v = tame(v, klast - (st * kTile + 8 * part), odd);  // uniform
+    vb[buf][d * 8 + (part ^ ((d >> 1) & 7))] = __builtin_bit_cast(u32x4, v);
+  };
+  auto store_step = [&](int buf, int st) {
+    if constexpr (Q4) {
+#pragma unroll
+      for (int i = 0; i < kCodes; ++i) {
+        const int c = tid + NT * i;
+        half8_t lo[2], hi[2];
+        if (c < 256) {
+          const int key = c >> 2, part = c & 3;
+          dequant_key(pre[i], pre_ks[i], lo, hi);
+          const int sw = swap23(key & 15);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            kb[buf][key * 16 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
+            kb[buf][key * 16 + ((8 + 2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
+          }
+        } else {
+          const int c2 = c - 256, j = c2 >> 2, part = c2 & 3;
+          dequant_val<false>(pre[i], pre_vs, lo);
+          dequant_val<true>(pre[i], pre_vs, hi);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            uint32_t odd = 0;
+            put_val(buf, st, j, 2 * part + x, lo[x], odd);
+            put_val(buf, st, j + 64, 2 * part + x, hi[x], odd);
+            if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * (2 * part + x)));
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCells; ++i) {
+        const int c = tid + NT * i;
+        kb[buf][(c & ~15) + ((c & 15) ^ swap23((c >> 4) & 15))] = pre[i];
+      }
+#pragma unroll
+      for (int i = 0; i < kCells; ++i) {
+        const int c = tid + NT * i;
+        const u32x4 w = pre[kCells + i];
+        uint32_t odd = 0;
+        put_val(buf, st, c >> 3, c & 7, __builtin_bit_cast(half8_t, w), odd);
+        if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * (c & 7)));
+      }
+    }
+  };
+
+  float m = kNoMax, l = 0.f;
+  float16_t o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  if (tid < 3) odd_keys[tid] = 0;
+  __syncthreads();
+  if (st0 < st1) {
+    load_step(st0);
+    store_step(st0 & 1, st0);
+  }
+  for (int st = st0; st < st1; ++st) {
+    const int key0 = st * kTile, buf = st & 1;
+    // step st is in its buffer, and every wavefront is done with step st - 1; what the barrier does not wait for: the
+    // loads of step st + 1
+    __syncthreads();
+    if (st + 1 < st1) load_step(st + 1);
+    if (tid == 0) odd_keys[(st + 2) % 3] = 0;
+    const bool past = key0 + kTile - 1 > pmin;  // uniform: some row of the workgroup may not read some key
+    if (owner && key0 <= wmax) {  // uniform in the wavefront
+      float16_t sc[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
+        const u32x4* row = &kb[buf][(32 * b + swap23(lc)) * 16];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const u32x4 w = row[(2 * x + h) ^ (lc & 15)];
+          sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), qf[x], sc[b], 0, 0, 0);
+        }
+      }
+      const bool tail = key0 + kTile - 1 > wmin;  // uniform
+      if (tail) {
+        const int lim = (lpos - key0 < kTile ? lpos - key0 : kTile) - 8 * h;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            sc[b][i] = 32 * b + 16 * (i >> 3) + (i & 7) <= lim ? sc[b][i] : -__builtin_inff();
+      }
+      float cm = sc[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) cm = fmaxf(cm, sc[b][i]);
+      cm = pair_fold(cm, [](float x, float y) { return fmaxf(x, y); }) * kScale;
+      if (__any(cm > m + kSlack)) {
+        const float mn = fmaxf(m, cm), alpha = exp2_fast(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[d] *= alpha;
+      }
+      const float ref = kShift - m;
+      half8_t pf[4];
+      float sum = 0.f;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = exp2_fast(__builtin_fmaf(sc[b][i], kScale, ref));
+          sum += p;
+          pf[2 * b + (i >> 3)][i & 7] = (half_t)p;
+        }
+      l += sum;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const u32x4 w = vb[buf][(32 * d + lc) * 8 + ((2 * x + h) ^ ((lc >> 1) & 7))];
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), pf[x], o[d], 0, 0, 0);
+        }
+      if (past) {
+        unsigned long long odd = odd_keys[st % 3];
+#pragma unroll 1
+        for (; odd; odd &= odd - 1) {
+          const int key = key0 + __builtin_ctzll(odd);
+          const OddValue ov = odd_value<Q4>(a, sg, key);
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float v = __shfl(ov.v[d >> 1], 32 * (d & 1) + 8 * (i >> 2) + 4 * h + (i & 3), kWave);
+              o[d][i] += key <= lpos ? v : 0.f;
+            }
+        }
+      }
+    }
+    if (st + 1 < st1) store_step((st + 1) & 1, st + 1);
+  }
+  if (!owner) return;
+  l = pair_fold(l, [](float x, float y) { return x + y; });
+  if constexpr (SPLIT) {
+    const int64_t at = ((int64_t)blockIdx.x * a.nslots + blockIdx.y) * TQ + 32 * wave + lc;
+    float* po = a.part_o + at * kHd + 4 * h;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<float4_t*>(po + 32 * d + 8 * x) =
+            float4_t{o[d][4 * x], o[d][4 * x + 1], o[d][4 * x + 2], o[d][4 * x + 3]};
+    if (h == 0) a.part_ml[at] = make_float2(m, l);
+  } else {
+    if (wq + lc >= nq) return;
+    const int64_t pos = p0 + qj;
+    const bool bad = pos < 0 || pos >= a.len_bound;
+    const float inv = 1.f / l;
+    uint16_t* dst = a.out + ((int64_t)(sr.first + qj) * a.hq + g * G + (qi - qj * G)) * kHd + 4 * h;
+    const half_t nan = __builtin_bit_cast(half_t, kNanF16);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        half4_t v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = bad ? nan : (half_t)(o[d][4 * x + e] * inv);
+        *reinterpret_cast<half4_t*>(dst + 32 * d + 8 * x) = v;
+      }
+  }
+}
+
+// The parts of each query joined, in their order: a wavefront per query (lane t: dims 2 t, 2 t + 1).  Which parts hold
+// keys of the query's tile is what the kernels above decided, from the same numbers.  TQ: queries of an item (few rows:
+// the item is the sequence).
+template <bool FEW>
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int G = a.hq / a.hkv;
+  const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
+  int s = item, qt = 0;
+  if constexpr (!FEW) {
+    int t;
+    if (!find_tile(pr.b, item, [&](int i) { return (seq_rows(pr, i).n * G + TQ - 1) / TQ; }, s, t)) return;
+    qt = (seq_rows(pr, s).n * G + TQ - 1) / TQ - 1 - t;
+  }
+  const SeqRows sr = seq_rows(pr, s);
+  const int nq = sr.n * G, qx = blockIdx.y * 4 + wave, qi = qt * TQ + qx;
+  if (qx >= TQ || qi >= nq) return;
+  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
+  const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
+  const int64_t pl = p0 + qlast / G, klast = pl < a.len_bound ? pl : a.len_bound - 1;
+  const int nst = klast < 0 ? 0 : (int)(klast / kTile) + 1;
+  const int j = qi / G;
+  const int64_t base = (int64_t)blockIdx.x * a.nslots;
+  float M = kNoMax;
+  int parts = 0;
+  for (; parts < a.nslots; ++parts) {
+    int lo, hi;
+    slot_steps(nst, a.nslots, parts, FEW ? kFewWaves : 1, lo, hi);
+    if (lo >= hi && parts > 0) break;
+    M = fmaxf(M, a.part_ml[(base + parts) * TQ + qx].x);
+  }
+  float L = 0.f, x = 0.f, y = 0.f;
+  for (int i = 0; i < parts; ++i) {
+    const float2 ml = a.part_ml[(base + i) * TQ + qx];
+    const float2 v = *reinterpret_cast<const float2*>(a.part_o + ((base + i) * TQ + qx) * kHd + 2 * lane);
+    const float f = exp2_fast(ml.x - M);
+    L += f * ml.y;
+    x += f * v.x;
+    y += f * v.y;
+  }
+  const bool bad = p0 + j < 0 || p0 + j >= a.len_bound;
+  const half_t nan = __builtin_bit_cast(half_t, kNanF16);
+  half2_t r = {bad ? nan : (half_t)(x / L), bad ? nan : (half_t)(y / L)};
+  *reinterpret_cast<half2_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + 2 * lane) = r;
+}
+
+struct Plan {
+  bool few;
+  int tq, items, nslots;  // queries of an item, items, parts of the keys
+};
+
+Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
+  const int G = hq / hkv;
+  const int64_t steps = (len_bound + kTile - 1) / kTile;
+  Plan p;
+  p.few = (int64_t)pr.max_rows * G <= 64;
+  int64_t slots;
+  if (p.few) {
+    p.tq = pr.max_rows * G <= 16 ? 16 : (pr.max_rows * G <= 32 ? 32 : 64);
+    p.items = pr.b;
+    slots = 512 / ((int64_t)p.items * hkv);
+    const int64_t most = (steps + kFewWaves - 1) / kFewWaves;
+    slots = slots > most ? most : slots;
+  } else {
+    p.tq = 128;
+    const int64_t b = pr.b < pr.rows ? pr.b : pr.rows;
+    auto items = [&](int64_t tq) {
+      return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq : (int64_t)pr.b * (((int64_t)pr.max_rows * G + tq - 1) / tq);
+    };
+    if (items(256) * hkv >= 512) p.tq = 256;
+    p.items = (int)items(p.tq);
+    slots = items(p.tq) * hkv >= 256 ? 1 : 512 / (items(p.tq) * hkv);
+    slots = slots > steps / 4 ? steps / 4 : slots;
+  }
+  p.nslots = (int)(slots < 1 ? 1 : slots);
+  return p;
+}
+
+template <bool Q4>
+void launch_few(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
+  const dim3 block(64 * kFewWaves);
+  if (p.tq == 16)
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 1>), grid, block, 0, stream, pr, a);
+  else if (p.tq == 32)
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 2>), grid, block, 0, stream, pr, a);
+  else
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 4>), grid, block, 0, stream, pr, a);
+}
+
+template <bool Q4, int NW>
+void launch_prompt(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
+  if (p.nslots > 1)
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, NW, true>), grid, dim3(64 * NW), 0, stream, pr, a);
+  else
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, NW, false>), grid, dim3(64 * NW), 0, stream, pr, a);
+}
+
+}  // namespace
+
+hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int hq, int hkv, const int32_t* pos_base,
+                                   int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
+                                   uint16_t* out, hipStream_t stream) {
+  const Plan p = make_plan(pr, hq, hkv, len_bound);
+  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.nslots};
+  if (p.nslots > 1) {
+    const size_t queries = (size_t)p.items * hkv * p.nslots * p.tq;
+    void* ws = nullptr;
+    const hipError_t e = workspace(queries * (kHd * sizeof(float) + sizeof(float2)), stream, &ws);
+    if (e != hipSuccess) return e;
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + queries * kHd);
+  }
+  const bool q4 = cache.k4 != nullptr;
+  if (p.few) {
+    const dim3 grid((unsigned)p.nslots, (unsigned)(pr.b * hkv));
+    if (q4)
+      launch_few<true>(p, grid, pr, a, stream);
+    else
+      launch_few<false>(p, grid, pr, a, stream);
+    if (p.nslots > 1)
+      hipLaunchKernelGGL(packed_merge_kernel<true>, dim3((unsigned)(pr.b * hkv), (unsigned)(p.tq / 4)), dim3(256), 0,
+                         stream, pr, a, p.tq);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)(p.items * hkv), (unsigned)p.nslots);
+  if (p.tq == 256) {
+    if (q4)
+      launch_prompt<true, 8>(p, grid, pr, a, stream);
+    else
+      launch_prompt<false, 8>(p, grid, pr, a, stream);
+  } else {
+    if (q4)
+      launch_prompt<true, 4>(p, grid, pr, a, stream);
+    else
+      launch_prompt<false, 4>(p, grid, pr, a, stream);
+  }
+  if (p.nslots > 1)
+    hipLaunchKernelGGL(packed_merge_kernel<false>, dim3((unsigned)(p.items * hkv), (unsigned)(p.tq / 4)), dim3(256), 0,
+                       stream, pr, a, p.tq);
+  return hipGetLastError();
+}
+
+}  // namespace sq

@@ -202,4 +202,29 @@ hipError_t launch_spec_commit_multi(const int32_t* n_accepted, const int32_t* ne
                                     int32_t* pos_base, int32_t* out_tokens, int64_t out_capacity, int32_t* out_len,
                                     int32_t* status, hipStream_t stream);
 
+// Rows of b sequences packed one after the other: start [b + 1] (device), or null: max_rows rows each (packed.hip,
+// packed_attn.hip).
+struct PackedRows {
+  const int32_t* start;
+  int b, rows, max_rows;
+};
+// The caches of one layer: fp16 (k, v) or 4-bit (k4, ks, v4, vs; k4 null: fp16).
+struct KvCache {
+  uint16_t *k, *v;
+  uint8_t* k4;
+  uint16_t* ks;
+  uint8_t* v4;
+  uint16_t* vs;
+};
+hipError_t launch_packed_rope_kv(const float* qkv, const uint16_t* bias, const PackedRows& pr, int hq, int hkv,
+                                 const int32_t* pos_base, int pos_offset, int64_t len_bound, int64_t capacity,
+                                 double theta, uint16_t* q_out, const KvCache& cache, int32_t* status,
+                                 hipStream_t stream);
+hipError_t launch_packed_kv_read(const PackedRows& pr, int hkv, const int32_t* pos_base, int pos_offset,
+                                 int64_t len_bound, int64_t capacity, const KvCache& cache, uint16_t* k_out,
+                                 uint16_t* v_out, hipStream_t stream);
+hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int hq, int hkv, const int32_t* pos_base,
+                                   int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
+                                   uint16_t* out, hipStream_t stream);
+
 }  // namespace sq

@@ -1,0 +1,460 @@
+"""GPU checks of the calls over packed rows and the 4-bit cache (include/specquant_packed.h): the rotation and cache write
+against sq_rope_kv_f16 and the quantizer's formula in 64 bits, the attention against a 64-bit softmax, at lengths from
+none to thousands, odd sizes, every kernel and key split, stale and non-finite entries behind the mask."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_21704_amd as sq
+from paper_2609_21704_amd import _lib, synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+NAN = float("nan")
+I32, F16 = torch.int32, torch.float16
+
+
+def normal(shape, *seed, std=1.0):
+    return synth.normal_f16(shape, std, synth.stream_seed(71, *seed), torch.device(DEV))
+
+
+def starts(lens, lead=0):
+    s = [lead]
+    for n in lens:
+        s.append(s[-1] + n)
+    return torch.tensor(s, dtype=I32, device=DEV)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=I32, device=DEV)
+
+
+def empty_q4(b, hkv, cap):
+    return (torch.full((b, hkv, cap, 64), 0xA5, dtype=torch.uint8, device=DEV),
+            torch.full((b, hkv, cap, 4), NAN, dtype=F16, device=DEV),
+            torch.full((b, hkv, cap // 64, 64, 64), 0x5A, dtype=torch.uint8, device=DEV),
+            torch.full((b, hkv, cap // 64, 4, 64), NAN, dtype=F16, device=DEV))
+
+
+AT = [4 * (i // 4) + (0, 2, 1, 3)[i % 4] for i in range(64)]  # byte of element (position) i
+
+
+def values_q4(cache):
+    """[b][hkv][capacity][128] fp64 keys and values of a 4-bit cache, as the header lays them out."""
+    kc, ks, vc, vs = cache
+    b, h, cap, _ = kc.shape
+    vc = vc[..., AT].transpose(3, 4).reshape(b, h, cap, 64)
+    vs = vs.transpose(3, 4).reshape(b, h, cap, 4)
+
+    def val(c, s):
+        s = s.double()
+        v = torch.cat([((c & 15).double() - s[..., 1:2]) * s[..., 0:1], ((c >> 4).double() - s[..., 3:4]) * s[..., 2:3]], -1)
+        return v.float().half()
+
+    return val(kc[..., AT], ks), val(vc, vs)
+
+
+def quantized(w):
+    """What the 4-bit entry of fp16 vectors [..., 128] stands for, from the formula in fp64."""
+    x = w.double().reshape(*w.shape[:-1], 2, 64)
+    lo, hi = x.amin(-1, keepdim=True).clamp(max=0), x.amax(-1, keepdim=True).clamp(min=0)
+    want = (hi - lo) / 15
+    e = torch.floor(torch.log2(want.clamp(min=2.0 ** -40))).clamp(min=-14)
+    e = e + (torch.exp2(e + 1) <= want).double() - ((torch.exp2(e) > want) & (e > -14)).double()
+    ulp = torch.exp2(e - 10)
+    s = torch.where(want > 0, torch.ceil(want / ulp) * ulp, torch.ones_like(want))
+    z = torch.round(-lo / s).clamp(0, 15)
+    q = (torch.round(x / s) + z).clamp(0, 15) - z
+    q = torch.where((q * s).abs() >= 65520, q - q.sign(), q)
+    v = (q * s).reshape(w.shape).float().half()
+    bad = ~torch.isfinite(w.double()).reshape(x.shape).all(-1, keepdim=True).expand(x.shape).reshape(w.shape)
+    return torch.where(bad, torch.full_like(v, NAN), v), s, bad
+
+
+def same(a, b):
+    """The same bits, NaN for NaN."""
+    return torch.equal(torch.nan_to_num(a.float(), nan=7e8), torch.nan_to_num(b.float(), nan=7e8))
+
+
+# (rows, past) per sequence, hq, hkv, capacity, rows before and after them
+ROWS = [([(1, 0)], 4, 4, 64, 0, 0),
+        ([(1, 63), (1, 64)], 7, 1, 128, 0, 0),
+        ([(2, 1), (0, 5), (2, 126)], 28, 4, 128, 1, 2),
+        ([(17, 3), (1, 0), (0, 0), (40, 0), (16, 16), (5, 59)], 12, 2, 128, 2, 3),
+        ([(300, 0), (33, 1000), (129, 7)], 8, 8, 1088, 0, 5),
+        ([(1, i % 60) for i in range(150)], 3, 1, 64, 0, 1)]
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,cap,lead,tail", ROWS)
+@pytest.mark.parametrize("bias", [True, False])
+def test_rope_write(seqs, hq, hkv, cap, lead, tail, bias):
+    b, lens, past = len(seqs), [n for n, _ in seqs], [p for _, p in seqs]
+    rows = lead + sum(lens) + tail
+    qkv = normal((rows, (hq + 2 * hkv) * 128), 1, rows).float() * 1.37
+    bv = normal(((hq + 2 * hkv) * 128,), 2, hq) if bias else None
+    start, pos = starts(lens, lead), ints([p - 5 for p in past])
+    args = dict(max_rows=max(lens), pos_offset=5)
+    status = torch.zeros(1, dtype=I32, device=DEV)
+    k = torch.full((b, hkv, cap, 128), 3.0, dtype=F16, device=DEV)
+    v = torch.full((b, hkv, 128, cap), 5.0, dtype=F16, device=DEV)
+    q = torch.full((rows, hq, 128), 9.0, dtype=F16, device=DEV)
+    sq.sq_packed_rope_kv_f16(qkv, bv, start, pos, hq, k, v, q_out=q, status=status, **args)
+    # the block call, sequence by sequence and in blocks of up to 64 rows: the same bits, nothing else written
+    k2, v2, q2 = torch.full_like(k, 3.0), torch.full_like(v, 5.0), torch.full_like(q, 9.0)
+    for i, (n, p) in enumerate(seqs):
+        for r in range(0, n, 64):
+            m = min(64, n - r)
+            at = int(start[i]) + r
+            q2[at:at + m] = sq.sq_rope_kv_f16(qkv[at:at + m].contiguous(), bv, ints([p]), r, m, hq, k2[i:i + 1], v2[i:i + 1])
+    assert torch.equal(q, q2) and torch.equal(k, k2) and torch.equal(v, v2)
+
+    c = empty_q4(b, hkv, cap)
+    q4 = torch.full((rows, hq, 128), 9.0, dtype=F16, device=DEV)
+    sq.sq_packed_rope_kv_q4(qkv, bv, start, pos, hq, *c, q_out=q4, status=status, **args)
+    assert torch.equal(q4, q) and int(status) == 0
+    kv, vv = values_q4(c)
+    written = torch.zeros(b, cap, dtype=torch.bool, device=DEV)
+    for i, (n, p) in enumerate(seqs):
+        written[i, p:p + n] = True
+    at = written[:, None].expand(b, hkv, cap)
+    for got, entry in ((kv, k), (vv, v.transpose(2, 3))):
+        want, s, _ = quantized(entry[at])
+        assert same(got[at], want)
+        # half a step of the group's scale off, and half an ulp of the value
+        err = (want.double() - entry[at].double()).abs().reshape(-1, 2, 64)
+        assert bool((err <= s / 2 + want.double().abs().reshape(-1, 2, 64) * 2.0 ** -11 + 2.0 ** -25).all())
+        assert bool(torch.isnan(got[~at]).all())  # (untouched: NaN scales)
+    e = empty_q4(b, hkv, cap)
+    keep = ~written
+    assert torch.equal(c[0][keep[:, None].expand(b, hkv, cap)], e[0][keep[:, None].expand(b, hkv, cap)])
+    vb = keep[:, :, None].expand(b, cap, 64).reshape(b, cap // 64, 64, 64).transpose(2, 3)[:, None]
+    vb = vb.expand(c[2].shape)
+    assert torch.equal(c[2][..., AT][vb], e[2][..., AT][vb])
+    ko = torch.full((rows, hkv, 128), 9.0, dtype=F16, device=DEV)
+    vo = torch.full((rows, hkv, 128), 9.0, dtype=F16, device=DEV)
+    sq.sq_packed_kv_read_q4(*c, start, pos, rows, k_out=ko, v_out=vo, **args)
+    covered = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    for i, (n, p) in enumerate(seqs):
+        a0 = int(start[i])
+        covered[a0:a0 + n] = True
+        assert same(ko[a0:a0 + n], kv[i, :, p:p + n].transpose(0, 1)) and same(vo[a0:a0 + n], vv[i, :, p:p + n].transpose(0, 1))
+    assert bool((ko[~covered] == 9).all()) and bool((vo[~covered] == 9).all()) and bool((q[~covered] == 9).all())
+
+
+def test_special_groups():
+    """Groups of zeros, of one sign, of subnormals, of the largest values, with infinities and NaN: as values and as
+    keys at position 0, where the turn changes nothing but that an infinity or NaN times its sine of 0 reaches the other
+    element of its pair, and with it the other group."""
+    rows = torch.zeros(9, 128, device=DEV)
+    rows[1] = torch.linspace(1, 2, 128)
+    rows[2] = -torch.linspace(1e-3, 2, 128)
+    rows[3, ::3] = 6e-8
+    rows[3, 1::3] = -1.8e-7
+    rows[4] = torch.linspace(-65504, 65504, 128)
+    rows[5, :64], rows[5, 64:] = 65504, -65504
+    rows[6, 70] = float("inf")
+    rows[7, 3] = NAN
+    rows[8] = torch.linspace(-61000, 65504, 128).flip(0)
+    qkv = torch.cat([torch.zeros(9, 128, device=DEV), rows, rows], 1)
+    c = empty_q4(9, 1, 64)
+    sq.sq_packed_rope_kv_q4(qkv, None, None, ints([0] * 9), 1, *c)
+    want, _, bad = quantized(rows.half())
+    kv, vv = values_q4(c)
+    wk = want.clone()
+    wk[6:8] = NAN
+    assert same(kv[:, 0, 0], wk) and same(vv[:, 0, 0], want)
+    assert int(bad.sum()) == 128 and bool(torch.isfinite(want[~bad]).all())
+    ko, vo = sq.sq_packed_kv_read_q4(*c, None, ints([0] * 9), 9)
+    assert same(ko[:, 0], wk) and same(vo[:, 0], want)
+
+
+def test_bad_positions_and_rows():
+    hq, hkv, cap = 4, 2, 128
+    for q4 in (False, True):
+        cache = empty_q4(2, hkv, cap) if q4 else (torch.full((2, hkv, cap, 128), 3.0, dtype=F16, device=DEV),
+                                                   torch.full((2, hkv, 128, cap), 3.0, dtype=F16, device=DEV))
+        rope = sq.sq_packed_rope_kv_q4 if q4 else sq.sq_packed_rope_kv_f16
+        attn = sq.sq_packed_attention_q4 if q4 else sq.sq_packed_attention_f16
+        qkv = normal((9, (hq + 2 * hkv) * 128), 3).float()
+        before = [t.clone() for t in cache]
+        status = torch.zeros(1, dtype=I32, device=DEV)
+        # sequence 0 at -2, -1, 0, 1; sequence 1 at 98 .. 102 with a bound of 100
+        q = rope(qkv, None, starts([4, 5]), ints([-2, 98]), hq, *cache, max_rows=5, len_bound=100, status=status)
+        assert int(status) == _lib.DEV_BAD_POS
+        bad = torch.tensor([1, 1, 0, 0, 0, 0, 1, 1, 1], dtype=torch.bool, device=DEV)
+        assert torch.equal(torch.isnan(q).flatten(1).all(1), bad) and torch.equal(torch.isnan(q).flatten(1).any(1), bad)
+        if q4:
+            k, v = sq.sq_packed_kv_read_q4(*cache, starts([4, 5]), ints([-2, 98]), 9, max_rows=5, len_bound=100)
+            assert torch.equal(torch.isnan(k).flatten(1).any(1), bad) and torch.equal(torch.isnan(v).flatten(1).all(1), bad)
+            assert torch.equal(cache[0][:, :, 100:], before[0][:, :, 100:])
+        else:
+            assert torch.equal(cache[0][:, :, 100:], before[0][:, :, 100:])
+            assert torch.equal(cache[1][..., 100:], before[1][..., 100:])
+        # sequence 1 reads entries 0 .. 97 nothing wrote: finite ones for this
+        rope(normal((98, (hq + 2 * hkv) * 128), 4).float(), None, ints([0, 0, 98]), ints([0, 0]), hq, *cache)
+        for most in (5, 40):  # both kernels
+            out = attn(torch.where(bad[:, None, None], torch.ones_like(q), q), *cache, starts([4, 5]), ints([-2, 98]), max_rows=most, len_bound=100)
+            assert torch.equal(torch.isnan(out).flatten(1).any(1), bad) and torch.equal(torch.isnan(out).flatten(1).all(1), bad)
+        for wrong, most in (([0, 6, 3], 9), ([-1, 4, 9], 9), ([0, 4, 10], 9), ([0, 4, 9], 4)):
+            status.zero_()
+            rope(qkv, None, ints(wrong), ints([3, 20]), hq, *cache, max_rows=most, status=status)
+            assert int(status) == _lib.DEV_BAD_ROWS
+            attn(q.nan_to_num(), *cache, ints(wrong), ints([3, 20]), max_rows=most)
+
+
+def attention_case(seqs, hq, hkv, cap, seed, std=1.3):
+    b, rows = len(seqs), sum(n for n, _ in seqs)
+    q = normal((rows, hq, 128), seed, rows, std=std)
+    k, v = normal((b, hkv, cap, 128), seed, 1), normal((b, hkv, cap, 128), seed, 2)
+    return q, k, v
+
+
+def pack_q4(k, v):
+    """The 4-bit cache of given keys and values [b][hkv][capacity][128], written by the library: keys as values, which are
+    not rotated."""
+    b, hkv, cap, _ = k.shape
+    cache = empty_q4(b, hkv, cap)
+    ks = empty_q4(b, hkv, cap)
+    for w, dst in ((v, cache), (k, ks)):
+        u = torch.zeros(b, cap, 3, hkv, 128, device=DEV)
+        u[:, :, 2] = w.transpose(1, 2).float()
+        sq.sq_packed_rope_kv_q4(u.reshape(b * cap, -1), None, None, ints([0] * b), hkv, *dst)
+    kc = ks[2][..., AT].transpose(3, 4).reshape(b, hkv, cap, 64)[..., AT]  # (the exchange is its own inverse)
+    return kc.contiguous(), ks[3].transpose(3, 4).reshape(b, hkv, cap, 4).contiguous(), cache[2], cache[3]
+
+
+def check_attention(out, q, k, v, seqs, lead=0):
+    """Against a softmax in 64 bits.  A score: 128 fp32 terms of exact products, scaled, and two more roundings; its error
+    moves every weight.  A weight: binary16, half an ulp (2^-11), or 2^-32 of the largest; exponentials and fp32 sums to 2^-18.
+    The result: binary16."""
+    hq, hkv = q.shape[1], k.shape[1]
+    g = hq // hkv
+    at = lead
+    for i, (n, p) in enumerate(seqs):
+        if n == 0:
+            continue
+        keys = p + n
+        kd, vd = k[i, :, :keys].double(), v[i, :, :keys].double()
+        kt, ka = kd.transpose(1, 2).contiguous(), kd.abs().transpose(1, 2).contiguous()
+        for r in range(0, n, 512):
+            m = min(512, n - r)
+            qd = q[at + r:at + r + m].double().view(m, hkv, g, 128).permute(1, 0, 2, 3).reshape(hkv, m * g, 128).contiguous()
+            s = torch.matmul(qd, kt) / math.sqrt(128)
+            mask = torch.arange(keys, device=DEV)[None] > (p + r + torch.arange(m, device=DEV).repeat_interleave(g))[:, None]
+            s = s.masked_fill(mask, -math.inf)
+            w = torch.softmax(s, -1)
+            ref, mag = torch.matmul(w, vd), torch.matmul(w, vd.abs())
+            dot = (torch.matmul(qd.abs(), ka) / math.sqrt(128)).masked_fill(mask, 0).amax(-1, keepdim=True)
+            bound = mag * (2 * dot * 132 * 2.0 ** -24 + 2.0 ** -11 + 2.0 ** -18) + keys * 2.0 ** -32 * vd.abs().amax()
+            bound = bound + ref.abs() * 2.0 ** -11 + 2.0 ** -25
+            got = out[at + r:at + r + m].double().view(m, hkv, g, 128).permute(1, 0, 2, 3).reshape(hkv, m * g, 128)
+            assert bool(((got - ref).abs() <= bound).all()), (i, r, float(((got - ref).abs() / bound).max()))
+        at += n
+
+
+# (rows, past) per sequence, hq, hkv, capacity: few queries (one, two and four tiles of 16; one part and many), many (128 and
+# 256 queries a workgroup, one part and many); tiles and steps met, missed and crossed by one
+ATTN = [([(1, 0)], 1, 1, 64), ([(1, 63)], 16, 1, 64), ([(1, 64), (1, 0), (1, 127)], 28, 4, 128),
+        ([(1, 700), (0, 3), (1, 4095), (1, 255)], 12, 2, 4096), ([(2, 31), (1, 1000), (2, 318)], 28, 4, 1088),
+        ([(4, 60), (3, 2044)], 8, 1, 2048), ([(9, 0), (9, 500), (8, 55)], 28, 4, 576), ([(64, 0)], 1, 1, 64),
+        ([(5, 3000)], 48, 4, 3008), ([(1, 19)] * 70, 8, 8, 64),
+        ([(65, 0)], 1, 1, 128), ([(19, 45), (1, 3)], 28, 4, 64), ([(100, 0), (0, 0), (1, 0), (64, 64), (37, 1)], 28, 4, 128),
+        ([(57, 8000), (17, 333)], 28, 4, 8064), ([(130, 62)], 7, 1, 192), ([(255, 1), (257, 0)], 1, 1, 320),
+        ([(900, 0), (331, 12)], 40, 8, 960), ([(2300, 0)], 28, 4, 2304), ([(700, 0), (1300, 0), (90, 500)], 16, 16, 1344),
+        ([(3, 0)] * 80, 28, 1, 64)]
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,cap", ATTN)
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_attention(seqs, hq, hkv, cap, fmt):
+    b, most = len(seqs), max(n for n, _ in seqs)
+    q, k, v = attention_case(seqs, hq, hkv, cap, 11)
+    pos = ints([p for _, p in seqs])
+    start = starts([n for n, _ in seqs])
+    out = torch.full_like(q, 9.0)
+    if fmt == "f16":
+        vt = v.transpose(2, 3).contiguous()
+        for i, (n, p) in enumerate(seqs):  # what follows the last row's entry may hold anything
+            k[i, :, p + n:] = NAN
+            vt[i, :, :, p + n:] = float("inf")
+        sq.sq_packed_attention_f16(q, k, vt, start, pos, max_rows=most, out=out)
+        again = sq.sq_packed_attention_f16(q, k, vt, start, pos, max_rows=most)
+    else:
+        cache = pack_q4(k, v)
+        k, v = values_q4(cache)
+        assert same(k, quantized(normal((b, hkv, cap, 128), 11, 1))[0])
+        for i, (n, p) in enumerate(seqs):
+            cache[1][i, :, p + n:] = NAN
+            cache[3][i].transpose(2, 3).reshape(hkv, cap, 4)
+            blocks = cache[3][i].transpose(2, 3).reshape(hkv, cap, 4).clone()
+            blocks[:, p + n:] = NAN
+            cache[3][i] = blocks.view(hkv, cap // 64, 64, 4).transpose(2, 3)
+        sq.sq_packed_attention_q4(q, *cache, start, pos, max_rows=most, out=out)
+        again = sq.sq_packed_attention_q4(q, *cache, start, pos, max_rows=most)
+    assert torch.equal(out, again)  # the same bits every time
+    check_attention(out, q, k, v, seqs)
+    if len({n for n, _ in seqs}) == 1:  # without row_start
+        u = (sq.sq_packed_attention_f16(q, k, vt, None, pos) if fmt == "f16" else
+             sq.sq_packed_attention_q4(q, *cache, None, pos))
+        assert torch.equal(u, out)
+
+
+@pytest.mark.parametrize("rows,past", [(3, 61), (40, 100), (200, 0)])
+def test_later_entries_do_not_reach_earlier_rows(rows, past):
+    """A value that is not finite in a row's own block reaches the rows from its position on and no other, in its own
+    dimension; so does a key of NaN."""
+    hq, hkv, cap = 14, 2, 320
+    q, k, v = attention_case([(rows, past)], hq, hkv, cap, 13)
+    clean = sq.sq_packed_attention_f16(q, k, v.transpose(2, 3).contiguous(), starts([rows]), ints([past]))
+    at = rows // 2
+    v2 = v.clone()
+    v2[0, 0, past + at, 5] = float("inf")
+    v2[0, 0, past + at, 70] = NAN
+    out = sq.sq_packed_attention_f16(q, k, v2.transpose(2, 3).contiguous(), starts([rows]), ints([past]))
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[at:, :hq // hkv, 5] = hit[at:, :hq // hkv, 70] = True
+    assert torch.equal(~torch.isfinite(out), hit)
+    assert torch.equal(out[~hit], clean[~hit])
+    k2 = k.clone()
+    k2[0, 1, past + at, 9] = NAN
+    out = sq.sq_packed_attention_f16(q, k2, v.transpose(2, 3).contiguous(), starts([rows]), ints([past]))
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[at:, hq // hkv:] = True
+    assert torch.equal(torch.isnan(out), hit) and torch.equal(out[~hit], clean[~hit])
+    cache = pack_q4(k, v)
+    clean = sq.sq_packed_attention_q4(q, *cache, starts([rows]), ints([past]))
+    vs = cache[3].transpose(3, 4).reshape(1, hkv, cap, 4).clone()
+    vs[0, 0, past + at, 2] = NAN  # elements 64 .. 127 of one value
+    cache = (*cache[:3], vs.view(1, hkv, cap // 64, 64, 4).transpose(3, 4).contiguous())
+    out = sq.sq_packed_attention_q4(q, *cache, starts([rows]), ints([past]))
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[at:, :hq // hkv, 64:] = True
+    assert torch.equal(torch.isnan(out), hit) and torch.equal(out[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("rows,past", [(1, 500), (9, 2000), (150, 900)])
+def test_extreme_scores(rows, past):
+    """Scores far apart, growing with the position and falling with it, equal ones, and -inf from infinite keys: the
+    reference maximum moves every step, once, or never."""
+    hq, hkv, cap = 8, 2, 2112
+    n = past + rows
+    q, k, v = attention_case([(rows, past)], hq, hkv, cap, 17)
+    ramp = torch.linspace(0, 40, n, device=DEV)
+    for way in ("up", "down", "flat", "far"):
+        kk, qq = k.clone(), q.clone()
+        if way == "flat":
+            kk[:] = kk[:, :, :1]
+        else:
+            qq[..., 0] = 8.0
+            kk[0, :, :n, 0] = (ramp if way == "up" else ramp.flip(0)).half() * (6 if way == "far" else 1)
+        out = sq.sq_packed_attention_f16(qq, kk, v.transpose(2, 3).contiguous(), starts([rows]), ints([past]))
+        check_attention(out, qq, kk, v, [(rows, past)])
+    kk = k.clone()
+    qq = q.clone()
+    qq[..., 0] = 1.0
+    kk[0, :, 3:past, 0] = -float("inf")  # weight zero
+    out = sq.sq_packed_attention_f16(qq, kk, v.transpose(2, 3).contiguous(), starts([rows]), ints([past]))
+    keep = [0, 1, 2, *range(past, n)]
+    ks, vs = torch.zeros_like(k), torch.zeros_like(v)
+    ks[:, :, :len(keep)], vs[:, :, :len(keep)] = k[:, :, keep], v[:, :, keep]
+    check_attention(out, qq, ks, vs, [(rows, 3)])
+
+
+def test_long_cache_offsets():
+    """Entries whose byte offsets pass 32 bits: the last sequence of a cache of more than 4 GiB, both formats."""
+    b, hkv, cap, rows = 17, 8, 131072, 3
+    n = 4000
+    pos = ints([0] * (b - 1) + [cap - rows])
+    lens = [0] * (b - 1) + [rows]
+    qkv = normal((rows, (8 + 2 * hkv) * 128), 21).float()
+    k = torch.zeros((b, hkv, cap, 128), dtype=F16, device=DEV)
+    vt = torch.zeros((b, hkv, 128, cap), dtype=F16, device=DEV)
+    k[-1, :, -n:] = normal((hkv, n, 128), 22)
+    vt[-1, :, :, -n:] = normal((hkv, 128, n), 23)
+    assert k.numel() * 2 > 1 << 32
+    q = sq.sq_packed_rope_kv_f16(qkv, None, starts(lens), pos, 8, k, vt, max_rows=rows)
+    out = sq.sq_packed_attention_f16(q, k, vt, starts(lens), pos, max_rows=rows)
+    check_attention(out, q, k[-1:], vt[-1:].transpose(2, 3), [(rows, cap - rows)])
+    many = sq.sq_packed_attention_f16(q, k, vt, starts(lens), pos, max_rows=70)
+    check_attention(many, q, k[-1:], vt[-1:].transpose(2, 3), [(rows, cap - rows)])
+
+
+def test_long_cache_offsets_q4():
+    b, hkv, cap, rows = 66, 8, 131072, 2
+    c = (torch.zeros((b, hkv, cap, 64), dtype=torch.uint8, device=DEV), torch.zeros((b, hkv, cap, 4), dtype=F16, device=DEV),
+         torch.zeros((b, hkv, cap // 64, 64, 64), dtype=torch.uint8, device=DEV),
+         torch.zeros((b, hkv, cap // 64, 4, 64), dtype=F16, device=DEV))
+    assert c[0].numel() > 1 << 32
+    lens, first = [0] * (b - 1) + [200], [0] * (b - 1) + [cap - 202]
+    qkv = normal((200, (8 + 2 * hkv) * 128), 24).float()
+    sq.sq_packed_rope_kv_q4(qkv, None, starts(lens), ints(first), 8, *c)
+    lens[-1], first[-1] = rows, cap - rows
+    q = sq.sq_packed_rope_kv_q4(qkv[:rows].contiguous(), None, starts(lens), ints(first), 8, *c, max_rows=rows)
+    out = sq.sq_packed_attention_q4(q, *c, starts(lens), ints(first), max_rows=rows)
+    k, v = values_q4([t[-1:] for t in c])
+    check_attention(out, q, k, v, [(rows, cap - rows)])
+    ko, _ = sq.sq_packed_kv_read_q4(*c, starts(lens), ints(first), rows, max_rows=rows)
+    assert same(ko, k[0, :, -rows:].transpose(0, 1))
+
+
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_pass_captured(fmt):
+    """A prompt, then single tokens, as a decoder makes them: the tokens' calls recorded in a graph that moves the positions
+    on the device, on a stream of its own; every replay against the eager calls."""
+    hq, hkv, cap, lens = 14, 2, 512, [130, 7, 64]
+    b, rows = len(lens), sum(lens)
+
+    def cache():
+        if fmt == "q4":
+            return empty_q4(b, hkv, cap)
+        return (torch.zeros((b, hkv, cap, 128), dtype=F16, device=DEV), torch.zeros((b, hkv, 128, cap), dtype=F16, device=DEV))
+
+    rope = sq.sq_packed_rope_kv_q4 if fmt == "q4" else sq.sq_packed_rope_kv_f16
+    attn = sq.sq_packed_attention_q4 if fmt == "q4" else sq.sq_packed_attention_f16
+    qkv = normal((rows, (hq + 2 * hkv) * 128), 31).float()
+    tok = normal((4, b, (hq + 2 * hkv) * 128), 32).float()
+    c1, c2 = cache(), cache()
+    for c in (c1, c2):
+        q = rope(qkv, None, starts(lens), ints([0] * b), hq, *c)
+        attn(q, *c, starts(lens), ints([0] * b), max_rows=130)
+    one = starts([1] * b)
+    eager = []
+    pos = ints(lens)
+    for i in range(4):
+        q = rope(tok[i], None, one, pos, hq, *c1, max_rows=1)
+        eager.append(attn(q, *c1, one, pos, max_rows=1))
+        pos = pos + 1
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    x, p = tok[0].clone(), ints(lens)
+    q, out = torch.empty((b, hq, 128), dtype=F16, device=DEV), torch.empty((b, hq, 128), dtype=F16, device=DEV)
+    with torch.cuda.stream(side):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            rope(x, None, one, p, hq, *c2, max_rows=1, q_out=q)
+            attn(q, *c2, one, p, max_rows=1, out=out)
+            p += 1
+    torch.cuda.synchronize()
+    for i in range(4):
+        x.copy_(tok[i])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[i]), i
+    for a, bb in zip(c1, c2):
+        assert same(a, bb)
+
+
+def test_strided_and_other_tensors_are_refused():
+    q = normal((4, 4, 128), 41)
+    k, v = normal((1, 2, 64, 128), 42), normal((1, 2, 128, 64), 43)
+    start, pos = starts([4]), ints([0])
+    with pytest.raises(ValueError, match="contiguous"):
+        sq.sq_packed_attention_f16(normal((4, 8, 128), 44)[:, ::2], k, v, start, pos)
+    with pytest.raises(ValueError, match="GPU"):
+        sq.sq_packed_attention_f16(q, k, v, start.cpu(), pos)
+    with pytest.raises(_lib.SpecQuantError, match="SHAPE"):
+        sq.sq_packed_attention_f16(normal((4, 3, 128), 45), k, v, start, pos)
+    with pytest.raises(_lib.SpecQuantError, match="ALIAS"):
+        sq.sq_packed_attention_f16(q, k, v, start, pos, out=q)
+    assert sq.sq_packed_attention_f16(q[:0], k, v, starts([0]), pos).shape == (0, 4, 128)
