@@ -157,16 +157,23 @@ __device__ __forceinline__ half8_t tame(half8_t f, int left, uint32_t& odd) {
 // for all the queries (NQT tiles of 16), and meet in LDS.  v_mfma_f32_16x16x32_f16: lane l holds row / column li = l %
 // 16 and k = 8 lg .. +8 (lg = l / 16); D[4 lg + i][li].  Row r of the key tile kt is key 16 (r / 4) + 4 kt + r % 4, so a
 // lane ends with the scores of keys 16 lg .. 16 lg + 15 of query li, and takes the values of those keys as they lie.
-constexpr int kFewWaves = 4;
+// A step's keys are loaded while the step before takes its values, and the other way round, each into the registers that
+// were just used (fp16 and two tiles: the registers do not hold both, and a step's loads are issued at its start).  Up to
+// 32 queries: all eight wavefronts take keys; up to 64: half of them the first 32, half the rest, over the same keys.
+constexpr int kFewWaves = 8;
 
-template <bool Q4, int NQT>
-__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(NQT > 2 ? 1 : 2))) void few_attn_kernel(PackedRows pr, AttnArgs a) {
-  __shared__ __align__(16) float ob[kFewWaves][16][kHd + 4];
-  __shared__ float2 ml[kFewWaves][16];
+template <bool Q4, int NQT, int HALVES>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2))) void few_attn_kernel(PackedRows pr,
+                                                                                                        AttnArgs a) {
+  constexpr int NW = kFewWaves / HALVES;  // wavefronts that share the keys of a half's queries
+  constexpr bool kAhead = Q4 || NQT == 1;
+  __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
+  __shared__ float2 ml[kFewWaves][16 * NQT];
   const int slot = blockIdx.x, s = blockIdx.y / a.hkv, g = blockIdx.y - s * a.hkv;
   const int64_t sg = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 % NW;
+  const int q0 = wave8 / NW * (16 * NQT);  // the wavefront's first query
   const int G = a.hq / a.hkv;
   const SeqRows sr = seq_rows(pr, s);
   const int nq = sr.n * G;
@@ -176,14 +183,14 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   const int64_t klast = pl < a.len_bound ? pl : a.len_bound - 1;  // (rows past the bound are not computed)
   const int nst = klast < 0 ? 0 : (int)(klast / kTile) + 1;
   int st0, st1;
-  slot_steps(nst, a.nslots, slot, kFewWaves, st0, st1);
+  slot_steps(nst, a.nslots, slot, NW, st0, st1);
   if (st0 >= st1 && slot > 0) return;  // the part has no keys (part 0 always answers: rows without any key)
 
   half8_t qf[NQT][4];
   int lpos[NQT];  // the position of this lane's query, clipped to [-1, 2^31)
 #pragma unroll
   for (int t = 0; t < NQT; ++t) {
-    const int qi = 16 * t + li, qc = qi < nq ? qi : nq - 1;
+    const int qi = q0 + 16 * t + li, qc = qi < nq ? qi : nq - 1;
     const int j = qc / G;
     const uint16_t* qp = a.q + ((int64_t)(sr.first + j) * a.hq + g * G + (qc - j * G)) * kHd;
 #pragma unroll
@@ -202,61 +209,79 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     for (int d = 0; d < 8; ++d) o[t][d] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
   const int krow = 16 * (li >> 2) + (li & 3);  // + 4 kt: this lane's key of a tile
-  for (int st = st0 + wave; st < st1; st += kFewWaves) {
-    const int64_t key0 = (int64_t)st * kTile;
-    float4_t sc[NQT][4];
-    u32x4 vw[Q4 ? 4 : 16];  // 4-bit: codes of byte row 16 j + li; fp16: positions 16 lg .. +16 of dim 16 d + li
-    ValScales vs;
-    if constexpr (Q4) {
-      u32x4 kw[4];
-      uint2 ksz[4];
+  u32x4 kw[Q4 ? 4 : 16], vw[Q4 ? 4 : 16];  // 4-bit: a key's 16 bytes lg, byte rows 16 j + li; fp16: 32 lg .. +32 of a
+  uint2 ksz[4];                            // key, positions 16 lg .. +16 of dim 16 d + li
+  ValScales vs;
+  auto load_k = [&](int st) {
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const int64_t e = sg * a.capacity + key0 + krow + 4 * kt;
+    for (int kt = 0; kt < 4; ++kt) {
+      const int64_t e = sg * a.capacity + (int64_t)st * kTile + krow + 4 * kt;
+      if constexpr (Q4) {
         kw[kt] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + lg];
         ksz[kt] = reinterpret_cast<const uint2*>(a.c.ks)[e];
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) kw[4 * kt + x] = *reinterpret_cast<const u32x4*>(a.c.k + e * kHd + 32 * lg + 8 * x);
       }
-      vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * lg);
+    }
+  };
+  auto load_vs = [&](int st) { vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * lg); };
+  auto load_v = [&](int st) {
+    if constexpr (Q4) {
+      if constexpr (NQT == 1) load_vs(st);  // (two tiles: within the step, the registers again)
+      const uint8_t* vp = a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 + li * 64 + 16 * lg;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        vw[j] = *reinterpret_cast<const u32x4*>(a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 +
-                                                (16 * j + li) * 64 + 16 * lg);
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        half8_t lo[2], hi[2];
-        dequant_key(kw[kt], ksz[kt], lo, hi);
-#pragma unroll
-        for (int t = 0; t < NQT; ++t) {
-          float4_t acc = {0.f, 0.f, 0.f, 0.f};
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[0], qf[t][0], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[1], qf[t][1], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[0], qf[t][2], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[1], qf[t][3], acc, 0, 0, 0);
-          sc[t][kt] = acc;
-        }
-      }
+      for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(vp + 1024 * j);
     } else {
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const uint16_t* kp = a.c.k + (sg * a.capacity + key0 + krow + 4 * kt) * kHd + 32 * lg;
-        half8_t kf[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) kf[x] = *reinterpret_cast<const half8_t*>(kp + 8 * x);
-#pragma unroll
-        for (int t = 0; t < NQT; ++t) {
-          float4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x], qf[t][x], acc, 0, 0, 0);
-          sc[t][kt] = acc;
-        }
-      }
-#pragma unroll
       for (int d = 0; d < 8; ++d) {
-        const uint16_t* vp = a.c.v + (sg * kHd + 16 * d + li) * a.capacity + key0 + 16 * lg;
+        const uint16_t* vp = a.c.v + (sg * kHd + 16 * d + li) * a.capacity + (int64_t)st * kTile + 16 * lg;
         vw[2 * d] = *reinterpret_cast<const u32x4*>(vp);
         vw[2 * d + 1] = *reinterpret_cast<const u32x4*>(vp + 8);
       }
     }
+  };
+  const int end = HALVES == 1 || q0 < nq ? st1 : 0;
+  if (kAhead && st0 + wave < end) {
+    load_k(st0 + wave);
+    load_v(st0 + wave);
+  }
+  for (int st = st0 + wave; st < end; st += NW) {
+    const int64_t key0 = (int64_t)st * kTile;
+    const int next = st + NW < st1 ? st + NW : st;  // (the last step's loads are repeated: no branch around loads)
+    float4_t sc[NQT][4];
+    if constexpr (!kAhead) {
+      load_k(st);
+      load_v(st);
+    }
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      half8_t kf[4];
+      if constexpr (Q4) {
+        half8_t lo[2], hi[2];
+        dequant_key(kw[kt], ksz[kt], lo, hi);
+        kf[0] = lo[0];
+        kf[1] = lo[1];
+        kf[2] = hi[0];
+        kf[3] = hi[1];
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const u32x4 w = kw[4 * kt + x];
+          kf[x] = __builtin_bit_cast(half8_t, w);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NQT; ++t) {
+        float4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x], qf[t][x], acc, 0, 0, 0);
+        sc[t][kt] = acc;
+      }
+    }
+    if constexpr (Q4 && NQT > 1) load_vs(st);
+    if constexpr (kAhead) load_k(next);
+    __builtin_amdgcn_sched_barrier(0);
     // only a step past the first row's position holds keys that some row may not read
     const bool tail = key0 + kTile - 1 > p0;  // uniform
     half8_t pf[NQT][2];
@@ -325,6 +350,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         product(d, __builtin_bit_cast(half8_t, w0), __builtin_bit_cast(half8_t, w1));
       }
     }
+    if constexpr (kAhead) load_v(next);
+    __builtin_amdgcn_sched_barrier(0);
     if (tail && __any(odd != 0)) {
 #pragma unroll 1
       for (int key = 0; key < kTile; ++key) {
@@ -341,37 +368,33 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       }
     }
   }
-  // the wavefronts' sums meet, a query tile at a time
-  const int nq_pad = 16 * NQT;
-#pragma unroll 1
+  // the wavefronts' sums meet
+  const int nq_pad = 16 * NQT * HALVES;
+#pragma unroll
   for (int t = 0; t < NQT; ++t) {
-    if (16 * t >= nq) break;  // uniform
-    if (t) __syncthreads();
-    float mt = 0.f, lt = 0.f;
-    float4_t ot[8];
+    const float lt = quad_sum(l[t]);
+    if (lg == 0) ml[wave8][16 * t + li] = make_float2(m[t], lt);
 #pragma unroll
-    for (int x = 0; x < NQT; ++x)
-      if (x == t) {
-        mt = m[x];
-        lt = l[x];
+    for (int d = 0; d < 8; ++d) *reinterpret_cast<float4_t*>(&ob[wave8][16 * t + li][16 * d + 4 * lg]) = o[t][d];
+  }
+  __syncthreads();
+  for (int qi = tid >> 4; qi < nq; qi += 4 * kFewWaves) {
+    const int d0 = 8 * (tid & 15), w0 = qi / (16 * NQT) * NW, qx = qi & (16 * NQT - 1);
+    float M = kNoMax, L = 0.f, r[8] = {};
 #pragma unroll
-        for (int d = 0; d < 8; ++d) ot[d] = o[x][d];
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w0 + w][qx].x);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float2 x = ml[w0 + w][qx];
+      const float f = exp2_fast(x.x - M);
+      L += f * x.y;
+      const float4_t u = *reinterpret_cast<const float4_t*>(&ob[w0 + w][qx][d0]);
+      const float4_t v = *reinterpret_cast<const float4_t*>(&ob[w0 + w][qx][d0 + 4]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r[i] += f * u[i];
+        r[4 + i] += f * v[i];
       }
-    lt = quad_sum(lt);
-    if (lg == 0) ml[wave][li] = make_float2(mt, lt);
-#pragma unroll
-    for (int d = 0; d < 8; ++d) *reinterpret_cast<float4_t*>(&ob[wave][li][16 * d + 4 * lg]) = ot[d];
-    __syncthreads();
-    const int qr = tid >> 4, d0 = 8 * (tid & 15), qi = 16 * t + qr;
-    float M = kNoMax, L = 0.f, f[kFewWaves], r[8] = {};
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, ml[w][qr].x);
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-      f[w] = exp2_fast(ml[w][qr].x - M);
-      L += f[w] * ml[w][qr].y;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) r[x] += f[w] * ob[w][qr][d0 + x];
     }
     if (a.part_o) {
       const int64_t at = (sg * a.nslots + slot) * nq_pad + qi;
@@ -379,7 +402,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       po[0] = float4_t{r[0], r[1], r[2], r[3]};
       po[1] = float4_t{r[4], r[5], r[6], r[7]};
       if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
-    } else if (qi < nq) {
+    } else {
       const int j = qi / G;
       const int64_t pos = p0 + j;
       const bool bad = pos < 0 || pos >= a.len_bound;
@@ -649,11 +672,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// The parts of each query joined, in their order: a wavefront per query (lane t: dims 2 t, 2 t + 1).  Which parts hold
-// keys of the query's tile is what the kernels above decided, from the same numbers.  TQ: queries of an item (few rows:
-// the item is the sequence).
+// The parts of each query joined, in their order: a wavefront per query, lane i the weight of part i (at most 512 parts:
+// eight a lane), then every lane two dimensions, eight parts' sums in flight.  Which parts hold keys of the query's tile
+// is what the kernels above decided, from the same numbers.  TQ: queries of an item (few rows: the item is the
+// sequence); grain: the steps that a part's are a multiple of.
 template <bool FEW>
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ) {
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int G = a.hq / a.hkv;
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
@@ -670,25 +694,48 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
   const int64_t pl = p0 + qlast / G, klast = pl < a.len_bound ? pl : a.len_bound - 1;
   const int nst = klast < 0 ? 0 : (int)(klast / kTile) + 1;
-  const int j = qi / G;
+  int span, parts;
+  slot_steps(nst, a.nslots, 0, grain, parts, span);  // part 0: steps 0 .. span
+  parts = span > 0 ? (nst + span - 1) / span : 1;
   const int64_t base = (int64_t)blockIdx.x * a.nslots;
-  float M = kNoMax;
-  int parts = 0;
-  for (; parts < a.nslots; ++parts) {
-    int lo, hi;
-    slot_steps(nst, a.nslots, parts, FEW ? kFewWaves : 1, lo, hi);
-    if (lo >= hi && parts > 0) break;
-    M = fmaxf(M, a.part_ml[(base + parts) * TQ + qx].x);
+  constexpr int kMost = 8;
+  float2 ml[kMost];
+  float M = kNoMax, L = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int p = 64 * i + lane;
+    ml[i] = make_float2(kNoMax, 0.f);
+    if (p < parts) ml[i] = a.part_ml[(base + p) * TQ + qx];
+    M = fmaxf(M, ml[i].x);
   }
-  float L = 0.f, x = 0.f, y = 0.f;
-  for (int i = 0; i < parts; ++i) {
-    const float2 ml = a.part_ml[(base + i) * TQ + qx];
-    const float2 v = *reinterpret_cast<const float2*>(a.part_o + ((base + i) * TQ + qx) * kHd + 2 * lane);
-    const float f = exp2_fast(ml.x - M);
-    L += f * ml.y;
-    x += f * v.x;
-    y += f * v.y;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, kWave));
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    ml[i].x = exp2_fast(ml[i].x - M);
+    L += ml[i].x * ml[i].y;
   }
+  L = wave_sum(L);
+  float x = 0.f, y = 0.f;
+  const float* po = a.part_o + (base * TQ + qx) * kHd + 2 * lane;
+  for (int p0i = 0; p0i < parts; p0i += 8) {
+    float2 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = p0i + i < parts ? p0i + i : parts - 1;
+      v[i] = *reinterpret_cast<const float2*>(po + (int64_t)p * TQ * kHd);
+    }
+    float fw = ml[0].x;
+#pragma unroll
+    for (int i = 1; i < kMost; ++i) fw = (p0i >> 6) == i ? ml[i].x : fw;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = p0i + i < parts ? __shfl(fw, (p0i & 63) + i, kWave) : 0.f;
+      x += p0i + i < parts ? f * v[i].x : 0.f;
+      y += p0i + i < parts ? f * v[i].y : 0.f;
+    }
+  }
+  const int j = qi / G;
   const bool bad = p0 + j < 0 || p0 + j >= a.len_bound;
   const half_t nan = __builtin_bit_cast(half_t, kNanF16);
   half2_t r = {bad ? nan : (half_t)(x / L), bad ? nan : (half_t)(y / L)};
@@ -697,7 +744,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
 
 struct Plan {
   bool few;
-  int tq, items, nslots;  // queries of an item, items, parts of the keys
+  int tq, items, nslots, grain;  // queries of an item, items, parts of the keys, steps that a part's are a multiple of
 };
 
 Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
@@ -709,11 +756,13 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
   if (p.few) {
     p.tq = pr.max_rows * G <= 16 ? 16 : (pr.max_rows * G <= 32 ? 32 : 64);
     p.items = pr.b;
-    slots = 512 / ((int64_t)p.items * hkv);
-    const int64_t most = (steps + kFewWaves - 1) / kFewWaves;
+    p.grain = p.tq > 32 ? kFewWaves / 2 : kFewWaves;
+    slots = 256 / ((int64_t)p.items * hkv);
+    const int64_t most = (steps + p.grain - 1) / p.grain;
     slots = slots > most ? most : slots;
   } else {
     p.tq = 128;
+    p.grain = 1;
     const int64_t b = pr.b < pr.rows ? pr.b : pr.rows;
     auto items = [&](int64_t tq) {
       return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq : (int64_t)pr.b * (((int64_t)pr.max_rows * G + tq - 1) / tq);
@@ -731,11 +780,11 @@ template <bool Q4>
 void launch_few(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
   const dim3 block(64 * kFewWaves);
   if (p.tq == 16)
-    hipLaunchKernelGGL((few_attn_kernel<Q4, 1>), grid, block, 0, stream, pr, a);
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 1, 1>), grid, block, 0, stream, pr, a);
   else if (p.tq == 32)
-    hipLaunchKernelGGL((few_attn_kernel<Q4, 2>), grid, block, 0, stream, pr, a);
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 2, 1>), grid, block, 0, stream, pr, a);
   else
-    hipLaunchKernelGGL((few_attn_kernel<Q4, 4>), grid, block, 0, stream, pr, a);
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 2, 2>), grid, block, 0, stream, pr, a);
 }
 
 template <bool Q4, int NW>
@@ -770,7 +819,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
       launch_few<false>(p, grid, pr, a, stream);
     if (p.nslots > 1)
       hipLaunchKernelGGL(packed_merge_kernel<true>, dim3((unsigned)(pr.b * hkv), (unsigned)(p.tq / 4)), dim3(256), 0,
-                         stream, pr, a, p.tq);
+                         stream, pr, a, p.tq, p.grain);
     return hipGetLastError();
   }
   const dim3 grid((unsigned)(p.items * hkv), (unsigned)p.nslots);
@@ -787,7 +836,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
   }
   if (p.nslots > 1)
     hipLaunchKernelGGL(packed_merge_kernel<false>, dim3((unsigned)(p.items * hkv), (unsigned)(p.tq / 4)), dim3(256), 0,
-                       stream, pr, a, p.tq);
+                       stream, pr, a, p.tq, p.grain);
   return hipGetLastError();
 }
 
