@@ -34,9 +34,9 @@ struct AttnArgs {
   int pos_offset, hq, hkv;
   int64_t len_bound, capacity;
   uint16_t* out;
-  float* part_o;    // [item][slot][query][128], null without splitting
-  float2* part_ml;  // [item][slot][query]
-  int nslots;
+  float* part_o;    // [unit][kv head][query][128], null without splitting
+  float2* part_ml;  // [unit][kv head][query]
+  int most;         // parts of one kv head, 0 without splitting
 };
 
 // max / sum over the two lanes that share a column of a 32 x 32 product
@@ -50,12 +50,138 @@ __device__ __forceinline__ float pair_fold(float v, OP op) {
 
 __device__ __forceinline__ bool nonfinite_h(half_t v) { return (__builtin_bit_cast(uint16_t, v) & 0x7C00) == 0x7C00; }
 
-// The keys of part `slot` of `n` steps of 64 split evenly over nslots parts, in multiples of `grain` steps.
-__device__ __forceinline__ void slot_steps(int n, int nslots, int slot, int grain, int& lo, int& hi) {
-  int span = (n + nslots - 1) / nslots;
-  span = (span + grain - 1) / grain * grain;
-  lo = slot * span;
-  hi = lo + span < n ? lo + span : n;
+// How the work is laid over workgroups.  A sequence's queries are `tiles` tiles, each over the sequence's `steps` steps of
+// 64 keys, and every tile's steps are cut into parts of `span`: `span` is what keeps the number of parts of all sequences
+// within `most` (0: no cutting), so that sequences of different lengths give workgroups of like length.  Every workgroup
+// forms it for itself from the device's lengths: with S = sum of tiles * steps and N = sum of tiles, S / (most - N) always
+// suffices and S / most never does; the smallest of four values between that does is taken (up to 64 sequences, whose
+// sums are one reduction; the first for more).
+struct SeqWork {
+  int tiles, steps;
+};
+struct Unit {
+  int s, tile, part, span, steps;
+};
+
+__device__ __forceinline__ float wave_total(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, quad_sum(v));
+  float x = __builtin_bit_cast(float, u);
+  x = dpp_add<0xB1>(x);   // quad_perm [1,0,3,2]
+  x = dpp_add<0x4E>(x);   // quad_perm [2,3,0,1]
+  x = dpp_add<0x141>(x);  // row_half_mirror
+  return dpp_add<0x140>(x);  // row_mirror
+}
+
+template <class F>
+struct Planner {
+  int b, span, lane;
+  F work;
+  SeqWork mine;
+
+  __device__ __forceinline__ SeqWork at(int base) const {
+    if (base == 0) return mine;
+    return base + lane < b ? work(base + lane) : SeqWork{0, 0};
+  }
+  static __device__ __forceinline__ int parts(SeqWork w, int span) {
+    return w.steps > span ? (w.steps + span - 1) / span : 1;
+  }
+
+  __device__ __forceinline__ Planner(int b, int most, int grain, F work) : b(b), span(1 << 30), lane(threadIdx.x & 63), work(work) {
+    mine = lane < b ? work(lane) : SeqWork{0, 0};
+    if (most == 0) return;
+    float S = 0.f, N = 0.f;  // (sums a little off in fp32; S is taken 2^-16 larger)
+    for (int base = 0; base < b; base += kWave) {
+      const SeqWork w = at(base);
+      S += wave_total((float)w.tiles * (float)w.steps);
+      N += wave_total((float)w.tiles);
+    }
+    S *= 1.f + 0x1p-16f;
+    auto up = [&](float x) { return ((int)x / grain + 1) * grain; };
+    const float room = (float)most - N;
+    const int hi = up(S / (room < 1.f ? 1.f : room));
+    span = hi;
+    if (b > kWave) return;
+    const int lo = up(S / (float)most - 1.f);
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      const int c = lo + (hi - lo) / grain * i / 4 * grain;
+      if (wave_total((float)(mine.tiles * parts(mine, c))) <= (float)most) span = c;
+    }
+    span = __builtin_amdgcn_readfirstlane(span);
+  }
+
+  // Unit `item` of the list (sequence 0: tile 0 with its parts, tile 1, ..; sequence 1: ..); false past its end.
+  __device__ __forceinline__ bool find(int item, Unit& u) const {
+    int before = 0;
+    for (int base = 0; base < b; base += kWave) {
+      const SeqWork w = at(base);
+      const int np = parts(w, span), n = w.tiles * np;
+      const int incl = scan(n);
+      const int total = __builtin_amdgcn_readlane(incl, kWave - 1);
+      if (item < before + total) {
+        const int l = __builtin_ctzll(__ballot(before + incl > item));
+        const int k = item - before - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
+        const int pl = __builtin_amdgcn_readlane(np, l);
+        u.s = base + l;
+        u.tile = k / pl;
+        u.part = k - u.tile * pl;
+        u.span = span;
+        u.steps = __builtin_amdgcn_readlane(w.steps, l);
+        return true;
+      }
+      before += total;
+    }
+    return false;
+  }
+
+  // Tile `item` of the list without parts, and the index of its first part in the list with them.
+  __device__ __forceinline__ bool find_tile_parts(int item, Unit& u, int& first) const {
+    int before = 0, before_p = 0;
+    for (int base = 0; base < b; base += kWave) {
+      const SeqWork w = at(base);
+      const int np = parts(w, span);
+      const int incl = scan(w.tiles), incl_p = scan(w.tiles * np);
+      const int total = __builtin_amdgcn_readlane(incl, kWave - 1);
+      if (item < before + total) {
+        const int l = __builtin_ctzll(__ballot(before + incl > item));
+        const int tl = __builtin_amdgcn_readlane(w.tiles, l), pl = __builtin_amdgcn_readlane(np, l);
+        u.s = base + l;
+        u.tile = item - before - (__builtin_amdgcn_readlane(incl, l) - tl);
+        u.part = 0;
+        u.span = span;
+        u.steps = __builtin_amdgcn_readlane(w.steps, l);
+        first = before_p + __builtin_amdgcn_readlane(incl_p, l) - tl * pl + u.tile * pl;
+        return true;
+      }
+      before += total;
+      before_p += __builtin_amdgcn_readlane(incl_p, kWave - 1);
+    }
+    return false;
+  }
+
+  __device__ __forceinline__ int scan(int n) const {
+    int incl = n;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const int o = __shfl_up(incl, d, kWave);
+      incl += lane >= d ? o : 0;
+    }
+    return incl;
+  }
+};
+
+// The last key that rows up to position `pl` of a sequence read, and the steps of 64 up to it.
+__device__ __forceinline__ int last_key(int64_t pl, int64_t len_bound) {
+  const int64_t k = pl < len_bound ? pl : len_bound - 1;  // (rows past the bound are not computed)
+  return k < -1 ? -1 : (int)k;
+}
+__device__ __forceinline__ int steps_to(int klast) { return klast < 0 ? 0 : klast / kTile + 1; }
+
+// Tiles of TQ queries of a sequence, and its steps.
+__device__ __forceinline__ SeqWork seq_work(const PackedRows& pr, const AttnArgs& a, int G, int TQ, int s) {
+  const SeqRows sr = seq_rows(pr, s);
+  const int64_t pl = (int64_t)a.pos_base[s] + a.pos_offset + sr.n - 1;
+  return {(sr.n * G + TQ - 1) / TQ, steps_to(last_key(pl, a.len_bound))};
 }
 
 // ------------------------------------------------------------------ dequant
@@ -169,22 +295,27 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   constexpr bool kAhead = Q4 || NQT == 1;
   __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
   __shared__ float2 ml[kFewWaves][16 * NQT];
-  const int slot = blockIdx.x, s = blockIdx.y / a.hkv, g = blockIdx.y - s * a.hkv;
-  const int64_t sg = blockIdx.y;
+  const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 % NW;
   const int q0 = wave8 / NW * (16 * NQT);  // the wavefront's first query
   const int G = a.hq / a.hkv;
+  Unit u;
+  if (a.most) {
+    const Planner plan(pr.b, a.most, NW, [&](int i) { return seq_work(pr, a, G, 16 * NQT * HALVES, i); });
+    if (!plan.find(item, u)) return;
+  } else {  // an item a sequence
+    const SeqWork w = seq_work(pr, a, G, 16 * NQT * HALVES, item);
+    if (w.tiles == 0) return;
+    u = {item, 0, 0, 1 << 30, w.steps};
+  }
+  const int s = u.s;
+  const int64_t sg = (int64_t)s * a.hkv + g;
   const SeqRows sr = seq_rows(pr, s);
   const int nq = sr.n * G;
-  if (nq == 0) return;
   const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
-  const int64_t pl = p0 + sr.n - 1;
-  const int64_t klast = pl < a.len_bound ? pl : a.len_bound - 1;  // (rows past the bound are not computed)
-  const int nst = klast < 0 ? 0 : (int)(klast / kTile) + 1;
-  int st0, st1;
-  slot_steps(nst, a.nslots, slot, NW, st0, st1);
-  if (st0 >= st1 && slot > 0) return;  // the part has no keys (part 0 always answers: rows without any key)
+  const int64_t klast = last_key(p0 + sr.n - 1, a.len_bound);
+  const int st0 = u.part * u.span, st1 = st0 + u.span < u.steps ? st0 + u.span : u.steps;
 
   half8_t qf[NQT][4];
   int lpos[NQT];  // the position of this lane's query, clipped to [-1, 2^31)
@@ -397,7 +528,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       }
     }
     if (a.part_o) {
-      const int64_t at = (sg * a.nslots + slot) * nq_pad + qi;
+      const int64_t at = (int64_t)blockIdx.x * nq_pad + qi;
       float4_t* po = reinterpret_cast<float4_t*>(a.part_o + at * kHd + d0);
       po[0] = float4_t{r[0], r[1], r[2], r[3]};
       po[1] = float4_t{r[4], r[5], r[6], r[7]};
@@ -416,7 +547,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 
 // -------------------------------------------------------------- many rows
 // One workgroup per (tile of 32 NW queries, kv head, part of the keys): each wavefront 32 queries, the keys in steps of
-// 64 through two LDS buffers (the next step's loads in flight meanwhile, one barrier a step).
+// 64 through LDS buffers, one barrier a step.  fp16 entries go from memory to LDS directly, kRing - 1 steps ahead; 4-bit
+// ones through registers, one step ahead, and become halves on the way.
 // v_mfma_f32_32x32x16_f16: lane l holds row / column lc = l % 32 and k = 8 h .. +8 (h = l / 32), and of D rows 8 (i / 4) +
 // 4 h + i % 4 of column lc.  Row r of a key tile is the key r with bits 2 and 3 exchanged, so that a lane's 16 scores
 // are keys 16 (i / 8) + 8 h + i % 8: the P^T fragments of two steps of 16 keys.
@@ -424,33 +556,54 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 // dimension) with cell c at c ^ (d / 2 % 8): 16 lanes of one fragment read 16 different 16-byte banks.
 __device__ __forceinline__ int swap23(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
 
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 bytes per lane from memory to LDS: lane l's go to dst + 16 l (dst uniform).  In assembly, because the compiler waits
+// for all loads of the builtin before any read of LDS, whichever buffer it reads; the waits are barrier_after_loads.
+// There is no result register, and the addresses are read when the load is issued.
+__device__ __forceinline__ void load_to_lds(const void* src, void* dst) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)dst);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(at) : "memory", "m0");
+}
+
+// All but the wavefront's last N loads, and everything it did in LDS, done by every wavefront.
+template <int N>
+__device__ __forceinline__ void barrier_after_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+constexpr int ring(bool q4, int nw) { return q4 || nw < 8 ? 2 : 3; }
+
 template <bool Q4, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
                                                                                                       AttnArgs a) {
-  constexpr int NT = 64 * NW, TQ = 32 * NW;
-  constexpr int kCells = 1024 / NT;               // fp16: 16-byte cells of keys (and of values) per thread
+  constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW);
+  constexpr int kLoads = 16 / NW;                 // fp16: loads of 1 KB of keys (and of values) per wavefront and step
   constexpr int kCodes = NW >= 8 ? 1 : 512 / NT;  // 4-bit: 16-byte cells of codes per thread
-  __shared__ __align__(16) u32x4 kb[2][1024], vb[2][1024];
+  __shared__ __align__(16) u32x4 kb[kRing][1024], vb[kRing][1024];
   __shared__ unsigned long long odd_keys[3];  // keys of a step whose values are not finite
   const int G = a.hq / a.hkv;
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int s, t;
-  if (!find_tile(pr.b, item, [&](int i) { return (seq_rows(pr, i).n * G + TQ - 1) / TQ; }, s, t)) return;
+  Unit u;
+  {
+    const Planner plan(pr.b, SPLIT ? a.most : 0, 1, [&](int i) { return seq_work(pr, a, G, TQ, i); });
+    if (!plan.find(item, u)) return;
+  }
+  const int s = u.s;
   const SeqRows sr = seq_rows(pr, s);
   const int nq = sr.n * G;
-  const int qt = (nq + TQ - 1) / TQ - 1 - t;  // the latest rows (the most keys) first
+  const int qt = (nq + TQ - 1) / TQ - 1 - u.tile;  // the latest rows (the most keys) first
   const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
   const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
-  const int64_t pmin = p0 + qt * TQ / G, pl = p0 + qlast / G;
-  const int64_t klast64 = pl < a.len_bound ? pl : a.len_bound - 1;
-  const int klast = klast64 < -1 ? -1 : (int)klast64;
-  int st0 = 0, st1 = klast < 0 ? 0 : klast / kTile + 1;
-  if constexpr (SPLIT) {
-    slot_steps(st1, a.nslots, blockIdx.y, 1, st0, st1);
-    if (st0 >= st1 && blockIdx.y > 0) return;
-  }
+  const int64_t pmin = p0 + qt * TQ / G;
+  const int klast = last_key(p0 + qlast / G, a.len_bound), nst = steps_to(klast);
+  const int st0 = SPLIT ? u.part * u.span : 0;
+  const int st1 = SPLIT && st0 + u.span < nst ? st0 + u.span : nst;
+  if (SPLIT && u.part > 0 && st0 >= st1) return;  // (part 0 always answers: rows without any key)
   const int64_t sg = (int64_t)s * a.hkv + g;
   const int wq = qt * TQ + 32 * wave;                       // the wavefront's first query
   const bool owner = wq < nq;
@@ -459,43 +612,54 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int lpos = clip(p0 + qj);
   const int wmin = clip(p0 + wq / G);                       // of the wavefront's queries
   const int wmax = clip(p0 + (wq + 31 < nq ? wq + 31 : nq - 1) / G);
-  const uint16_t* qp = a.q + ((int64_t)(sr.first + qj) * a.hq + g * G + (qi - qj * G)) * kHd + 8 * h;
-  half8_t qf[8];
-#pragma unroll
-  for (int x = 0; x < 8; ++x) qf[x] = *reinterpret_cast<const half8_t*>(qp + 16 * x);
 
-  u32x4 pre[Q4 ? kCodes : 2 * kCells];
+  // fp16: load i of a step takes cells 64 (wave + NW i) .. +64 of the keys and of the values; what a cell of LDS holds is
+  // chosen by where its lane reads
+  const uint16_t* kp[kLoads];
+  const uint16_t* vp[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int ci = wave + NW * i;
+    const int row = 4 * ci + (lane >> 4), d = 8 * ci + (lane >> 3);
+    kp[i] = Q4 ? nullptr : a.c.k + (sg * a.capacity + row) * kHd + ((lane & 15) ^ swap23(row & 15)) * 8;
+    vp[i] = Q4 ? nullptr : a.c.v + (sg * kHd + d) * a.capacity + ((lane & 7) ^ ((d >> 1) & 7)) * 8;
+  }
+  auto issue_step = [&](int st, int buf) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_to_lds(kp[i] + (int64_t)st * (kTile * kHd), &kb[buf][64 * (wave + NW * i)]);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_to_lds(vp[i] + (int64_t)st * kTile, &vb[buf][64 * (wave + NW * i)]);
+  };
+  // ... and in a step past the tile's first position its values are tamed where they lie
+  auto tame_step = [&](int st, int buf) {
+#pragma unroll
+    for (int i = 0; i < 1024 / NT; ++i) {
+      const int c = tid + NT * i, part = (c & 7) ^ ((c >> 4) & 7);
+      const u32x4 w = vb[buf][c];
+      uint32_t odd = 0;
+      vb[buf][c] = __builtin_bit_cast(u32x4, tame(__builtin_bit_cast(half8_t, w), klast - (st * kTile + 8 * part), odd));
+      if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * part));
+    }
+  };
+
+  u32x4 pre[Q4 ? kCodes : 1];
   uint2 pre_ks[Q4 ? kCodes : 1];
   ValScales pre_vs;
   // 4-bit cell c: key c / 4, part c % 4 of it (c < 256), byte (c - 256) / 4 of the block of values, positions 16 (c % 4)
   // .. +16; which of the two is uniform across a wavefront
   auto load_step = [&](int st) {
     const int64_t key0 = (int64_t)st * kTile;
-    if constexpr (Q4) {
 #pragma unroll
-      for (int i = 0; i < kCodes; ++i) {
-        const int c = tid + NT * i;
-        if (c < 256) {
-          const int64_t e = sg * a.capacity + key0 + (c >> 2);
-          pre[i] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + (c & 3)];
-          pre_ks[i] = reinterpret_cast<const uint2*>(a.c.ks)[e];
-        } else {
-          const int c2 = c - 256;
-          pre[i] = *reinterpret_cast<const u32x4*>(a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 + 16 * c2);
-          pre_vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * (c2 & 3));
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kCells; ++i) {
-        const int c = tid + NT * i;
-        pre[i] = *reinterpret_cast<const u32x4*>(a.c.k + (sg * a.capacity + key0 + (c >> 4)) * kHd + (c & 15) * 8);
-      }
-#pragma unroll
-      for (int i = 0; i < kCells; ++i) {
-        const int c = tid + NT * i;
-        pre[kCells + i] =
-            *reinterpret_cast<const u32x4*>(a.c.v + (sg * kHd + (c >> 3)) * a.capacity + key0 + (c & 7) * 8);
+    for (int i = 0; i < kCodes; ++i) {
+      const int c = tid + NT * i;
+      if (c < 256) {
+        const int64_t e = sg * a.capacity + key0 + (c >> 2);
+        pre[i] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + (c & 3)];
+        pre_ks[i] = reinterpret_cast<const uint2*>(a.c.ks)[e];
+      } else {
+        const int c2 = c - 256;
+        pre[i] = *reinterpret_cast<const u32x4*>(a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 + 16 * c2);
+        pre_vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * (c2 & 3));
       }
     }
   };
@@ -504,84 +668,107 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if (st * (int64_t)kTile + kTile - 1 > pmin) v = tame(v, klast - (st * kTile + 8 * part), odd);  // uniform
     vb[buf][d * 8 + (part ^ ((d >> 1) & 7))] = __builtin_bit_cast(u32x4, v);
   };
-  auto store_step = [&](int buf, int st) {
-    if constexpr (Q4) {
+  auto store_step = [&](int st, int buf) {
 #pragma unroll
-      for (int i = 0; i < kCodes; ++i) {
-        const int c = tid + NT * i;
-        half8_t lo[2], hi[2];
-        if (c < 256) {
-          const int key = c >> 2, part = c & 3;
-          dequant_key(pre[i], pre_ks[i], lo, hi);
-          const int sw = swap23(key & 15);
+    for (int i = 0; i < kCodes; ++i) {
+      const int c = tid + NT * i;
+      half8_t lo[2], hi[2];
+      if (c < 256) {
+        const int key = c >> 2, part = c & 3;
+        dequant_key(pre[i], pre_ks[i], lo, hi);
+        const int sw = swap23(key & 15);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            kb[buf][key * 16 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
-            kb[buf][key * 16 + ((8 + 2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
-          }
-        } else {
-          const int c2 = c - 256, j = c2 >> 2, part = c2 & 3;
-          dequant_val<false>(pre[i], pre_vs, lo);
-          dequant_val<true>(pre[i], pre_vs, hi);
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            uint32_t odd = 0;
-            put_val(buf, st, j, 2 * part + x, lo[x], odd);
-            put_val(buf, st, j + 64, 2 * part + x, hi[x], odd);
-            if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * (2 * part + x)));
-          }
+        for (int x = 0; x < 2; ++x) {
+          kb[buf][key * 16 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
+          kb[buf][key * 16 + ((8 + 2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
         }
-      }
-    } else {
+      } else {
+        const int c2 = c - 256, j = c2 >> 2, part = c2 & 3;
+        dequant_val<false>(pre[i], pre_vs, lo);
+        dequant_val<true>(pre[i], pre_vs, hi);
 #pragma unroll
-      for (int i = 0; i < kCells; ++i) {
-        const int c = tid + NT * i;
-        kb[buf][(c & ~15) + ((c & 15) ^ swap23((c >> 4) & 15))] = pre[i];
-      }
-#pragma unroll
-      for (int i = 0; i < kCells; ++i) {
-        const int c = tid + NT * i;
-        const u32x4 w = pre[kCells + i];
-        uint32_t odd = 0;
-        put_val(buf, st, c >> 3, c & 7, __builtin_bit_cast(half8_t, w), odd);
-        if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * (c & 7)));
+        for (int x = 0; x < 2; ++x) {
+          uint32_t odd = 0;
+          put_val(buf, st, j, 2 * part + x, lo[x], odd);
+          put_val(buf, st, j + 64, 2 * part + x, hi[x], odd);
+          if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * (2 * part + x)));
+        }
       }
     }
   };
 
+  if (tid < 3) odd_keys[tid] = 0;
+  if constexpr (Q4) {
+    __syncthreads();
+    if (st0 < st1) {
+      load_step(st0);
+      store_step(st0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i)
+      if (st0 + i < st1) issue_step(st0 + i, i);
+  }
+  half8_t qf[8];
+  {
+    const uint16_t* qp = a.q + ((int64_t)(sr.first + qj) * a.hq + g * G + (qi - qj * G)) * kHd + 8 * h;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) qf[x] = *reinterpret_cast<const half8_t*>(qp + 16 * x);
+    // they have arrived: a wait for them in the loop would be one for the keys in flight too
+#pragma unroll
+    for (int x = 0; x < 8; ++x) asm volatile("" : "+v"(qf[x]));
+  }
   float m = kNoMax, l = 0.f;
   float16_t o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-  if (tid < 3) odd_keys[tid] = 0;
-  __syncthreads();
-  if (st0 < st1) {
-    load_step(st0);
-    store_step(st0 & 1, st0);
-  }
+  const int krow = swap23(lc) * 16, vrow = lc * 8, vsw = (lc >> 1) & 7;
+  int buf = 0;
   for (int st = st0; st < st1; ++st) {
-    const int key0 = st * kTile, buf = st & 1;
-    // step st is in its buffer, and every wavefront is done with step st - 1; what the barrier does not wait for: the
-    // loads of step st + 1
-    __syncthreads();
-    if (st + 1 < st1) load_step(st + 1);
-    if (tid == 0) odd_keys[(st + 2) % 3] = 0;
+    const int key0 = st * kTile;
     const bool past = key0 + kTile - 1 > pmin;  // uniform: some row of the workgroup may not read some key
+    // step st is in its buffer, and every wavefront is done with step st - 1
+    if constexpr (Q4) {
+      __syncthreads();
+      if (st + 1 < st1) load_step(st + 1);
+    } else {
+      if (st + kRing - 2 < st1)  // the steps st + 1 .. st + kRing - 2 may stay in flight
+        barrier_after_loads<(kRing - 2) * 2 * kLoads>();
+      else
+        barrier_after_loads<0>();
+      if (st + kRing - 1 < st1) issue_step(st + kRing - 1, buf == 0 ? kRing - 1 : buf - 1);
+      if (past) {
+        tame_step(st, buf);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+    }
+    if (tid == 0) odd_keys[(st + 2) % 3] = 0;
     if (owner && key0 <= wmax) {  // uniform in the wavefront
       float16_t sc[2];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
-        const u32x4* row = &kb[buf][(32 * b + swap23(lc)) * 16];
+      // fragment i of the keys: half i % 2 of the tile, dimensions 16 (i / 2) .. +16; kDeep of them ahead of the products
+      constexpr int kDeep = Q4 ? 2 : 4;
+      u32x4 f[kDeep];
+      auto key_frag = [&](int i) { return kb[buf][(i & 1) * 512 + krow + ((2 * (i >> 1) + h) ^ (lc & 15))]; };
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const u32x4 w = row[(2 * x + h) ^ (lc & 15)];
-          sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), qf[x], sc[b], 0, 0, 0);
-        }
+      for (int i = 0; i < kDeep; ++i) f[i] = key_frag(i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const u32x4 w = f[i % kDeep];
+        sc[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), qf[i >> 1], sc[i & 1], 0, 0, 0);
+        if (i + kDeep < 16) f[i % kDeep] = key_frag(i + kDeep);
       }
+      // fragment i of the values: dimensions 32 (i % 4) .. +32, keys 16 (i / 4) .. +16
+      auto val_frag = [&](int i) { return vb[buf][(i & 3) * 256 + vrow + ((2 * (i >> 2) + h) ^ vsw)]; };
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) f[i] = val_frag(i);
       const bool tail = key0 + kTile - 1 > wmin;  // uniform
       if (tail) {
         const int lim = (lpos - key0 < kTile ? lpos - key0 : kTile) - 8 * h;
@@ -608,21 +795,21 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       half8_t pf[4];
       float sum = 0.f;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int x = 0; x < 4; ++x) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float p = exp2_fast(__builtin_fmaf(sc[b][i], kScale, ref));
+        for (int e = 0; e < 8; ++e) {
+          const float p = exp2_fast(__builtin_fmaf(sc[x >> 1][8 * (x & 1) + e], kScale, ref));
           sum += p;
-          pf[2 * b + (i >> 3)][i & 7] = (half_t)p;
+          pf[x][e] = (half_t)p;
         }
+      }
       l += sum;
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const u32x4 w = vb[buf][(32 * d + lc) * 8 + ((2 * x + h) ^ ((lc >> 1) & 7))];
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), pf[x], o[d], 0, 0, 0);
-        }
+      for (int i = 0; i < 16; ++i) {
+        const u32x4 w = f[i % kDeep];
+        o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), pf[i >> 2], o[i & 3], 0, 0, 0);
+        if (i + kDeep < 16) f[i % kDeep] = val_frag(i + kDeep);
+      }
       if (past) {
         unsigned long long odd = odd_keys[st % 3];
 #pragma unroll 1
@@ -639,12 +826,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
       }
     }
-    if (st + 1 < st1) store_step((st + 1) & 1, st + 1);
+    if constexpr (Q4) {
+      if (st + 1 < st1) store_step(st + 1, buf ^ 1);
+    }
+    buf = buf + 1 == kRing ? 0 : buf + 1;
   }
   if (!owner) return;
   l = pair_fold(l, [](float x, float y) { return x + y; });
   if constexpr (SPLIT) {
-    const int64_t at = ((int64_t)blockIdx.x * a.nslots + blockIdx.y) * TQ + 32 * wave + lc;
+    const int64_t at = (int64_t)blockIdx.x * TQ + 32 * wave + lc;
     float* po = a.part_o + at * kHd + 4 * h;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -673,31 +863,27 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 }
 
 // The parts of each query joined, in their order: a wavefront per query, lane i the weight of part i (at most 512 parts:
-// eight a lane), then every lane two dimensions, eight parts' sums in flight.  Which parts hold keys of the query's tile
-// is what the kernels above decided, from the same numbers.  TQ: queries of an item (few rows: the item is the
-// sequence); grain: the steps that a part's are a multiple of.
-template <bool FEW>
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain) {
+// eight a lane), then every lane two dimensions, eight parts' sums in flight.
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain, bool few) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int G = a.hq / a.hkv;
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
-  int s = item, qt = 0;
-  if constexpr (!FEW) {
-    int t;
-    if (!find_tile(pr.b, item, [&](int i) { return (seq_rows(pr, i).n * G + TQ - 1) / TQ; }, s, t)) return;
-    qt = (seq_rows(pr, s).n * G + TQ - 1) / TQ - 1 - t;
+  Unit u;
+  int first;
+  {
+    const Planner plan(pr.b, a.most, grain, [&](int i) { return seq_work(pr, a, G, TQ, i); });
+    if (!plan.find_tile_parts(item, u, first)) return;
   }
+  const int s = u.s;
   const SeqRows sr = seq_rows(pr, s);
-  const int nq = sr.n * G, qx = blockIdx.y * 4 + wave, qi = qt * TQ + qx;
+  const int nq = sr.n * G, qt = few ? 0 : (nq + TQ - 1) / TQ - 1 - u.tile;
+  const int qx = blockIdx.y * 4 + wave, qi = qt * TQ + qx;
   if (qx >= TQ || qi >= nq) return;
   const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
   const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
-  const int64_t pl = p0 + qlast / G, klast = pl < a.len_bound ? pl : a.len_bound - 1;
-  const int nst = klast < 0 ? 0 : (int)(klast / kTile) + 1;
-  int span, parts;
-  slot_steps(nst, a.nslots, 0, grain, parts, span);  // part 0: steps 0 .. span
-  parts = span > 0 ? (nst + span - 1) / span : 1;
-  const int64_t base = (int64_t)blockIdx.x * a.nslots;
+  const int nst = steps_to(last_key(p0 + qlast / G, a.len_bound));
+  const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
+  const int64_t row0 = ((int64_t)first * a.hkv + g) * TQ + qx, stride = (int64_t)a.hkv * TQ;  // (row p: part p's sums)
   constexpr int kMost = 8;
   float2 ml[kMost];
   float M = kNoMax, L = 0.f;
@@ -705,7 +891,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   for (int i = 0; i < kMost; ++i) {
     const int p = 64 * i + lane;
     ml[i] = make_float2(kNoMax, 0.f);
-    if (p < parts) ml[i] = a.part_ml[(base + p) * TQ + qx];
+    if (p < parts) ml[i] = a.part_ml[row0 + p * stride];
     M = fmaxf(M, ml[i].x);
   }
 #pragma unroll
@@ -717,13 +903,13 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   }
   L = wave_sum(L);
   float x = 0.f, y = 0.f;
-  const float* po = a.part_o + (base * TQ + qx) * kHd + 2 * lane;
+  const float* po = a.part_o + row0 * kHd + 2 * lane;
   for (int p0i = 0; p0i < parts; p0i += 8) {
     float2 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int p = p0i + i < parts ? p0i + i : parts - 1;
-      v[i] = *reinterpret_cast<const float2*>(po + (int64_t)p * TQ * kHd);
+      v[i] = *reinterpret_cast<const float2*>(po + p * stride * kHd);
     }
     float fw = ml[0].x;
 #pragma unroll
@@ -744,35 +930,36 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
 
 struct Plan {
   bool few;
-  int tq, items, nslots, grain;  // queries of an item, items, parts of the keys, steps that a part's are a multiple of
+  int tq, grain;    // queries of a tile; steps that a part's are a multiple of
+  int tiles, most;  // tiles at most; parts at most (0: the keys are not split)
 };
 
 Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
   const int G = hq / hkv;
   const int64_t steps = (len_bound + kTile - 1) / kTile;
+  const int64_t b = pr.b < pr.rows ? pr.b : pr.rows;
   Plan p;
   p.few = (int64_t)pr.max_rows * G <= 64;
-  int64_t slots;
+  p.grain = 1;
+  int64_t most = 0;
   if (p.few) {
     p.tq = pr.max_rows * G <= 16 ? 16 : (pr.max_rows * G <= 32 ? 32 : 64);
-    p.items = pr.b;
     p.grain = p.tq > 32 ? kFewWaves / 2 : kFewWaves;
-    slots = 256 / ((int64_t)p.items * hkv);
-    const int64_t most = (steps + p.grain - 1) / p.grain;
-    slots = slots > most ? most : slots;
+    p.tiles = pr.b;
+    most = 256 / hkv;
+    if (2 * b > most) most = 1024 / hkv;
+    if (2 * b > most || steps <= p.grain) most = 0;
   } else {
-    p.tq = 128;
-    p.grain = 1;
-    const int64_t b = pr.b < pr.rows ? pr.b : pr.rows;
-    auto items = [&](int64_t tq) {
-      return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq : (int64_t)pr.b * (((int64_t)pr.max_rows * G + tq - 1) / tq);
+    auto tiles = [&](int64_t tq) {
+      return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq
+                      : (int64_t)pr.b * (((int64_t)pr.max_rows * G + tq - 1) / tq);
     };
-    if (items(256) * hkv >= 512) p.tq = 256;
-    p.items = (int)items(p.tq);
-    slots = items(p.tq) * hkv >= 256 ? 1 : 512 / (items(p.tq) * hkv);
-    slots = slots > steps / 4 ? steps / 4 : slots;
+    p.tq = tiles(256) * hkv >= 512 ? 256 : 128;
+    p.tiles = (int)tiles(p.tq);
+    most = 256 / hkv;
+    if (2 * p.tiles > most || steps <= 4) most = 0;
   }
-  p.nslots = (int)(slots < 1 ? 1 : slots);
+  p.most = (int)most;
   return p;
 }
 
@@ -789,7 +976,7 @@ void launch_few(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& 
 
 template <bool Q4, int NW>
 void launch_prompt(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
-  if (p.nslots > 1)
+  if (p.most)
     hipLaunchKernelGGL((prompt_attn_kernel<Q4, NW, true>), grid, dim3(64 * NW), 0, stream, pr, a);
   else
     hipLaunchKernelGGL((prompt_attn_kernel<Q4, NW, false>), grid, dim3(64 * NW), 0, stream, pr, a);
@@ -801,9 +988,10 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
                                    int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
                                    uint16_t* out, hipStream_t stream) {
   const Plan p = make_plan(pr, hq, hkv, len_bound);
-  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.nslots};
-  if (p.nslots > 1) {
-    const size_t queries = (size_t)p.items * hkv * p.nslots * p.tq;
+  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most};
+  const int units = p.most ? p.most : p.tiles;
+  if (p.most) {
+    const size_t queries = (size_t)units * hkv * p.tq;
     void* ws = nullptr;
     const hipError_t e = workspace(queries * (kHd * sizeof(float) + sizeof(float2)), stream, &ws);
     if (e != hipSuccess) return e;
@@ -811,19 +999,13 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     a.part_ml = reinterpret_cast<float2*>(a.part_o + queries * kHd);
   }
   const bool q4 = cache.k4 != nullptr;
+  const dim3 grid((unsigned)(units * hkv));
   if (p.few) {
-    const dim3 grid((unsigned)p.nslots, (unsigned)(pr.b * hkv));
     if (q4)
       launch_few<true>(p, grid, pr, a, stream);
     else
       launch_few<false>(p, grid, pr, a, stream);
-    if (p.nslots > 1)
-      hipLaunchKernelGGL(packed_merge_kernel<true>, dim3((unsigned)(pr.b * hkv), (unsigned)(p.tq / 4)), dim3(256), 0,
-                         stream, pr, a, p.tq, p.grain);
-    return hipGetLastError();
-  }
-  const dim3 grid((unsigned)(p.items * hkv), (unsigned)p.nslots);
-  if (p.tq == 256) {
+  } else if (p.tq == 256) {
     if (q4)
       launch_prompt<true, 8>(p, grid, pr, a, stream);
     else
@@ -834,9 +1016,9 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     else
       launch_prompt<false, 4>(p, grid, pr, a, stream);
   }
-  if (p.nslots > 1)
-    hipLaunchKernelGGL(packed_merge_kernel<false>, dim3((unsigned)(p.items * hkv), (unsigned)(p.tq / 4)), dim3(256), 0,
-                       stream, pr, a, p.tq, p.grain);
+  if (p.most)
+    hipLaunchKernelGGL(packed_merge_kernel, dim3((unsigned)(p.tiles * hkv), (unsigned)(p.tq / 4)), dim3(256), 0, stream,
+                       pr, a, p.tq, p.grain, p.few);
   return hipGetLastError();
 }
 
