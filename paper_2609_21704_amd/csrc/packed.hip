@@ -260,6 +260,7 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedRows pr, const i
   RowTile rt;
   if (!row_tile(pr, pos_base, pos_offset, blockIdx.x, rt)) return;  // uniform
   const int64_t base = rt.pos0 - rt.shift;
+  const CodeConsts kc;
   for (int g = blockIdx.y; g < hkv; g += gridDim.y) {
     const int64_t sg = (int64_t)rt.s * hkv + g;
     __syncthreads();
@@ -295,11 +296,11 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedRows pr, const i
         const half2_t s0 = bits_h2(sz[w][0] * 0x10001u), z0 = bits_h2(sz[w][1] * 0x10001u);
         const half2_t s1 = bits_h2(sz[w][2] * 0x10001u), z1 = bits_h2(sz[w][3] * 0x10001u);
         half2_t p, q;
-        code_pairs<false>(w ? vw : kw, p, q);
+        code_pairs<false>(kc, w ? vw : kw, p, q);
         p = (p - zero_pair<false>(z0)) * s0;
         q = (q - zero_pair<false>(z0)) * s0;
         *reinterpret_cast<half4_t*>(dst) = half4_t{p[0], p[1], q[0], q[1]};
-        code_pairs<true>(w ? vw : kw, p, q);
+        code_pairs<true>(kc, w ? vw : kw, p, q);
         p = (p - zero_pair<true>(z1)) * s1;
         q = (q - zero_pair<true>(z1)) * s1;
         *reinterpret_cast<half4_t*>(dst + 64) = half4_t{p[0], p[1], q[0], q[1]};

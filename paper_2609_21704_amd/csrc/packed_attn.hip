@@ -14,6 +14,8 @@
 // output's own rounding is, and independent from key to key.  Weights are kept times 2^7, and the reference maximum is
 // moved only when a row's maximum passes it by 2^8, so they stay below 2^15 and a weight loses bits only
 // below 2^-21 of the row's largest.
+#include <type_traits>
+
 #include "sq_internal.hpp"
 #include "sq_packed.hpp"
 
@@ -159,14 +161,15 @@ struct Planner {
     return false;
   }
 
-  __device__ __forceinline__ int scan(int n) const {
-    int incl = n;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int o = __shfl_up(incl, d, kWave);
-      incl += lane >= d ? o : 0;
-    }
-    return incl;
+  // sum over the lanes up to this one
+  static __device__ __forceinline__ int scan(int n) {
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xF, 0xF, true);  // row_shr:1
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xF, 0xF, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xF, 0xF, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xF, 0xF, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1 and 3
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2 and 3
+    return n;
   }
 };
 
@@ -187,11 +190,11 @@ __device__ __forceinline__ SeqWork seq_work(const PackedRows& pr, const AttnArgs
 // ------------------------------------------------------------------ dequant
 // Sixteen bytes of codes to 16 halves of the low and 16 of the high nibbles: f16((c - z) s), the difference exact.
 template <bool HIGH, class Z, class S>
-__device__ __forceinline__ void dequant16(u32x4 w, Z zero, S scale, half8_t (&o)[2]) {
+__device__ __forceinline__ void dequant16(const CodeConsts& k, u32x4 w, Z zero, S scale, half8_t (&o)[2]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     half2_t a, b;
-    code_pairs<HIGH>(w[i], a, b);
+    code_pairs<HIGH>(k, w[i], a, b);
     a = (a - zero(2 * i)) * scale(2 * i);
     b = (b - zero(2 * i + 1)) * scale(2 * i + 1);
     o[i >> 1][4 * (i & 1) + 0] = a[0];
@@ -202,11 +205,11 @@ __device__ __forceinline__ void dequant16(u32x4 w, Z zero, S scale, half8_t (&o)
 }
 
 // A key's part: 16 elements of each group, with the key's own scales and zeros.
-__device__ __forceinline__ void dequant_key(u32x4 w, uint2 sz, half8_t (&lo)[2], half8_t (&hi)[2]) {
+__device__ __forceinline__ void dequant_key(const CodeConsts& k, u32x4 w, uint2 sz, half8_t (&lo)[2], half8_t (&hi)[2]) {
   const half2_t s0 = bits_h2((sz.x & 0xFFFF) * 0x10001u), z0 = zero_pair<false>(bits_h2((sz.x >> 16) * 0x10001u));
   const half2_t s1 = bits_h2((sz.y & 0xFFFF) * 0x10001u), z1 = zero_pair<true>(bits_h2((sz.y >> 16) * 0x10001u));
-  dequant16<false>(w, [&](int) { return z0; }, [&](int) { return s0; }, lo);
-  dequant16<true>(w, [&](int) { return z1; }, [&](int) { return s1; }, hi);
+  dequant16<false>(k, w, [&](int) { return z0; }, [&](int) { return s0; }, lo);
+  dequant16<true>(k, w, [&](int) { return z1; }, [&](int) { return s1; }, hi);
 }
 
 // Scales and zeros of 16 consecutive positions of a block of values: [4][64] halves, 32 bytes of each row.
@@ -222,10 +225,10 @@ __device__ __forceinline__ ValScales load_val_scales(const uint16_t* vs) {
   return r;
 }
 template <bool HIGH>
-__device__ __forceinline__ void dequant_val(u32x4 w, const ValScales& v, half8_t (&o)[2]) {
+__device__ __forceinline__ void dequant_val(const CodeConsts& k, u32x4 w, const ValScales& v, half8_t (&o)[2]) {
   constexpr int si = HIGH ? 2 : 0;
   dequant16<HIGH>(
-      w,
+      k, w,
       [&](int i) {
         const uint32_t z = v.p[si + 1][i >> 2][i & 3];
         return zero_pair<HIGH>(bits_h2(z));
@@ -265,17 +268,24 @@ __device__ __forceinline__ OddValue odd_value(const AttnArgs& a, int64_t sg, int
   return r;
 }
 
-// Values in a step of which some row may read only a part of the keys: those after the last key `left` (an index into
-// the fragment) are stale and zeroed; one that is not finite is zeroed too, since a zero weight times it is NaN, and its
-// key noted in `odd`: add_odd gives it to the rows that read it.
-__device__ __forceinline__ half8_t tame(half8_t f, int left, uint32_t& odd) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const bool nf = e <= left && nonfinite_h(f[e]);
-    odd |= nf ? 1u << e : 0u;
-    f[e] = e > left || nf ? (half_t)0 : f[e];
-  }
-  return f;
+// A step past a tile's first row holds keys that some row may not read.  What must not reach a row there: values after
+// the last row's position (stale, anything), and values that are not finite, since a zero weight times one is NaN.  Both
+// are zeroed for the products; where a value was not finite, odd_values later adds it to the rows that do read it.
+// The halves of words of positions e, e + 1 up to the last key `left`:
+__device__ __forceinline__ uint32_t keep_mask(int e, int left) {
+  return (e <= left ? 0xFFFFu : 0u) | (e + 1 <= left ? 0xFFFF0000u : 0u);
+}
+// bit 15 of every half that is not finite: a full exponent carries into it
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) { return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t without(uint32_t w, uint32_t odd) { return w & ~(odd | (odd - (odd >> 15))); }
+
+// The same for the scales and zeros of a word's two positions: stale ones become 0, and a scale that is not finite does
+// (a zero always is finite), so that the values they give do.
+__device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, bool scale, uint32_t& odd) {
+  w &= keep_mask(e, left);
+  const uint32_t o = scale ? odd_halves(w) : 0u;
+  odd |= o;
+  return without(w, o);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -295,6 +305,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   constexpr bool kAhead = Q4 || NQT == 1;
   __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
   __shared__ float2 ml[kFewWaves][16 * NQT];
+  __shared__ __align__(16) uint16_t vsb[Q4 ? kFewWaves : 1][4][64];  // a step's scales and zeros of values, per wavefront
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 % NW;
@@ -332,6 +343,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   }
   float m[NQT], l[NQT];
   float4_t o[NQT][8];
+  half8_t pf[NQT][2];
 #pragma unroll
   for (int t = 0; t < NQT; ++t) {
     m[t] = kNoMax;
@@ -339,36 +351,51 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
     for (int d = 0; d < 8; ++d) o[t][d] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
+  const CodeConsts kc;
   const int krow = 16 * (li >> 2) + (li & 3);  // + 4 kt: this lane's key of a tile
   u32x4 kw[Q4 ? 4 : 16], vw[Q4 ? 4 : 16];  // 4-bit: a key's 16 bytes lg, byte rows 16 j + li; fp16: 32 lg .. +32 of a
   uint2 ksz[4];                            // key, positions 16 lg .. +16 of dim 16 d + li
-  ValScales vs;
+  uint2 vsr;  // 4-bit: this lane's 8 of the 512 bytes of a step's scales and zeros of values
+  // uniform bases and 32-bit lane offsets: the addresses stay out of the vector registers
+  const uint8_t* k4 = a.c.k4 + sg * a.capacity * 64;
+  const uint16_t* ks = a.c.ks + sg * a.capacity * 4;
+  const uint8_t* v4 = a.c.v4 + sg * a.capacity * 64;
+  const uint16_t* vs4 = a.c.vs + sg * a.capacity * 4;
+  const uint16_t* k16 = a.c.k + sg * a.capacity * kHd;
+  const uint16_t* v16 = a.c.v + sg * kHd * a.capacity;
+  const int64_t vlane = (int64_t)li * a.capacity + 16 * lg;
   auto load_k = [&](int st) {
+    if constexpr (Q4) {
+      const uint8_t* kst = k4 + (int64_t)st * (kTile * 64);
+      const uint16_t* sst = ks + (int64_t)st * (kTile * 4);
+      const uint32_t at = krow * 64 + 16 * lg, as = krow * 8;
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
-      const int64_t e = sg * a.capacity + (int64_t)st * kTile + krow + 4 * kt;
-      if constexpr (Q4) {
-        kw[kt] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + lg];
-        ksz[kt] = reinterpret_cast<const uint2*>(a.c.ks)[e];
-      } else {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) kw[4 * kt + x] = *reinterpret_cast<const u32x4*>(a.c.k + e * kHd + 32 * lg + 8 * x);
+      for (int kt = 0; kt < 4; ++kt) {
+        kw[kt] = *reinterpret_cast<const u32x4*>(kst + (at + 256 * kt));
+        ksz[kt] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(sst) + (as + 32 * kt));
       }
+    } else {
+      const uint8_t* kst = reinterpret_cast<const uint8_t*>(k16 + (int64_t)st * (kTile * kHd));
+      const uint32_t at = krow * 256 + 64 * lg;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) kw[4 * kt + x] = *reinterpret_cast<const u32x4*>(kst + (at + 1024 * kt + 16 * x));
     }
   };
-  auto load_vs = [&](int st) { vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * lg); };
   auto load_v = [&](int st) {
     if constexpr (Q4) {
-      if constexpr (NQT == 1) load_vs(st);  // (two tiles: within the step, the registers again)
-      const uint8_t* vp = a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 + li * 64 + 16 * lg;
+      vsr = reinterpret_cast<const uint2*>(vs4 + (int64_t)st * 256)[(uint32_t)lane];
+      const uint8_t* vst = v4 + (int64_t)st * 4096;
+      const uint32_t at = li * 64 + 16 * lg;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(vp + 1024 * j);
+      for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(vst + (at + 1024 * j));
     } else {
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
-        const uint16_t* vp = a.c.v + (sg * kHd + 16 * d + li) * a.capacity + (int64_t)st * kTile + 16 * lg;
-        vw[2 * d] = *reinterpret_cast<const u32x4*>(vp);
-        vw[2 * d + 1] = *reinterpret_cast<const u32x4*>(vp + 8);
+        const uint16_t* vst = v16 + (int64_t)16 * d * a.capacity + (int64_t)st * kTile;
+        vw[2 * d] = *reinterpret_cast<const u32x4*>(vst + vlane);
+        vw[2 * d + 1] = *reinterpret_cast<const u32x4*>(vst + vlane + 8);
       }
     }
   };
@@ -377,6 +404,14 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     load_k(st0 + wave);
     load_v(st0 + wave);
   }
+  auto product = [&](int d, half8_t v0, half8_t v1) {
+#pragma unroll
+    for (int t = 0; t < NQT; ++t) {
+      o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[t][0], o[t][d], 0, 0, 0);
+      o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[t][1], o[t][d], 0, 0, 0);
+    }
+  };
+  bool odd_seen = false;
   for (int st = st0 + wave; st < end; st += NW) {
     const int64_t key0 = (int64_t)st * kTile;
     const int next = st + NW < st1 ? st + NW : st;  // (the last step's loads are repeated: no branch around loads)
@@ -390,7 +425,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       half8_t kf[4];
       if constexpr (Q4) {
         half8_t lo[2], hi[2];
-        dequant_key(kw[kt], ksz[kt], lo, hi);
+        dequant_key(kc, kw[kt], ksz[kt], lo, hi);
         kf[0] = lo[0];
         kf[1] = lo[1];
         kf[2] = hi[0];
@@ -409,13 +444,12 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         for (int x = 0; x < 4; ++x) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x], qf[t][x], acc, 0, 0, 0);
         sc[t][kt] = acc;
       }
+      if constexpr (NQT > 1) __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (Q4 && NQT > 1) load_vs(st);
     if constexpr (kAhead) load_k(next);
     __builtin_amdgcn_sched_barrier(0);
     // only a step past the first row's position holds keys that some row may not read
     const bool tail = key0 + kTile - 1 > p0;  // uniform
-    half8_t pf[NQT][2];
 #pragma unroll
     for (int t = 0; t < NQT; ++t) {
       if (tail) {
@@ -450,29 +484,59 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         }
       l[t] += sum;
     }
-    uint32_t odd = 0;  // of this lane's 16 keys
-    const int left = (int)(klast - key0 < kTile ? klast - key0 : kTile) - 16 * lg;
-    auto product = [&](int d, half8_t v0, half8_t v1) {
-      if (tail) {
-        uint32_t o0 = 0, o1 = 0;
-        v0 = tame(v0, left, o0);
-        v1 = tame(v1, left - 8, o1);
-        odd |= o0 | o1 << 8;
-      }
+    if (tail) {
+      uint32_t odd = 0;
+      if constexpr (Q4) {
+        const int left = (int)(klast - key0 < kTile ? klast - key0 : kTile) - 4 * li;  // row lg of the four
+        vsr.x = tame_scales(vsr.x, 0, left, (lg & 1) == 0, odd);
+        vsr.y = tame_scales(vsr.y, 2, left, (lg & 1) == 0, odd);
+      } else {
+        const int left = (int)(klast - key0 < kTile ? klast - key0 : kTile) - 16 * lg;
 #pragma unroll
-      for (int t = 0; t < NQT; ++t) {
-        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[t][0], o[t][d], 0, 0, 0);
-        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[t][1], o[t][d], 0, 0, 0);
+        for (int x = 0; x < 8; ++x) {
+          const uint32_t keep = keep_mask(2 * x, left);
+#pragma unroll
+          for (int d = 0; d < 8; ++d) {
+            vw[2 * d + (x >> 2)][x & 3] &= keep;
+            odd |= odd_halves(vw[2 * d + (x >> 2)][x & 3]);
+          }
+        }
+        if (__any(odd != 0)) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            asm volatile("" : "+v"(vw[x]));  // (or the tests above would be kept in registers for this)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vw[x][i] = without(vw[x][i], odd_halves(vw[x][i]));
+          }
+        }
       }
-    };
+      odd_seen |= __any(odd != 0);
+    }
     if constexpr (Q4) {
+      // every lane needs the scales and zeros of its keys: handed round in LDS, two of the four rows at a time
+      reinterpret_cast<uint2*>(vsb[wave8])[lane] = vsr;
+      ValScales vs;
+      auto rows = [&](int r) {
+#pragma unroll
+        for (int i = r; i < r + 2; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) vs.p[i][x] = *reinterpret_cast<const u32x4*>(&vsb[wave8][i][16 * lg + 8 * x]);
+      };
+      rows(0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         half8_t x[2];
-        dequant_val<false>(vw[j], vs, x);
+        dequant_val<false>(kc, vw[j], vs, x);
         product(j, x[0], x[1]);
-        dequant_val<true>(vw[j], vs, x);
+        if constexpr (NQT > 1) __builtin_amdgcn_sched_barrier(0);
+      }
+      rows(2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        half8_t x[2];
+        dequant_val<true>(kc, vw[j], vs, x);
         product(4 + j, x[0], x[1]);
+        if constexpr (NQT > 1) __builtin_amdgcn_sched_barrier(0);
       }
     } else {
 #pragma unroll
@@ -483,18 +547,23 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     }
     if constexpr (kAhead) load_v(next);
     __builtin_amdgcn_sched_barrier(0);
-    if (tail && __any(odd != 0)) {
+  }
+  if (odd_seen) {
 #pragma unroll 1
-      for (int key = 0; key < kTile; ++key) {
-        if (!(__ballot((odd >> (key & 15)) & 1) >> (16 * (key >> 4)) & 0xFFFF)) continue;  // uniform
-        const OddValue ov = odd_value<Q4>(a, sg, key0 + key);
+    for (int st = st0 + wave; st < end; st += NW) {
+      const int64_t key0 = (int64_t)st * kTile;
+      if (key0 + kTile - 1 <= p0) continue;
+#pragma unroll 1
+      for (int64_t key = key0; key < key0 + kTile && key <= klast; ++key) {
+        const OddValue ov = odd_value<Q4>(a, sg, key);
+        if (!__any(ov.v[0] != 0.f || ov.v[1] != 0.f)) continue;
 #pragma unroll
         for (int d = 0; d < 8; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float v = __shfl(ov.v[d >> 2], 16 * (d & 3) + 4 * lg + i, kWave);
 #pragma unroll
-            for (int t = 0; t < NQT; ++t) o[t][d][i] += key0 + key <= lpos[t] ? v : 0.f;
+            for (int t = 0; t < NQT; ++t) o[t][d][i] += key <= lpos[t] ? v : 0.f;
           }
       }
     }
@@ -583,7 +652,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   constexpr int kLoads = 16 / NW;                 // fp16: loads of 1 KB of keys (and of values) per wavefront and step
   constexpr int kCodes = NW >= 8 ? 1 : 512 / NT;  // 4-bit: 16-byte cells of codes per thread
   __shared__ __align__(16) u32x4 kb[kRing][1024], vb[kRing][1024];
-  __shared__ unsigned long long odd_keys[3];  // keys of a step whose values are not finite
+  __shared__ int odd_seen;  // a value was not finite
   const int G = a.hq / a.hkv;
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5;
@@ -630,18 +699,25 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_to_lds(vp[i] + (int64_t)st * kTile, &vb[buf][64 * (wave + NW * i)]);
   };
-  // ... and in a step past the tile's first position its values are tamed where they lie
+  // ... and in a step past the tile's first position the values are tamed where they lie
   auto tame_step = [&](int st, int buf) {
+    uint32_t odd = 0;
 #pragma unroll
     for (int i = 0; i < 1024 / NT; ++i) {
-      const int c = tid + NT * i, part = (c & 7) ^ ((c >> 4) & 7);
-      const u32x4 w = vb[buf][c];
-      uint32_t odd = 0;
-      vb[buf][c] = __builtin_bit_cast(u32x4, tame(__builtin_bit_cast(half8_t, w), klast - (st * kTile + 8 * part), odd));
-      if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * part));
+      const int c = tid + NT * i, left = klast - (st * kTile + 8 * ((c & 7) ^ ((c >> 4) & 7)));
+      u32x4 w = vb[buf][c];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t v = w[x] & keep_mask(2 * x, left), o = odd_halves(v);
+        odd |= o;
+        w[x] = without(v, o);
+      }
+      vb[buf][c] = w;
     }
+    if (odd) odd_seen = 1;
   };
 
+  const CodeConsts kc;
   u32x4 pre[Q4 ? kCodes : 1];
   uint2 pre_ks[Q4 ? kCodes : 1];
   ValScales pre_vs;
@@ -663,11 +739,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
     }
   };
-  // a cell of eight positions of a dimension into the buffer
-  auto put_val = [&](int buf, int st, int d, int part, half8_t v, uint32_t& odd) {
-    if (st * (int64_t)kTile + kTile - 1 > pmin) v = tame(v, klast - (st * kTile + 8 * part), odd);  // uniform
-    vb[buf][d * 8 + (part ^ ((d >> 1) & 7))] = __builtin_bit_cast(u32x4, v);
-  };
   auto store_step = [&](int st, int buf) {
 #pragma unroll
     for (int i = 0; i < kCodes; ++i) {
@@ -675,7 +746,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       half8_t lo[2], hi[2];
       if (c < 256) {
         const int key = c >> 2, part = c & 3;
-        dequant_key(pre[i], pre_ks[i], lo, hi);
+        dequant_key(kc, pre[i], pre_ks[i], lo, hi);
         const int sw = swap23(key & 15);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -684,20 +755,29 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
       } else {
         const int c2 = c - 256, j = c2 >> 2, part = c2 & 3;
-        dequant_val<false>(pre[i], pre_vs, lo);
-        dequant_val<true>(pre[i], pre_vs, hi);
+        if (st * (int64_t)kTile + kTile - 1 > pmin) {  // uniform
+          uint32_t odd = 0;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              pre_vs.p[r][x >> 2][x & 3] =
+                  tame_scales(pre_vs.p[r][x >> 2][x & 3], 2 * x, klast - (st * kTile + 16 * part), (r & 1) == 0, odd);
+          if (odd) odd_seen = 1;
+        }
+        dequant_val<false>(kc, pre[i], pre_vs, lo);
+        dequant_val<true>(kc, pre[i], pre_vs, hi);
+        const int sw = (j >> 1) & 7;  // (of j + 64 too)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          uint32_t odd = 0;
-          put_val(buf, st, j, 2 * part + x, lo[x], odd);
-          put_val(buf, st, j + 64, 2 * part + x, hi[x], odd);
-          if (odd) atomicOr(&odd_keys[st % 3], (unsigned long long)odd << (8 * (2 * part + x)));
+          vb[buf][j * 8 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
+          vb[buf][(j + 64) * 8 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
         }
       }
     }
   };
 
-  if (tid < 3) odd_keys[tid] = 0;
+  if (tid == 0) odd_seen = 0;
   if constexpr (Q4) {
     __syncthreads();
     if (st0 < st1) {
@@ -746,7 +826,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         asm volatile("" ::: "memory");
       }
     }
-    if (tid == 0) odd_keys[(st + 2) % 3] = 0;
     if (owner && key0 <= wmax) {  // uniform in the wavefront
       float16_t sc[2];
 #pragma unroll
@@ -810,21 +889,6 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, w), pf[i >> 2], o[i & 3], 0, 0, 0);
         if (i + kDeep < 16) f[i % kDeep] = val_frag(i + kDeep);
       }
-      if (past) {
-        unsigned long long odd = odd_keys[st % 3];
-#pragma unroll 1
-        for (; odd; odd &= odd - 1) {
-          const int key = key0 + __builtin_ctzll(odd);
-          const OddValue ov = odd_value<Q4>(a, sg, key);
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float v = __shfl(ov.v[d >> 1], 32 * (d & 1) + 8 * (i >> 2) + 4 * h + (i & 3), kWave);
-              o[d][i] += key <= lpos ? v : 0.f;
-            }
-        }
-      }
     }
     if constexpr (Q4) {
       if (st + 1 < st1) store_step(st + 1, buf ^ 1);
@@ -832,6 +896,24 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     buf = buf + 1 == kRing ? 0 : buf + 1;
   }
   if (!owner) return;
+  if (odd_seen) {  // (written before the last step's barrier)
+#pragma unroll 1
+    for (int st = st0; st < st1; ++st) {
+      if (st * (int64_t)kTile + kTile - 1 <= pmin) continue;
+#pragma unroll 1
+      for (int key = st * kTile; key < st * kTile + kTile && key <= wmax && key <= klast; ++key) {
+        const OddValue ov = odd_value<Q4>(a, sg, key);
+        if (!__any(ov.v[0] != 0.f || ov.v[1] != 0.f)) continue;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float v = __shfl(ov.v[d >> 1], 32 * (d & 1) + 8 * (i >> 2) + 4 * h + (i & 3), kWave);
+            o[d][i] += key <= lpos ? v : 0.f;
+          }
+      }
+    }
+  }
   l = pair_fold(l, [](float x, float y) { return x + y; });
   if constexpr (SPLIT) {
     const int64_t at = (int64_t)blockIdx.x * TQ + 32 * wave + lc;
@@ -948,7 +1030,7 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
     p.tiles = pr.b;
     most = 256 / hkv;
     if (2 * b > most) most = 1024 / hkv;
-    if (2 * b > most || steps <= p.grain) most = 0;
+    if (2 * b > most || steps <= 2 * p.grain) most = 0;
   } else {
     auto tiles = [&](int64_t tq) {
       return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq

@@ -55,12 +55,18 @@ __device__ __forceinline__ int swap01(int i) { return (i & ~3) | ((i & 1) << 1) 
 __device__ __forceinline__ half2_t bits_h2(uint32_t u) { return __builtin_bit_cast(half2_t, u); }
 
 // Word `w` of four bytes to halves: codes 0 .. 3's low (HIGH: high) nibbles as 1024 + c (64 + c): c in the lowest (the
-// lowest bits but four) mantissa bits, one operation a pair.
+// lowest bits but four) mantissa bits, one v_and_or_b32 a pair.  That instruction takes no literals: the masks are held
+// in scalar, the other constants in vector registers, opaque to the compiler, which would split it otherwise.
+struct CodeConsts {
+  uint32_t mask[2], one[2];
+  __device__ __forceinline__ CodeConsts() : mask{0x000F000Fu, 0x00F000F0u}, one{0x64006400u, 0x54005400u} {
+    asm("" : "+s"(mask[0]), "+s"(mask[1]), "+v"(one[0]), "+v"(one[1]));
+  }
+};
 template <bool HIGH>
-__device__ __forceinline__ void code_pairs(uint32_t w, half2_t& a, half2_t& b) {
-  constexpr uint32_t mask = HIGH ? 0x00F000F0u : 0x000F000Fu, one = HIGH ? 0x54005400u : 0x64006400u;
-  a = bits_h2((w & mask) | one);
-  b = bits_h2(((w >> 8) & mask) | one);
+__device__ __forceinline__ void code_pairs(const CodeConsts& k, uint32_t w, half2_t& a, half2_t& b) {
+  a = bits_h2((w & k.mask[HIGH]) | k.one[HIGH]);
+  b = bits_h2(((w >> 8) & k.mask[HIGH]) | k.one[HIGH]);
 }
 // What code_pairs adds to the zero: (1024 + c) - (1024 + z) is exact.
 template <bool HIGH>
