@@ -294,7 +294,7 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
 // 16 and k = 8 lg .. +8 (lg = l / 16); D[4 lg + i][li].  Row r of the key tile kt is key 16 (r / 4) + 4 kt + r % 4, so a
 // lane ends with the scores of keys 16 lg .. 16 lg + 15 of query li, and takes the values of those keys as they lie.
 // A step's keys are loaded while the step before takes its values, and the other way round, each into the registers that
-// were just used (fp16 and two tiles: the registers do not hold both, and a step's loads are issued at its start).  Up to
+// were just used (fp16 and two tiles: the registers hold only one of the two, loaded when its turn comes).  Up to
 // 32 queries: all eight wavefronts take keys; up to 64: half of them the first 32, half the rest, over the same keys.
 constexpr int kFewWaves = 8;
 
@@ -416,10 +416,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     const int64_t key0 = (int64_t)st * kTile;
     const int next = st + NW < st1 ? st + NW : st;  // (the last step's loads are repeated: no branch around loads)
     float4_t sc[NQT][4];
-    if constexpr (!kAhead) {
-      load_k(st);
-      load_v(st);
-    }
+    if constexpr (!kAhead) load_k(st);
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       half8_t kf[4];
@@ -446,7 +443,10 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       }
       if constexpr (NQT > 1) __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (kAhead) load_k(next);
+    if constexpr (kAhead)
+      load_k(next);
+    else
+      load_v(st);
     __builtin_amdgcn_sched_barrier(0);
     // only a step past the first row's position holds keys that some row may not read
     const bool tail = key0 + kTile - 1 > p0;  // uniform
@@ -496,18 +496,17 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         for (int x = 0; x < 8; ++x) {
           const uint32_t keep = keep_mask(2 * x, left);
 #pragma unroll
-          for (int d = 0; d < 8; ++d) {
-            vw[2 * d + (x >> 2)][x & 3] &= keep;
-            odd |= odd_halves(vw[2 * d + (x >> 2)][x & 3]);
-          }
+          for (int d = 0; d < 8; ++d) vw[2 * d + (x >> 2)][x & 3] &= keep;
         }
-        if (__any(odd != 0)) {
+        if (sr.n > 1) {  // (a single row reads every key that is left)
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            asm volatile("" : "+v"(vw[x]));  // (or the tests above would be kept in registers for this)
+          for (int x = 0; x < 16; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vw[x][i] = without(vw[x][i], odd_halves(vw[x][i]));
-          }
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t o = odd_halves(vw[x][i]);
+              odd |= o;
+              vw[x][i] = without(vw[x][i], o);
+            }
         }
       }
       odd_seen |= __any(odd != 0);
