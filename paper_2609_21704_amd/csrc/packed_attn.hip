@@ -60,9 +60,13 @@ __device__ __forceinline__ bool nonfinite_h(half_t v) { return (__builtin_bit_ca
 // sums are one reduction; the first for more).
 struct SeqWork {
   int tiles, steps;
+  SeqRows rows;
+  int64_t p0;  // position of the first row
 };
 struct Unit {
   int s, tile, part, span, steps;
+  SeqRows rows;
+  int64_t p0;
 };
 
 __device__ __forceinline__ float wave_total(float v) {
@@ -82,14 +86,14 @@ struct Planner {
 
   __device__ __forceinline__ SeqWork at(int base) const {
     if (base == 0) return mine;
-    return base + lane < b ? work(base + lane) : SeqWork{0, 0};
+    return base + lane < b ? work(base + lane) : SeqWork{};
   }
   static __device__ __forceinline__ int parts(SeqWork w, int span) {
     return w.steps > span ? (w.steps + span - 1) / span : 1;
   }
 
   __device__ __forceinline__ Planner(int b, int most, int grain, F work) : b(b), span(1 << 30), lane(threadIdx.x & 63), work(work) {
-    mine = lane < b ? work(lane) : SeqWork{0, 0};
+    mine = lane < b ? work(lane) : SeqWork{};
     if (most == 0) return;
     float S = 0.f, N = 0.f;  // (sums a little off in fp32; S is taken 2^-16 larger)
     for (int base = 0; base < b; base += kWave) {
@@ -112,6 +116,17 @@ struct Planner {
     span = __builtin_amdgcn_readfirstlane(span);
   }
 
+  // what lane l holds of sequence s
+  __device__ __forceinline__ void fill(Unit& u, int s, const SeqWork& w, int l) const {
+    u.s = s;
+    u.span = span;
+    u.steps = __builtin_amdgcn_readlane(w.steps, l);
+    u.rows.first = __builtin_amdgcn_readlane(w.rows.first, l);
+    u.rows.n = __builtin_amdgcn_readlane(w.rows.n, l);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)w.p0, l);
+    u.p0 = (int64_t)__builtin_amdgcn_readlane((int)(w.p0 >> 32), l) << 32 | lo;
+  }
+
   // Unit `item` of the list (sequence 0: tile 0 with its parts, tile 1, ..; sequence 1: ..); false past its end.
   __device__ __forceinline__ bool find(int item, Unit& u) const {
     int before = 0;
@@ -124,11 +139,9 @@ struct Planner {
         const int l = __builtin_ctzll(__ballot(before + incl > item));
         const int k = item - before - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(n, l));
         const int pl = __builtin_amdgcn_readlane(np, l);
-        u.s = base + l;
+        fill(u, base + l, w, l);
         u.tile = k / pl;
         u.part = k - u.tile * pl;
-        u.span = span;
-        u.steps = __builtin_amdgcn_readlane(w.steps, l);
         return true;
       }
       before += total;
@@ -147,11 +160,9 @@ struct Planner {
       if (item < before + total) {
         const int l = __builtin_ctzll(__ballot(before + incl > item));
         const int tl = __builtin_amdgcn_readlane(w.tiles, l), pl = __builtin_amdgcn_readlane(np, l);
-        u.s = base + l;
+        fill(u, base + l, w, l);
         u.tile = item - before - (__builtin_amdgcn_readlane(incl, l) - tl);
         u.part = 0;
-        u.span = span;
-        u.steps = __builtin_amdgcn_readlane(w.steps, l);
         first = before_p + __builtin_amdgcn_readlane(incl_p, l) - tl * pl + u.tile * pl;
         return true;
       }
@@ -182,9 +193,9 @@ __device__ __forceinline__ int steps_to(int klast) { return klast < 0 ? 0 : klas
 
 // Tiles of TQ queries of a sequence, and its steps.
 __device__ __forceinline__ SeqWork seq_work(const PackedRows& pr, const AttnArgs& a, int G, int TQ, int s) {
+  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
   const SeqRows sr = seq_rows(pr, s);
-  const int64_t pl = (int64_t)a.pos_base[s] + a.pos_offset + sr.n - 1;
-  return {(sr.n * G + TQ - 1) / TQ, steps_to(last_key(pl, a.len_bound))};
+  return {(sr.n * G + TQ - 1) / TQ, steps_to(last_key(p0 + sr.n - 1, a.len_bound)), sr, p0};
 }
 
 // ------------------------------------------------------------------ dequant
@@ -318,13 +329,12 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   } else {  // an item a sequence
     const SeqWork w = seq_work(pr, a, G, 16 * NQT * HALVES, item);
     if (w.tiles == 0) return;
-    u = {item, 0, 0, 1 << 30, w.steps};
+    u = {item, 0, 0, 1 << 30, w.steps, w.rows, w.p0};
   }
-  const int s = u.s;
-  const int64_t sg = (int64_t)s * a.hkv + g;
-  const SeqRows sr = seq_rows(pr, s);
+  const int64_t sg = (int64_t)u.s * a.hkv + g;
+  const SeqRows sr = u.rows;
   const int nq = sr.n * G;
-  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
+  const int64_t p0 = u.p0;
   const int64_t klast = last_key(p0 + sr.n - 1, a.len_bound);
   const int st0 = u.part * u.span, st1 = st0 + u.span < u.steps ? st0 + u.span : u.steps;
 
@@ -661,18 +671,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const Planner plan(pr.b, SPLIT ? a.most : 0, 1, [&](int i) { return seq_work(pr, a, G, TQ, i); });
     if (!plan.find(item, u)) return;
   }
-  const int s = u.s;
-  const SeqRows sr = seq_rows(pr, s);
+  const SeqRows sr = u.rows;
   const int nq = sr.n * G;
   const int qt = (nq + TQ - 1) / TQ - 1 - u.tile;  // the latest rows (the most keys) first
-  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
+  const int64_t p0 = u.p0;
   const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
   const int64_t pmin = p0 + qt * TQ / G;
   const int klast = last_key(p0 + qlast / G, a.len_bound), nst = steps_to(klast);
   const int st0 = SPLIT ? u.part * u.span : 0;
   const int st1 = SPLIT && st0 + u.span < nst ? st0 + u.span : nst;
   if (SPLIT && u.part > 0 && st0 >= st1) return;  // (part 0 always answers: rows without any key)
-  const int64_t sg = (int64_t)s * a.hkv + g;
+  const int64_t sg = (int64_t)u.s * a.hkv + g;
   const int wq = qt * TQ + 32 * wave;                       // the wavefront's first query
   const bool owner = wq < nq;
   const int qi = wq + lc < nq ? wq + lc : nq - 1, qj = qi / G;
@@ -955,12 +964,11 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
     const Planner plan(pr.b, a.most, grain, [&](int i) { return seq_work(pr, a, G, TQ, i); });
     if (!plan.find_tile_parts(item, u, first)) return;
   }
-  const int s = u.s;
-  const SeqRows sr = seq_rows(pr, s);
+  const SeqRows sr = u.rows;
   const int nq = sr.n * G, qt = few ? 0 : (nq + TQ - 1) / TQ - 1 - u.tile;
   const int qx = blockIdx.y * 4 + wave, qi = qt * TQ + qx;
   if (qx >= TQ || qi >= nq) return;
-  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
+  const int64_t p0 = u.p0;
   const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
   const int nst = steps_to(last_key(p0 + qlast / G, a.len_bound));
   const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
