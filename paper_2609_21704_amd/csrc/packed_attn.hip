@@ -50,8 +50,6 @@ __device__ __forceinline__ float pair_fold(float v, OP op) {
   return op(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1));
 }
 
-__device__ __forceinline__ bool nonfinite_h(half_t v) { return (__builtin_bit_cast(uint16_t, v) & 0x7C00) == 0x7C00; }
-
 // How the work is laid over workgroups.  A sequence's queries are `tiles` tiles, each over the sequence's `steps` steps of
 // 64 keys, and every tile's steps are cut into parts of `span`: `span` is what keeps the number of parts of all sequences
 // within `most` (0: no cutting), so that sequences of different lengths give workgroups of like length.  Every workgroup
@@ -118,7 +116,7 @@ struct Planner {
 
   // what lane l holds of sequence s
   __device__ __forceinline__ void fill(Unit& u, int s, const SeqWork& w, int l) const {
-    u.s = s;
+    u.s = __builtin_amdgcn_readfirstlane(s);
     u.span = span;
     u.steps = __builtin_amdgcn_readlane(w.steps, l);
     u.rows.first = __builtin_amdgcn_readlane(w.rows.first, l);
@@ -636,12 +634,15 @@ __device__ __forceinline__ int swap23(int i) { return (i & ~12) | ((i & 4) << 1)
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// 16 bytes per lane from memory to LDS: lane l's go to dst + 16 l (dst uniform).  In assembly, because the compiler waits
-// for all loads of the builtin before any read of LDS, whichever buffer it reads; the waits are barrier_after_loads.
-// There is no result register, and the addresses are read when the load is issued.
-__device__ __forceinline__ void load_to_lds(const void* src, void* dst) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)dst);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(at) : "memory", "m0");
+// 16 bytes per lane from memory to LDS: from base + off (off per lane) to the LDS address dst + 16 l for lane l.  In
+// assembly, because the compiler waits for all loads of the builtin before any read of LDS, whichever buffer it reads;
+// the waits are barrier_after_loads.  There is no result register, and the addresses are read when the load is issued.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst) : "memory");
+}
+template <class T>
+__device__ __forceinline__ uint32_t lds_address(T* p) {
+  return (uint32_t)(uintptr_t)(lds_void*)p;
 }
 
 // All but the wavefront's last N loads, and everything it did in LDS, done by every wavefront.
@@ -678,10 +679,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
   const int64_t pmin = p0 + qt * TQ / G;
   const int klast = last_key(p0 + qlast / G, a.len_bound), nst = steps_to(klast);
-  const int st0 = SPLIT ? u.part * u.span : 0;
+  const int st0 = SPLIT ? __builtin_amdgcn_readfirstlane(u.part * u.span) : 0;
   const int st1 = SPLIT && st0 + u.span < nst ? st0 + u.span : nst;
   if (SPLIT && u.part > 0 && st0 >= st1) return;  // (part 0 always answers: rows without any key)
-  const int64_t sg = (int64_t)u.s * a.hkv + g;
+  const int64_t sg = (int64_t)__builtin_amdgcn_readfirstlane(u.s) * a.hkv + g;
   const int wq = qt * TQ + 32 * wave;                       // the wavefront's first query
   const bool owner = wq < nq;
   const int qi = wq + lc < nq ? wq + lc : nq - 1, qj = qi / G;
@@ -691,21 +692,25 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int wmax = clip(p0 + (wq + 31 < nq ? wq + 31 : nq - 1) / G);
 
   // fp16: load i of a step takes cells 64 (wave + NW i) .. +64 of the keys and of the values; what a cell of LDS holds is
-  // chosen by where its lane reads
-  const uint16_t* kp[kLoads];
-  const uint16_t* vp[kLoads];
+  // chosen by where its lane reads: a scalar base a load and a 32-bit offset a lane (seven rows of values at most)
+  const uint16_t* k16 = a.c.k + sg * a.capacity * kHd;
+  const uint16_t* v16[kLoads];
+  uint32_t koff[kLoads], voff;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int ci = wave + NW * i;
-    const int row = 4 * ci + (lane >> 4), d = 8 * ci + (lane >> 3);
-    kp[i] = Q4 ? nullptr : a.c.k + (sg * a.capacity + row) * kHd + ((lane & 15) ^ swap23(row & 15)) * 8;
-    vp[i] = Q4 ? nullptr : a.c.v + (sg * kHd + d) * a.capacity + ((lane & 7) ^ ((d >> 1) & 7)) * 8;
+    const int row = 4 * (wave + NW * i) + (lane >> 4);
+    koff[i] = row * 256 + 16 * ((lane & 15) ^ swap23(row & 15));
+    v16[i] = a.c.v + (sg * kHd + 8 * (wave + NW * i)) * a.capacity;
   }
+  // (dimension d = 8 (wave + NW i) + lane / 8: d / 2 % 8 is 4 (wave % 2) + lane / 16, NW even)
+  voff = (uint32_t)(lane >> 3) * (uint32_t)(2 * a.capacity) + 16 * ((lane & 7) ^ (4 * (wave & 1) + (lane >> 4)));
+  const uint32_t kdst = lds_address(&kb[0][64 * wave]), vdst = lds_address(&vb[0][64 * wave]);
   auto issue_step = [&](int st, int buf) {
+    const uint16_t* kst = k16 + (int64_t)st * (kTile * kHd);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds(kp[i] + (int64_t)st * (kTile * kHd), &kb[buf][64 * (wave + NW * i)]);
+    for (int i = 0; i < kLoads; ++i) load_to_lds(kst, koff[i], kdst + 16384 * buf + 1024 * NW * i);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds(vp[i] + (int64_t)st * kTile, &vb[buf][64 * (wave + NW * i)]);
+    for (int i = 0; i < kLoads; ++i) load_to_lds(v16[i] + (int64_t)st * kTile, voff, vdst + 16384 * buf + 1024 * NW * i);
   };
   // ... and in a step past the tile's first position the values are tamed where they lie
   auto tame_step = [&](int st, int buf) {
@@ -841,7 +846,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
       // fragment i of the keys: half i % 2 of the tile, dimensions 16 (i / 2) .. +16; kDeep of them ahead of the products
-      constexpr int kDeep = Q4 ? 2 : 4;
+      constexpr int kDeep = Q4 ? 2 : 8;
       u32x4 f[kDeep];
       auto key_frag = [&](int i) { return kb[buf][(i & 1) * 512 + krow + ((2 * (i >> 1) + h) ^ (lc & 15))]; };
 #pragma unroll
