@@ -39,6 +39,7 @@ struct AttnArgs {
   float* part_o;    // [unit][kv head][query][128], null without splitting
   float2* part_ml;  // [unit][kv head][query]
   int most;         // parts of one kv head, 0 without splitting
+  bool longest;     // the tiles with the most keys first (they do not all run at once)
 };
 
 // max / sum over the two lanes that share a column of a 32 x 32 product
@@ -67,6 +68,12 @@ struct Unit {
   int64_t p0;
 };
 
+template <int Ctrl>
+__device__ __forceinline__ float dpp_move(float v) {
+  return __builtin_bit_cast(float,
+                            __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), Ctrl, 0xF, 0xF, false));
+}
+
 __device__ __forceinline__ float wave_total(float v) {
   const uint32_t u = __builtin_bit_cast(uint32_t, quad_sum(v));
   float x = __builtin_bit_cast(float, u);
@@ -74,6 +81,14 @@ __device__ __forceinline__ float wave_total(float v) {
   x = dpp_add<0x4E>(x);   // quad_perm [2,3,0,1]
   x = dpp_add<0x141>(x);  // row_half_mirror
   return dpp_add<0x140>(x);  // row_mirror
+}
+
+__device__ __forceinline__ float wave_most(float v) {
+  float x = quad_max(v);
+  x = fmaxf(x, dpp_move<0xB1>(x));
+  x = fmaxf(x, dpp_move<0x4E>(x));
+  x = fmaxf(x, dpp_move<0x141>(x));
+  return fmaxf(x, dpp_move<0x140>(x));
 }
 
 template <class F>
@@ -145,6 +160,46 @@ struct Planner {
       before += total;
     }
     return false;
+  }
+
+  // Unit `item` of the list of whole tiles by the number of their keys, the most first, for up to 64 sequences (the plain
+  // list for more).  TQ queries are G-th as many rows, so a tile's place is its level: the sequence's tiles from its last,
+  // after as many as it is shorter than the longest sequence.  B(v), the tiles below level v, is one reduction; the search
+  // for the item's level takes three of them a turn.
+  __device__ __forceinline__ bool find_longest(int item, int G, int TQ, Unit& u) const {
+    if (b > kWave) return find(item, u);
+    const float longest = wave_most((float)mine.steps);
+    const int off = mine.tiles > 0 ? (int)((longest - (float)mine.steps) * (float)(kTile * G) / (float)TQ) : 1 << 24;
+    const int levels = (int)wave_most(mine.tiles > 0 ? (float)(off + mine.tiles) : 0.f);
+    auto below = [&](int v) {
+      const int n = v - off;
+      return wave_total((float)(n < 0 ? 0 : (n > mine.tiles ? mine.tiles : n)));
+    };
+    int lo = 0, hi = levels;  // B(lo) <= item < B(hi)
+    if ((float)item >= below(hi)) return false;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 3) / 4;
+      int cut[3];
+      float n[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        cut[i] = lo + step * (i + 1) < hi ? lo + step * (i + 1) : hi;
+        n[i] = below(cut[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        if (n[i] <= (float)item) lo = cut[i];
+      hi = lo + step < hi ? lo + step : hi;
+    }
+    const bool in = off <= lo && lo < off + mine.tiles;
+    const uint64_t set = __ballot(in);
+    const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0));
+    const int k = item - (int)below(lo);
+    const int l = __builtin_ctzll(__ballot(in && rank == k));
+    fill(u, l, mine, l);
+    u.tile = lo - __builtin_amdgcn_readlane(off, l);
+    u.part = 0;
+    return true;
   }
 
   // Tile `item` of the list without parts, and the index of its first part in the list with them.
@@ -317,8 +372,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   __shared__ __align__(16) uint16_t vsb[Q4 ? kFewWaves : 1][4][64];  // a step's scales and zeros of values, per wavefront
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
-  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 % NW;
-  const int q0 = wave8 / NW * (16 * NQT);  // the wavefront's first query
+  const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 / HALVES;
+  const int q0 = wave8 % HALVES * (16 * NQT);  // the wavefront's first query
   const int G = a.hq / a.hkv;
   Unit u;
   if (a.most) {
@@ -408,6 +463,15 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     }
   };
   const int end = HALVES == 1 || q0 < nq ? st1 : 0;
+  // Of the two wavefronts of a SIMD the older issues first and was done after 22 us of 36 with half of the steps (16
+  // sequences, 22k positions on average): the older ones take three of five, steps wave + NW {0, 1, 2} of every 5 NW / 2.
+  const bool older = wave < NW / 2;
+  int turn = 0;
+  auto advance = [&](int st) {
+    const int gap = older ? (turn == 2 ? NW / 2 : NW) : (turn == 1 ? NW + NW / 2 : NW);
+    turn = turn == (older ? 2 : 1) ? 0 : turn + 1;
+    return st + gap;
+  };
   if (kAhead && st0 + wave < end) {
     load_k(st0 + wave);
     load_v(st0 + wave);
@@ -420,9 +484,10 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     }
   };
   bool odd_seen = false;
-  for (int st = st0 + wave; st < end; st += NW) {
+  for (int st = st0 + wave, following; st < end; st = following) {
     const int64_t key0 = (int64_t)st * kTile;
-    const int next = st + NW < st1 ? st + NW : st;  // (the last step's loads are repeated: no branch around loads)
+    following = advance(st);
+    const int next = following < st1 ? following : st;  // (the last step's loads are repeated: no branch around loads)
     float4_t sc[NQT][4];
     if constexpr (!kAhead) load_k(st);
 #pragma unroll
@@ -556,8 +621,9 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     __builtin_amdgcn_sched_barrier(0);
   }
   if (odd_seen) {
+    turn = 0;
 #pragma unroll 1
-    for (int st = st0 + wave; st < end; st += NW) {
+    for (int st = st0 + wave; st < end; st = advance(st)) {
       const int64_t key0 = (int64_t)st * kTile;
       if (key0 + kTile - 1 <= p0) continue;
 #pragma unroll 1
@@ -586,17 +652,17 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   }
   __syncthreads();
   for (int qi = tid >> 4; qi < nq; qi += 4 * kFewWaves) {
-    const int d0 = 8 * (tid & 15), w0 = qi / (16 * NQT) * NW, qx = qi & (16 * NQT - 1);
+    const int d0 = 8 * (tid & 15), half = qi / (16 * NQT), qx = qi & (16 * NQT - 1);
     float M = kNoMax, L = 0.f, r[8] = {};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[w0 + w][qx].x);
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, ml[HALVES * w + half][qx].x);
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float2 x = ml[w0 + w][qx];
+      const float2 x = ml[HALVES * w + half][qx];
       const float f = exp2_fast(x.x - M);
       L += f * x.y;
-      const float4_t u = *reinterpret_cast<const float4_t*>(&ob[w0 + w][qx][d0]);
-      const float4_t v = *reinterpret_cast<const float4_t*>(&ob[w0 + w][qx][d0 + 4]);
+      const float4_t u = *reinterpret_cast<const float4_t*>(&ob[HALVES * w + half][qx][d0]);
+      const float4_t v = *reinterpret_cast<const float4_t*>(&ob[HALVES * w + half][qx][d0 + 4]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         r[i] += f * u[i];
@@ -670,7 +736,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   Unit u;
   {
     const Planner plan(pr.b, SPLIT ? a.most : 0, 1, [&](int i) { return seq_work(pr, a, G, TQ, i); });
-    if (!plan.find(item, u)) return;
+    if (!SPLIT && a.longest ? !plan.find_longest(item, G, TQ, u) : !plan.find(item, u)) return;
   }
   const SeqRows sr = u.rows;
   const int nq = sr.n * G;
@@ -939,45 +1005,42 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
             float4_t{o[d][4 * x], o[d][4 * x + 1], o[d][4 * x + 2], o[d][4 * x + 3]};
     if (h == 0) a.part_ml[at] = make_float2(m, l);
   } else {
-    if (wq + lc >= nq) return;
+    const bool real = wq + lc < nq;
     const int64_t pos = p0 + qj;
     const bool bad = pos < 0 || pos >= a.len_bound;
     const float inv = 1.f / l;
-    uint16_t* dst = a.out + ((int64_t)(sr.first + qj) * a.hq + g * G + (qi - qj * G)) * kHd + 4 * h;
-    const half_t nan = __builtin_bit_cast(half_t, kNanF16);
+    uint16_t* dst = a.out + ((int64_t)(sr.first + qj) * a.hq + g * G + (qi - qj * G)) * kHd + 8 * h;
+    // the lane pairs of a query exchange halves of every 16 dimensions, for stores of 16 bytes
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        half4_t v;
+      for (int x = 0; x < 4; x += 2) {
+        uint32_t w[2][2];  // dimensions 8 (x + j) + 4 h + 2 e, + 1
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = bad ? nan : (half_t)(o[d][4 * x + e] * inv);
-        *reinterpret_cast<half4_t*>(dst + 32 * d + 8 * x) = v;
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const half2_t v = {(half_t)(o[d][4 * (x + j) + 2 * e] * inv), (half_t)(o[d][4 * (x + j) + 2 * e + 1] * inv)};
+            w[j][e] = bad ? kNanF16 * 0x10001u : __builtin_bit_cast(uint32_t, v);
+          }
+        u32x4 c;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const auto s = __builtin_amdgcn_permlane32_swap(w[0][e], w[1][e], false, false);
+          const uint32_t s0 = s[0], s1 = s[1];
+          c[e] = s0;
+          c[2 + e] = s1;
+        }
+        if (real) *reinterpret_cast<u32x4*>(dst + 32 * d + 8 * x) = c;
       }
   }
 }
 
-// The parts of each query joined, in their order: a wavefront per query, lane i the weight of part i (at most 512 parts:
-// eight a lane), then every lane two dimensions, eight parts' sums in flight.
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain, bool few) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int G = a.hq / a.hkv;
-  const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
-  Unit u;
-  int first;
-  {
-    const Planner plan(pr.b, a.most, grain, [&](int i) { return seq_work(pr, a, G, TQ, i); });
-    if (!plan.find_tile_parts(item, u, first)) return;
-  }
-  const SeqRows sr = u.rows;
-  const int nq = sr.n * G, qt = few ? 0 : (nq + TQ - 1) / TQ - 1 - u.tile;
-  const int qx = blockIdx.y * 4 + wave, qi = qt * TQ + qx;
-  if (qx >= TQ || qi >= nq) return;
-  const int64_t p0 = u.p0;
-  const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
-  const int nst = steps_to(last_key(p0 + qlast / G, a.len_bound));
-  const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
-  const int64_t row0 = ((int64_t)first * a.hkv + g) * TQ + qx, stride = (int64_t)a.hkv * TQ;  // (row p: part p's sums)
+// The parts of query qi joined, in their order: lane i the weight of part i (at most 512 parts: eight a lane), then every
+// lane two dimensions, eight parts' sums in flight.  row0: the query's row of part 0's sums.
+__device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr, int64_t p0, int qi, int parts,
+                                     int64_t row0, int64_t stride) {
+  const int lane = threadIdx.x & 63;
   constexpr int kMost = 8;
   float2 ml[kMost];
   float M = kNoMax, L = 0.f;
@@ -1022,6 +1085,29 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   *reinterpret_cast<half2_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + 2 * lane) = r;
 }
 
+// Four queries of a tile a workgroup, one a wavefront (four a wavefront, 16 a workgroup: 11.7 us for 8.4).
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain, bool few) {
+  const int wave = threadIdx.x >> 6;
+  const int G = a.hq / a.hkv;
+  const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
+  Unit u;
+  int first;
+  {
+    const Planner plan(pr.b, a.most, grain, [&](int i) { return seq_work(pr, a, G, TQ, i); });
+    if (!plan.find_tile_parts(item, u, first)) return;
+  }
+  const SeqRows sr = u.rows;
+  const int nq = sr.n * G, qt = few ? 0 : (nq + TQ - 1) / TQ - 1 - u.tile;
+  const int64_t p0 = u.p0;
+  const int qlast = (qt + 1) * TQ < nq ? (qt + 1) * TQ - 1 : nq - 1;
+  const int nst = steps_to(last_key(p0 + qlast / G, a.len_bound));
+  const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
+  const int64_t stride = (int64_t)a.hkv * TQ;  // rows of the sums from one part to the next
+  const int qx = blockIdx.y * 4 + wave;
+  if (qt * TQ + qx < nq)
+    join(a, G, g, sr, p0, qt * TQ + qx, parts, ((int64_t)first * a.hkv + g) * TQ + qx, stride);
+}
+
 struct Plan {
   bool few;
   int tq, grain;    // queries of a tile; steps that a part's are a multiple of
@@ -1048,7 +1134,7 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
       return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq
                       : (int64_t)pr.b * (((int64_t)pr.max_rows * G + tq - 1) / tq);
     };
-    p.tq = tiles(256) * hkv >= 512 ? 256 : 128;
+    p.tq = tiles(256) * hkv >= 1536 ? 256 : 128;
     p.tiles = (int)tiles(p.tq);
     most = 256 / hkv;
     if (2 * p.tiles > most || steps <= 4) most = 0;
@@ -1082,7 +1168,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
                                    int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
                                    uint16_t* out, hipStream_t stream) {
   const Plan p = make_plan(pr, hq, hkv, len_bound);
-  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most};
+  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most, false};
   const int units = p.most ? p.most : p.tiles;
   if (p.most) {
     const size_t queries = (size_t)units * hkv * p.tq;
@@ -1094,6 +1180,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
   }
   const bool q4 = cache.k4 != nullptr;
   const dim3 grid((unsigned)(units * hkv));
+  a.longest = !p.few && (int64_t)units * hkv > (p.tq == 256 ? 256 : 512);
   if (p.few) {
     if (q4)
       launch_few<true>(p, grid, pr, a, stream);

@@ -262,7 +262,10 @@ ATTN = [([(1, 0)], 1, 1, 64), ([(1, 63)], 16, 1, 64), ([(1, 64), (1, 0), (1, 127
         ([(65, 0)], 1, 1, 128), ([(19, 45), (1, 3)], 28, 4, 64), ([(100, 0), (0, 0), (1, 0), (64, 64), (37, 1)], 28, 4, 128),
         ([(57, 8000), (17, 333)], 28, 4, 8064), ([(130, 62)], 7, 1, 192), ([(255, 1), (257, 0)], 1, 1, 320),
         ([(900, 0), (331, 12)], 40, 8, 960), ([(2300, 0)], 28, 4, 2304), ([(700, 0), (1300, 0), (90, 500)], 16, 16, 1344),
-        ([(3, 0)] * 80, 28, 1, 64)]
+        ([(3, 0)] * 80, 28, 1, 64),
+        # more tiles than run at once: 28 sequences of 0 to 300 rows, some after cached ones; more than 64; tiles of 256
+        ([((37 * i * i) % 301, (i % 5) * 40) for i in range(28)], 28, 4, 512),
+        ([((53 * i) % 61, i % 3) for i in range(90)], 40, 8, 64), ([(4900, 0), (4300, 400), (1, 0), (700, 0)], 40, 8, 4928)]
 
 
 @pytest.mark.parametrize("seqs,hq,hkv,cap", ATTN)
