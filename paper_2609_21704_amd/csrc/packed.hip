@@ -107,14 +107,17 @@ struct RopeArgs {
 };
 
 // Sixteen lanes take one (row, head): lane t the elements 4 t .. 4 t + 3 and 64 + those, which are four pairs of the
-// rotation and one word of codes.
+// rotation and one word of codes.  The 16 such groups of a workgroup take a row each and walk its heads, whose rows of
+// the projection follow one another in memory, one load ahead; where a tile has fewer rows (blocks, single tokens),
+// several groups share a row's heads.
 template <bool Q4>
 __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArgs a) {
-  __shared__ float2 tab[kTileRows][64];                     // cosine, sine of (row, pair)
-  __shared__ __align__(16) uint16_t vt[Q4 ? 1 : kHd][kTileRows];          // one head's values, position-minor
-  __shared__ __align__(16) uint8_t vc4[Q4 ? 64 : 1][kTileRows];
+  __shared__ float2 tab[kTileRows][64];                             // cosine, sine of (row, pair)
+  __shared__ __align__(16) uint16_t vt[Q4 ? 1 : kTileRows][kHd + 4];  // one head's values
+  __shared__ __align__(16) uint8_t vc4[Q4 ? kTileRows : 1][68];
   __shared__ uint16_t vs4[Q4 ? 4 : 1][kTileRows];
   const int tid = threadIdx.x, t0 = 4 * (tid & 15), unit = tid >> 4;
+  const double freq = rope_freq(tid & 63, a.base);  // (beside the loads of the rows' bounds)
   if (pr.start && a.status && blockIdx.x == 0 && blockIdx.y == 0) {
     for (int s = tid; s < pr.b; s += 256) {
       const int x = pr.start[s], y = pr.start[s + 1];
@@ -123,85 +126,107 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
   }
   RowTile rt;
   if (!row_tile(pr, a.pos_base, a.pos_offset, blockIdx.x, rt)) return;  // uniform
-  const double freq = rope_freq(tid & 63, a.base);
-  for (int r = tid >> 6; r < rt.nr; r += 4) tab[r][tid & 63] = rope_cos_sin(rt.pos0 + r, freq);
-  __syncthreads();
-  const int nh = a.hq + 2 * a.hkv, share = blockIdx.y, shares = gridDim.y;
-  auto valid = [&](int r) { return rt.pos0 + r >= 0 && rt.pos0 + r < a.len_bound; };
-  if (share == 0 && tid < rt.nr && !valid(tid)) flag(a.status, kBadPos);
-  const int turned = a.hq + a.hkv;
-  const int mine = (turned - share + shares - 1) / shares;  // heads share, share + shares, .. below `turned`
-  auto load = [&](int r, int hh, float4_t& lo, float4_t& hi) {
-    const float* src = a.qkv + ((int64_t)(rt.row0 + r) * nh + hh) * kHd + t0;
-    lo = *reinterpret_cast<const float4_t*>(src);
-    hi = *reinterpret_cast<const float4_t*>(src + 64);
+  const int nh = a.hq + 2 * a.hkv, turned = a.hq + a.hkv, share = blockIdx.y, shares = gridDim.y;
+  const int per = (turned + shares - 1) / shares, head0 = share * per;
+  const int head1 = head0 + per < turned ? head0 + per : turned;
+  const int lg = rt.nr > 8 ? 0 : (rt.nr > 4 ? 1 : (rt.nr > 2 ? 2 : (rt.nr > 1 ? 3 : 4)));  // 2^lg groups a row
+  const int r = unit >> lg, step = 1 << lg;
+  const bool busy = r < rt.nr;
+  struct Raw {
+    float4_t lo, hi;
+    half4_t bl, bh;
+  };
+  auto load = [&](int row, int hh) {
+    Raw w;
+    const float* src = a.qkv + ((int64_t)(rt.row0 + row) * nh + hh) * kHd + t0;
+    w.lo = *reinterpret_cast<const float4_t*>(src);
+    w.hi = *reinterpret_cast<const float4_t*>(src + 64);
     if (a.bias) {
-      const half4_t bl = *reinterpret_cast<const half4_t*>(a.bias + hh * kHd + t0);
-      const half4_t bh = *reinterpret_cast<const half4_t*>(a.bias + hh * kHd + t0 + 64);
+      w.bl = *reinterpret_cast<const half4_t*>(a.bias + hh * kHd + t0);
+      w.bh = *reinterpret_cast<const half4_t*>(a.bias + hh * kHd + t0 + 64);
+    }
+    return w;
+  };
+  auto add_bias = [&](Raw& w) {
+    if (a.bias) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        lo[x] += (float)bl[x];
-        hi[x] += (float)bh[x];
+        w.lo[x] += (float)w.bl[x];
+        w.hi[x] += (float)w.bh[x];
       }
     }
   };
-  for (int i = unit; i < rt.nr * mine; i += 16) {
-    const int r = i / mine, hh = share + (i - r * mine) * shares;
-    float4_t lo, hi;
-    load(r, hh, lo, hi);
-    half4_t ol, oh;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      float ra, re;
-      rope_turn(lo[x], hi[x], tab[r][t0 + x], ra, re);
-      ol[x] = (half_t)ra;
-      oh[x] = (half_t)re;
-    }
+  int hh = head0 + (unit & (step - 1));
+  Raw next;
+  if (busy && hh < head1) next = load(r, hh);
+  for (int i = tid >> 6; i < rt.nr; i += 4) tab[i][tid & 63] = rope_cos_sin(rt.pos0 + i, freq);
+  __syncthreads();
+  auto valid = [&](int row) { return rt.pos0 + row >= 0 && rt.pos0 + row < a.len_bound; };
+  if (share == 0 && tid < rt.nr && !valid(tid)) flag(a.status, kBadPos);
+  if (busy) {
     const bool ok = valid(r);
-    if (hh < a.hq) {
-      const half_t nan = __builtin_bit_cast(half_t, kNanF16);
-      if (!ok) ol = oh = half4_t{nan, nan, nan, nan};
-      uint16_t* dst = a.q_out + ((int64_t)(rt.row0 + r) * a.hq + hh) * kHd + t0;
-      *reinterpret_cast<half4_t*>(dst) = ol;
-      *reinterpret_cast<half4_t*>(dst + 64) = oh;
-    } else if (Q4) {
-      const half_t wl[4] = {ol[0], ol[1], ol[2], ol[3]}, wh[4] = {oh[0], oh[1], oh[2], oh[3]};
-      const Q4Group gl = quantize_group(wl), gh = quantize_group(wh);
-      if (ok) {
-        const int64_t e = ((int64_t)rt.s * a.hkv + (hh - a.hq)) * a.capacity + rt.pos0 + r;
-        uint32_t w = 0;
+    for (; hh < head1; hh += step) {
+      Raw w = next;
+      if (hh + step < head1) next = load(r, hh + step);
+      add_bias(w);
+      half4_t ol, oh;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) w |= (gl.code[x] | gh.code[x] << 4) << (8 * swap01(x));
-        reinterpret_cast<uint32_t*>(a.c.k4)[e * 16 + (tid & 15)] = w;
-        if ((tid & 15) == 0)
-          reinterpret_cast<uint2*>(a.c.ks)[e] = make_uint2(gl.scale | (uint32_t)gl.zero << 16,
-                                                           gh.scale | (uint32_t)gh.zero << 16);
+      for (int x = 0; x < 4; ++x) {
+        float ra, re;
+        rope_turn(w.lo[x], w.hi[x], tab[r][t0 + x], ra, re);
+        ol[x] = (half_t)ra;
+        oh[x] = (half_t)re;
       }
-    } else if (ok) {
-      uint16_t* dst =
-          a.c.k + (((int64_t)rt.s * a.hkv + (hh - a.hq)) * a.capacity + rt.pos0 + r) * kHd + t0;
-      *reinterpret_cast<half4_t*>(dst) = ol;
-      *reinterpret_cast<half4_t*>(dst + 64) = oh;
+      if (hh < a.hq) {
+        const half_t nan = __builtin_bit_cast(half_t, kNanF16);
+        if (!ok) ol = oh = half4_t{nan, nan, nan, nan};
+        uint16_t* dst = a.q_out + ((int64_t)(rt.row0 + r) * a.hq + hh) * kHd + t0;
+        *reinterpret_cast<half4_t*>(dst) = ol;
+        *reinterpret_cast<half4_t*>(dst + 64) = oh;
+      } else if (Q4) {
+        const half_t wl[4] = {ol[0], ol[1], ol[2], ol[3]}, wh[4] = {oh[0], oh[1], oh[2], oh[3]};
+        const Q4Group gl = quantize_group(wl), gh = quantize_group(wh);
+        if (ok) {
+          const int64_t e = ((int64_t)rt.s * a.hkv + (hh - a.hq)) * a.capacity + rt.pos0 + r;
+          uint32_t c = 0;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) c |= (gl.code[x] | gh.code[x] << 4) << (8 * swap01(x));
+          reinterpret_cast<uint32_t*>(a.c.k4)[e * 16 + (tid & 15)] = c;
+          if ((tid & 15) == 0)
+            reinterpret_cast<uint2*>(a.c.ks)[e] = make_uint2(gl.scale | (uint32_t)gl.zero << 16,
+                                                             gh.scale | (uint32_t)gh.zero << 16);
+        }
+      } else if (ok) {
+        uint16_t* dst = a.c.k + (((int64_t)rt.s * a.hkv + (hh - a.hq)) * a.capacity + rt.pos0 + r) * kHd + t0;
+        *reinterpret_cast<half4_t*>(dst) = ol;
+        *reinterpret_cast<half4_t*>(dst + 64) = oh;
+      }
     }
   }
-  // values: each head's rows meet in LDS, position-minor, and leave as runs of positions
+  // values: a group a row; each head's rows meet in LDS and leave as runs of positions
+  const int64_t base = rt.pos0 - rt.shift;  // a multiple of 16
+  auto inside = [&](int c) { return c >= rt.shift && c < rt.shift + rt.nr && valid(c - rt.shift); };
+  const bool mine = unit < rt.nr;
+  const int c = rt.shift + unit;  // the row's place among the 16 positions
+  if (mine && share < a.hkv) next = load(unit, turned + share);
   for (int g = share; g < a.hkv; g += shares) {
     const int64_t sg = (int64_t)rt.s * a.hkv + g;
-    __syncthreads();
-    for (int r = unit; r < rt.nr; r += 16) {
-      float4_t lo, hi;
-      load(r, turned + g, lo, hi);
+    if (g != share) __syncthreads();
+    if (mine) {
+      Raw w = next;
+      add_bias(w);
       half_t wl[4], wh[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        wl[x] = (half_t)lo[x];
-        wh[x] = (half_t)hi[x];
+        wl[x] = (half_t)w.lo[x];
+        wh[x] = (half_t)w.hi[x];
       }
-      const int c = rt.shift + r;  // the row's place among the 16 positions
       if constexpr (Q4) {
         const Q4Group gl = quantize_group(wl), gh = quantize_group(wh);
+        uint32_t b = 0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) vc4[t0 + x][swap01(c)] = (uint8_t)(gl.code[x] | gh.code[x] << 4);
+        for (int x = 0; x < 4; ++x) b |= (gl.code[x] | gh.code[x] << 4) << (8 * x);
+        *reinterpret_cast<uint32_t*>(&vc4[c][t0]) = b;
         if ((tid & 15) == 0) {
           vs4[0][c] = gl.scale;
           vs4[1][c] = gl.zero;
@@ -209,42 +234,46 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
           vs4[3][c] = gh.zero;
         }
       } else {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          vt[t0 + x][c] = __builtin_bit_cast(uint16_t, wl[x]);
-          vt[t0 + 64 + x][c] = __builtin_bit_cast(uint16_t, wh[x]);
-        }
+        *reinterpret_cast<half4_t*>(&vt[c][t0]) = half4_t{wl[0], wl[1], wl[2], wl[3]};
+        *reinterpret_cast<half4_t*>(&vt[c][t0 + 64]) = half4_t{wh[0], wh[1], wh[2], wh[3]};
       }
     }
+    if (mine && g + shares < a.hkv) next = load(unit, turned + g + shares);
     __syncthreads();
-    const int64_t base = rt.pos0 - rt.shift;  // a multiple of 16
-    const bool whole = rt.nr == kTileRows && base >= 0 && base + kTileRows <= a.len_bound;
-    auto inside = [&](int c) { return c >= rt.shift && c < rt.shift + rt.nr && valid(c - rt.shift); };
     if constexpr (Q4) {
-      uint8_t* blk = a.c.v4 + sg * a.capacity * 64 + (base >> 6) * 4096 + (base & 63);
-      uint16_t* sc = a.c.vs + sg * a.capacity * 4 + (base >> 6) * 256 + (base & 63);
-      if (whole) {
-        if (tid < 64) *reinterpret_cast<u32x4*>(blk + tid * 64) = *reinterpret_cast<const u32x4*>(vc4[tid]);
+      // thread: byte row j, four positions, whose bytes lie exchanged
+      const int j = tid & 63, p = 4 * (tid >> 6);
+      uint8_t* dst = a.c.v4 + sg * a.capacity * 64 + (base >> 6) * 4096 + j * 64 + (base & 63) + p;
+      if (inside(p) && inside(p + 1) && inside(p + 2) && inside(p + 3)) {
+        *reinterpret_cast<uint32_t*>(dst) =
+            vc4[p][j] | vc4[p + 2][j] << 8 | vc4[p + 1][j] << 16 | (uint32_t)vc4[p + 3][j] << 24;
       } else {
-        for (int i = tid; i < 64 * kTileRows; i += 256) {
-          const int j = i >> 4, c = i & 15;
-          if (inside(c)) blk[j * 64 + swap01(c)] = vc4[j][swap01(c)];
-        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (inside(p + i)) dst[swap01(i)] = vc4[p + i][j];
       }
-      if (tid >= 64 && tid < 128) {
-        const int c = tid & 15, p = (tid >> 4) & 3;
-        if (inside(c)) sc[p * 64 + c] = vs4[p][c];
-      }
+      if (tid < 64 && inside(tid & 15))
+        a.c.vs[sg * a.capacity * 4 + (base >> 6) * 256 + (base & 63) + (tid >> 4) * 64 + (tid & 15)] =
+            vs4[tid >> 4][tid & 15];
     } else {
-      uint16_t* vo = a.c.v + sg * kHd * a.capacity + base;
-      if (whole) {
-        const int d = tid >> 1, h = tid & 1;
-        *reinterpret_cast<u32x4*>(vo + (int64_t)d * a.capacity + 8 * h) = *reinterpret_cast<const u32x4*>(&vt[d][8 * h]);
+      // thread: dimension d, eight positions
+      const int d = tid & 127, p = 8 * (tid >> 7);
+      uint16_t* dst = a.c.v + (sg * kHd + d) * a.capacity + base + p;
+      uint16_t e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = vt[p + i][d];
+      bool all = true;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) all &= inside(p + i);
+      if (all) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+        *reinterpret_cast<u32x4*>(dst) = w;
       } else {
-        for (int i = tid; i < kHd * kTileRows; i += 256) {
-          const int d = i >> 4, c = i & 15;
-          if (inside(c)) vo[(int64_t)d * a.capacity + c] = vt[d][c];
-        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (inside(p + i)) dst[i] = e[i];
       }
     }
   }
