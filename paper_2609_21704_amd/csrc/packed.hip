@@ -49,6 +49,13 @@ __device__ __forceinline__ bool row_tile(const PackedRows& pr, const int32_t* po
   return true;
 }
 
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own.  Four tiles in a row hold the values of the same
+// 128-byte lines (64 positions of a dimension): of every 32 workgroups, each XCD gets four tiles in a row.
+__device__ __forceinline__ int tile_of_block() {
+  const int b = blockIdx.x;
+  return b < (gridDim.x & ~31) ? (b & ~31) + (b & 7) * 4 + (b >> 3 & 3) : b;
+}
+
 template <int Ctrl>
 __device__ __forceinline__ half2_t dpp_min2(half2_t v) {
   const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), Ctrl, 0xF, 0xF, false);
@@ -125,7 +132,7 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
     }
   }
   RowTile rt;
-  if (!row_tile(pr, a.pos_base, a.pos_offset, blockIdx.x, rt)) return;  // uniform
+  if (!row_tile(pr, a.pos_base, a.pos_offset, tile_of_block(), rt)) return;  // uniform
   const int nh = a.hq + 2 * a.hkv, turned = a.hq + a.hkv, share = blockIdx.y, shares = gridDim.y;
   const int per = (turned + shares - 1) / shares, head0 = share * per;
   const int head1 = head0 + per < turned ? head0 + per : turned;
@@ -287,7 +294,7 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedRows pr, const i
   __shared__ __align__(16) uint8_t vb[64][kTileRows];
   const int tid = threadIdx.x, t = tid & 15, unit = tid >> 4;
   RowTile rt;
-  if (!row_tile(pr, pos_base, pos_offset, blockIdx.x, rt)) return;  // uniform
+  if (!row_tile(pr, pos_base, pos_offset, tile_of_block(), rt)) return;  // uniform
   const int64_t base = rt.pos0 - rt.shift;
   const CodeConsts kc;
   for (int g = blockIdx.y; g < hkv; g += gridDim.y) {
