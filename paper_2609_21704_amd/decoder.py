@@ -108,6 +108,28 @@ class KVCache:
         self.k = [self.k_all[l] for l in range(layers)]
         self.v = [self.v_all[l] for l in range(layers)]
 
+    def layer(self, l: int):
+        return self.k[l], self.v[l]
+
+
+class KVCacheQ4:
+    """4-bit keys and values (include/specquant_packed.h), one allocation per array with the layers first: 144 bytes per
+    layer, row, kv head and position instead of 512.  layer(l) are the four views that the packed calls take."""
+
+    def __init__(self, cfg: Config, layers: int, rows: int, capacity: int, device):
+        if capacity % 64:
+            raise ValueError("the cache capacity must be a multiple of 64")
+        self.capacity = capacity
+        heads, blocks = (layers, rows, cfg.kv_heads), capacity // 64
+        u8, f16 = torch.uint8, torch.float16
+        self.k_codes = torch.zeros((*heads, capacity, HEAD_DIM // 2), dtype=u8, device=device)
+        self.k_scales = torch.zeros((*heads, capacity, 4), dtype=f16, device=device)
+        self.v_codes = torch.zeros((*heads, blocks, HEAD_DIM // 2, 64), dtype=u8, device=device)
+        self.v_scales = torch.zeros((*heads, blocks, 4, 64), dtype=f16, device=device)
+
+    def layer(self, l: int):
+        return self.k_codes[l], self.k_scales[l], self.v_codes[l], self.v_scales[l]
+
 
 class _Buffers:
     """Activations of a pass of up to `rows` rows."""
@@ -138,7 +160,13 @@ class SpecDecoder:
 
     def __init__(self, weights: DecoderWeights, batch: int | None = None, k: int | None = None,
                  capacity: int = 1024, temperature: float = 1.0, history: int = 4096, keep_pq: bool = False,
-                 chains: int = 1, fuse: bool = True):
+                 chains: int = 1, fuse: bool = True, draft_cache: str = "f16"):
+        """draft_cache "q4": the draft's cache in 4 bits.  Its drafts come from the coarser entries; what the rounds emit
+        follows the parent's distribution as before (one chain per sequence: entries are not adopted)."""
+        if draft_cache not in ("f16", "q4"):
+            raise ValueError("draft_cache must be 'f16' or 'q4'")
+        if draft_cache == "q4" and chains != 1:
+            raise ValueError("a 4-bit draft cache takes one chain per sequence")
         self.w = weights
         cfg = self.cfg = weights.cfg
         dev = self.device = weights.device
@@ -153,7 +181,7 @@ class SpecDecoder:
             raise ValueError("draft step 0 runs 2 rows per chain; a pass takes at most 64 rows")
         if R * (k + 1) > 64:
             raise ValueError("the verification pass takes at most 64 rows")
-        self.dcache = KVCache(cfg, L, R, capacity, dev)
+        self.dcache = (KVCacheQ4 if draft_cache == "q4" else KVCache)(cfg, L, R, capacity, dev)
         self.pcache = KVCache(cfg, L, R, capacity, dev)
         self.capacity = capacity
         self.buf = _Buffers(cfg, 64, dev)  # the largest pass: 64 rows (verification, prefill chunks)
@@ -229,14 +257,25 @@ class SpecDecoder:
         delta = None  # a projection output not yet added into h
         for l in range(w.layers):
             self._norm_linear(draft, (l, "qkv"), h, w.in_norm[l], delta, x, qkv)
-            if logits is None and l + 1 == w.layers and not self.attn_hook:  # nothing reads the last layer's output
+            if isinstance(cache, KVCacheQ4):
+                rows = dict(max_rows=rps, pos_offset=offset, len_bound=lb)
+                sq.sq_packed_rope_kv_q4(qkv, w.qkv_bias[l], None, self.pos_base, cfg.q_heads, *cache.layer(l), theta=THETA,
+                                        q_out=q, status=self.status, **rows)
+                if logits is None and l + 1 == w.layers and not self.attn_hook:
+                    return
+                if self.attn_hook:
+                    self.attn_hook(True, rps, offset)
+                sq.sq_packed_attention_q4(q, *cache.layer(l), None, self.pos_base, out=a, **rows)
+                if self.attn_hook:
+                    self.attn_hook(False, rps, offset)
+            elif logits is None and l + 1 == w.layers and not self.attn_hook:  # nothing reads the last layer's output
                 sq.sq_rope_kv_f16(qkv, w.qkv_bias[l], self.pos_base, offset, rps, cfg.q_heads, cache.k[l],
                                   cache.v[l], len_bound=lb, theta=THETA, q_out=q, status=self.status)
                 return
-            if not (self.fuse and self.attn_hook is None and
-                    sq.sq_rope_attention_f16(qkv, w.qkv_bias[l], self.pos_base, offset, rps, cfg.q_heads,
-                                             cache.k[l], cache.v[l], a, len_bound=lb, theta=THETA,
-                                             status=self.status)):
+            elif not (self.fuse and self.attn_hook is None and
+                      sq.sq_rope_attention_f16(qkv, w.qkv_bias[l], self.pos_base, offset, rps, cfg.q_heads,
+                                               cache.k[l], cache.v[l], a, len_bound=lb, theta=THETA,
+                                               status=self.status)):
                 sq.sq_rope_kv_f16(qkv, w.qkv_bias[l], self.pos_base, offset, rps, cfg.q_heads, cache.k[l],
                                   cache.v[l], len_bound=lb, theta=THETA, q_out=q, status=self.status)
                 if self.attn_hook:
@@ -256,32 +295,45 @@ class SpecDecoder:
         xf = b.xf[:M // group]
         self._norm_linear(draft, (cfg.layers, "lm_head"), h, w.final_norm, delta, xf, logits, group=group)
 
-    def _prefill_pass(self, draft: bool, tokens, n: int, offset: int):
+    def _prefill_pass(self, draft: bool, tokens, n: int, offset: int, packed=None):
         """One pass of tokens [R * n] (sequence-major) at positions offset + j that only fills the model's cache: no
         logits, and of the last layer no more than its keys and values.  Any number of rows; False (nothing done)
-        where a projection's row length has no kernel for them."""
+        where a projection's row length has no kernel for them.
+
+        packed = (row_start, len_bound): tokens [row_start[R]] packed, at most n of a sequence, from pos_base on."""
         cfg, w = self.cfg, self.w
         if not w.stack.prefill_takes(draft, w.layers):
             return False
-        M, H, dev = self.R * n, cfg.hidden, self.device
+        M, H, dev = tokens.numel(), cfg.hidden, self.device
         cache = self.dcache if draft else self.pcache
-        lb = offset + n
+        row_start, lb = (None, offset + n) if packed is None else packed
+        q4 = isinstance(cache, KVCacheQ4)
         f16, f32 = torch.float16, torch.float32
         h, x = torch.empty((M, H), dtype=f32, device=dev), torch.empty((M, H), dtype=f16, device=dev)
         qkv = torch.empty((M, cfg.q_dim + 2 * cfg.kv_dim), dtype=f32, device=dev)
         q = torch.empty((M, cfg.q_heads, HEAD_DIM), dtype=f16, device=dev)
         a, t = torch.empty_like(q), torch.empty((M, cfg.intermediate), dtype=f16, device=dev)
+        rows = dict(max_rows=n, pos_offset=offset, len_bound=lb)
         sq.sq_embed_block_f16(w.embed, tokens, h=h, status=self.status)
         for l in range(w.layers):
             sq.sq_add_rmsnorm_f16(h, w.in_norm[l], EPS, x=x)
             w.stack.prefill_linear(draft, (l, "qkv"), x, qkv)
-            sq.sq_prefill_rope_kv_f16(qkv, w.qkv_bias[l], self.pos_base, offset, n, cfg.q_heads, cache.k[l],
-                                      cache.v[l], len_bound=lb, theta=THETA, q_out=q, status=self.status)
+            if packed is None and not q4:
+                sq.sq_prefill_rope_kv_f16(qkv, w.qkv_bias[l], self.pos_base, offset, n, cfg.q_heads, cache.k[l],
+                                          cache.v[l], len_bound=lb, theta=THETA, q_out=q, status=self.status)
+            else:
+                (sq.sq_packed_rope_kv_q4 if q4 else sq.sq_packed_rope_kv_f16)(
+                    qkv, w.qkv_bias[l], row_start, self.pos_base, cfg.q_heads, *cache.layer(l), theta=THETA, q_out=q,
+                    status=self.status, **rows)
             if l + 1 == w.layers and not self.attn_hook:
                 break
             if self.attn_hook:
                 self.attn_hook(True, n, offset)
-            sq.sq_prefill_attention_f16(q, cache.k[l], cache.v[l], self.pos_base, offset, n, len_bound=lb, out=a)
+            if packed is None and not q4:
+                sq.sq_prefill_attention_f16(q, cache.k[l], cache.v[l], self.pos_base, offset, n, len_bound=lb, out=a)
+            else:
+                (sq.sq_packed_attention_q4 if q4 else sq.sq_packed_attention_f16)(
+                    q, *cache.layer(l), row_start, self.pos_base, out=a, **rows)
             if self.attn_hook:
                 self.attn_hook(False, n, offset)
             w.stack.prefill_linear(draft, (l, "o"), a.view(M, cfg.q_dim), h, sq.PREFILL_ADD)
@@ -289,6 +341,38 @@ class SpecDecoder:
             w.stack.prefill_linear(draft, (l, "gate_up"), x, t, sq.PREFILL_SILU)
             w.stack.prefill_linear(draft, (l, "down"), t, h, sq.PREFILL_ADD)
         return True
+
+    def prefill_packed(self, prompts, models=(True, False)):
+        """prefill() of prompts given as one list of token ids per sequence (2 .. capacity of them), their tokens packed
+        one after the other: no padding is computed, and prompts longer than a pass (PREFILL_ROWS rows over all
+        sequences) continue in the next."""
+        if len(prompts) != self.B or any(not 2 <= len(p) <= self.capacity for p in prompts):
+            raise ValueError("one prompt of 2 .. capacity tokens per sequence")
+        if not all(self.w.stack.prefill_takes(draft, self.w.layers) for draft in models):
+            raise ValueError("a projection of this model has no kernel for packed prompts: use prefill()")
+        prompts = [list(p) for p in prompts for _ in range(self.c)]
+        i32 = torch.int32
+        for draft in models:
+            done = [0] * self.R
+            while True:
+                left, take = PREFILL_ROWS, []
+                for p, d in zip(prompts, done):
+                    take.append(min(left, len(p) - 1 - d))
+                    left -= take[-1]
+                if sum(take) == 0:
+                    break
+                toks = [t for p, d, n in zip(prompts, done, take) for t in p[d:d + n]]
+                start = [0]
+                for n in take:
+                    start.append(start[-1] + n)
+                self.pos_base.copy_(torch.tensor(done, dtype=i32))
+                done = [d + n for d, n in zip(done, take)]
+                self._prefill_pass(draft, torch.tensor(toks, dtype=i32, device=self.device), max(take), 0,
+                                   packed=(torch.tensor(start, dtype=i32, device=self.device), max(done)))
+        self.pos_base.copy_(torch.tensor([len(p) - 1 for p in prompts], dtype=i32))
+        self.pending.copy_(torch.tensor([p[-1] for p in prompts], dtype=i32))
+        self.prev.copy_(torch.tensor([p[-2] for p in prompts], dtype=i32))
+        self.out_len.zero_()
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(True, False), lengths=None):
         """Feed prompt [B][Lp] (int32) but its last token to both models
@@ -441,6 +525,9 @@ class DirectDecoder(SpecDecoder):
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(False,), lengths=None):
         super().prefill(prompt, chunk, models=models, lengths=lengths)
+
+    def prefill_packed(self, prompts, models=(False,)):
+        super().prefill_packed(prompts, models=models)
 
     def set_uniforms(self, u: torch.Tensor, _unused=None):
         self.u.copy_(u.view(self.B, 1))

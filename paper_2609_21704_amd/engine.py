@@ -49,13 +49,14 @@ def weight_bytes(cfg: Config, layers: int | None = None) -> dict:
     }
 
 
-def cache_bytes(cfg: Config, layers: int, rows: int, capacity: int) -> int:
-    """Keys and values of one model's cache: fp16, per layer, row, kv head and position."""
-    return 2 * layers * rows * cfg.kv_heads * capacity * HEAD_DIM * 2
+def cache_bytes(cfg: Config, layers: int, rows: int, capacity: int, fmt: str = "f16") -> int:
+    """Keys and values of one model's cache, per layer, row, kv head and position: fp16, or ("q4") 4-bit codes with a
+    scale and a zero per 64."""
+    return 2 * layers * rows * cfg.kv_heads * capacity * (HEAD_DIM * 2 if fmt == "f16" else HEAD_DIM // 2 + 8)
 
 
 def placement(cfg: Config, free_bytes: int, batch: int, capacity: int, k: int, layers: int | None = None,
-              margin: float = 0.1) -> dict:
+              margin: float = 0.1, draft_cache: str = "f16") -> dict:
     """Which variants are resident, given the device's free HBM: the parent
     and its direct-decoding cache first (required), then the INT4 draft with
     the caches of its decoder, then the FP8 draft with its own.  `margin` of
@@ -68,7 +69,8 @@ def placement(cfg: Config, free_bytes: int, batch: int, capacity: int, k: int, l
     if direct > budget:
         raise MemoryError(f"the FP16 parent and its cache need {direct} bytes; {budget} are available")
     used, resident = direct, ["f16"]
-    spec_cache = 2 * cache_bytes(cfg, L, batch, capacity)  # draft and parent caches of one SpecDecoder
+    # parent and draft caches of one SpecDecoder
+    spec_cache = cache_bytes(cfg, L, batch, capacity) + cache_bytes(cfg, L, batch, capacity, draft_cache)
     for v in ("int4", "fp8"):
         if used + w[v] + spec_cache <= budget:
             used += w[v] + spec_cache
@@ -98,9 +100,12 @@ class Engine:
     def __init__(self, cfg: Config, device, layers: int | None = None, k: int | None = None, batch: int = 4,
                  capacity: int = 1024, temperature: float = 0.0, router: Router | None = None,
                  chains: int = 1, free_bytes: int | None = None, seed: int | None = None,
-                 parent: DecoderWeights | None = None, timed: bool = False):
-        """`parent`: existing FP16 parent weights (with one draft copy) to serve
-        from instead of building new ones.  `timed`: synchronise around each
+                 parent: DecoderWeights | None = None, timed: bool = False, draft_cache: str = "f16",
+                 packed: bool = False):
+        """`draft_cache`: "q4" keeps the drafts' caches in 4 bits.  `packed`: the
+        prompts of a batch go through the models packed, without padding and
+        without copies of a prompt for idle rows.  `parent`: existing FP16 parent
+        weights (with one draft copy) to serve from instead of building new ones.  `timed`: synchronise around each
         batch's prefill and rounds and add their wall time to `seconds`."""
         self.cfg = cfg
         self.device = torch.device(device)
@@ -111,7 +116,10 @@ class Engine:
         L = cfg.layers if layers is None else layers
         if free_bytes is None:
             free_bytes = torch.cuda.mem_get_info(self.device)[0]
-        self.plan = placement(cfg, free_bytes, batch * chains, capacity, self.k, L)
+        if draft_cache == "q4" and chains != 1:
+            raise ValueError("a 4-bit draft cache takes one chain per sequence")
+        self.draft_cache, self.packed = draft_cache, packed
+        self.plan = placement(cfg, free_bytes, batch * chains, capacity, self.k, L, draft_cache=draft_cache)
         resident = self.plan["resident"]
         if parent is None:
             first = "int4" if "int4" in resident else ("fp8" if "fp8" in resident else "none")
@@ -139,7 +147,7 @@ class Engine:
             else:
                 self.decoders[variant] = SpecDecoder(w, batch=self.batch, k=self.k, capacity=self.capacity,
                                                      temperature=self.T, chains=self.chains,
-                                                     history=self.capacity)
+                                                     history=self.capacity, draft_cache=self.draft_cache)
         return self.decoders[variant]
 
     def tokenize(self, prompt) -> list:
@@ -188,13 +196,17 @@ class Engine:
     def _run_batch(self, variant: str, toks: list, max_new: int) -> list:
         dec = self.decoder(variant)
         n = len(toks)
-        rows = toks + [toks[0]] * (self.batch - n)  # idle rows repeat the first prompt
-        Lp = max(len(t) for t in rows)
-        prompt = torch.zeros((self.batch, Lp), dtype=torch.int32)
-        for i, t in enumerate(rows):
-            prompt[i, :len(t)] = torch.tensor(t, dtype=torch.int32)
-        t0 = self._clock()
-        dec.prefill(prompt, lengths=[len(t) for t in rows])
+        if self.packed:
+            t0 = self._clock()
+            dec.prefill_packed(toks + [toks[0][:2]] * (self.batch - n))  # idle rows: two tokens of the first prompt
+        else:
+            rows = toks + [toks[0]] * (self.batch - n)  # idle rows repeat the first prompt
+            Lp = max(len(t) for t in rows)
+            prompt = torch.zeros((self.batch, Lp), dtype=torch.int32)
+            for i, t in enumerate(rows):
+                prompt[i, :len(t)] = torch.tensor(t, dtype=torch.int32)
+            t0 = self._clock()
+            dec.prefill(prompt, lengths=[len(t) for t in rows])
         t1 = self._clock()
         per_round = 1 if variant == "f16" else self.k + 1
         r = 0
