@@ -124,7 +124,9 @@ struct Planner {
 #pragma unroll
     for (int i = 3; i >= 0; --i) {
       const int c = lo + (hi - lo) / grain * i / 4 * grain;
-      if (wave_total((float)(mine.tiles * parts(mine, c))) <= (float)most) span = c;
+      // parts or one more: the quotient in fp32, 2^-20 larger (a tile without keys is a part too)
+      const float n = (float)(mine.steps + c - 1) * __builtin_amdgcn_rcpf((float)c) * (1.f + 0x1p-20f);
+      if (wave_total((float)mine.tiles * fmaxf(floorf(n), 1.f)) <= (float)most) span = c;
     }
     span = __builtin_amdgcn_readfirstlane(span);
   }
@@ -719,12 +721,14 @@ __device__ __forceinline__ void barrier_after_loads() {
   asm volatile("" ::: "memory");
 }
 
-constexpr int ring(bool q4, int nw) { return q4 || nw < 8 ? 2 : 3; }
+// Buffers of 32 KB: two where two workgroups share a CU; where keys are split, one has it for itself, and its keys
+// come from memory rather than from L2.
+constexpr int ring(bool q4, int nw, bool split) { return q4 ? 2 : (split ? 4 : (nw < 8 ? 2 : 3)); }
 
 template <bool Q4, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
                                                                                                       AttnArgs a) {
-  constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW);
+  constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW, SPLIT);
   constexpr int kLoads = 16 / NW;                 // fp16: loads of 1 KB of keys (and of values) per wavefront and step
   constexpr int kCodes = NW >= 8 ? 1 : 512 / NT;  // 4-bit: 16-byte cells of codes per thread
   __shared__ __align__(16) u32x4 kb[kRing][1024], vb[kRing][1024];
@@ -1085,7 +1089,7 @@ __device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr
   *reinterpret_cast<half2_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + 2 * lane) = r;
 }
 
-// Four queries of a tile a workgroup, one a wavefront (four a wavefront, 16 a workgroup: 11.7 us for 8.4).
+// Four queries of a tile a workgroup, one a wavefront (sixteen, in wavefronts or in turn: 7.1 and 11.2 us for 5.0).
 __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain, bool few) {
   const int wave = threadIdx.x >> 6;
   const int G = a.hq / a.hkv;
