@@ -721,14 +721,15 @@ __device__ __forceinline__ void barrier_after_loads() {
   asm volatile("" ::: "memory");
 }
 
-// Buffers of 32 KB: two where two workgroups share a CU; where keys are split, one has it for itself, and its keys
-// come from memory rather than from L2.
-constexpr int ring(bool q4, int nw, bool split) { return q4 ? 2 : (split ? 4 : (nw < 8 ? 2 : 3)); }
+// Buffers of 32 KB: two for workgroups of four wavefronts, two of which share a CU, three for those of eight.  Where
+// keys are split and a workgroup has its CU for itself, more do not help: 20.8 us with two, 22.5 with three and 24.2 with
+// four (three sequences of 17 to 60 rows after 3000 to 9000 cached positions, 28 query heads on 4).
+constexpr int ring(bool q4, int nw) { return q4 || nw < 8 ? 2 : 3; }
 
 template <bool Q4, int NW, bool SPLIT>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
                                                                                                       AttnArgs a) {
-  constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW, SPLIT);
+  constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW);
   constexpr int kLoads = 16 / NW;                 // fp16: loads of 1 KB of keys (and of values) per wavefront and step
   constexpr int kCodes = NW >= 8 ? 1 : 512 / NT;  // 4-bit: 16-byte cells of codes per thread
   __shared__ __align__(16) u32x4 kb[kRing][1024], vb[kRing][1024];
