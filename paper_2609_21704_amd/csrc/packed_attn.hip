@@ -27,6 +27,7 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 constexpr int kTile = 64;  // keys per step
 constexpr float kScale = 1.4426950408889634f * 0.08838834764831845f;  // log2(e) / sqrt(128)
 constexpr float kShift = 7.f, kSlack = 8.f;
+constexpr int kMaxParts = 1024;  // of one kv head's keys, all sequences
 constexpr float kNoMax = -1e30f;  // a finite start: exp2(kNoMax - m) = 0 and exp2(-inf - kNoMax) = 0
 
 struct AttnArgs {
@@ -1041,12 +1042,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
-// The parts of query qi joined, in their order: lane i the weight of part i (at most 512 parts: eight a lane), then every
+// The parts of query qi joined, in their order: lane i the weights of parts i, 64 + i, .. (at most kMost a lane), then every
 // lane two dimensions, eight parts' sums in flight.  row0: the query's row of part 0's sums.
+template <int kMost>
 __device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr, int64_t p0, int qi, int parts,
                                      int64_t row0, int64_t stride) {
   const int lane = threadIdx.x & 63;
-  constexpr int kMost = 8;
   float2 ml[kMost];
   float M = kNoMax, L = 0.f;
 #pragma unroll
@@ -1109,8 +1110,12 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
   const int64_t stride = (int64_t)a.hkv * TQ;  // rows of the sums from one part to the next
   const int qx = blockIdx.y * 4 + wave;
-  if (qt * TQ + qx < nq)
-    join(a, G, g, sr, p0, qt * TQ + qx, parts, ((int64_t)first * a.hkv + g) * TQ + qx, stride);
+  if (qt * TQ + qx >= nq) return;
+  const int64_t row0 = ((int64_t)first * a.hkv + g) * TQ + qx;
+  if (parts <= kWave)
+    join<1>(a, G, g, sr, p0, qt * TQ + qx, parts, row0, stride);
+  else
+    join<kMaxParts / kWave>(a, G, g, sr, p0, qt * TQ + qx, parts, row0, stride);
 }
 
 struct Plan {
@@ -1132,7 +1137,7 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
     p.grain = p.tq > 32 ? kFewWaves / 2 : kFewWaves;
     p.tiles = pr.b;
     most = 256 / hkv;
-    if (2 * b > most) most = 1024 / hkv;
+    if (2 * b > most) most = kMaxParts / hkv;
     if (2 * b > most || steps <= 2 * p.grain) most = 0;
   } else {
     auto tiles = [&](int64_t tq) {

@@ -401,6 +401,23 @@ def test_long_cache_offsets_q4():
     assert same(ko, k[0, :, -rows:].transpose(0, 1))
 
 
+def test_many_parts_of_one_sequence():
+    """One long sequence beside 129 short ones on one kv head: its keys in more than 512 parts."""
+    b, hq, cap = 130, 64, 140032
+    past = [10 + i % 3 for i in range(b - 1)] + [cap - 1]
+    c = (torch.randint(0, 256, (b, 1, cap, 64), dtype=torch.uint8, device=DEV), torch.zeros((b, 1, cap, 4), dtype=F16, device=DEV),
+         torch.randint(0, 256, (b, 1, cap // 64, 64, 64), dtype=torch.uint8, device=DEV),
+         torch.zeros((b, 1, cap // 64, 4, 64), dtype=F16, device=DEV))
+    c[1].view(-1, 2)[:] = torch.tensor([0.0625, 7.0], device=DEV)
+    c[3].view(-1, 2, 64)[:] = torch.tensor([0.125, 8.0], device=DEV)[:, None]
+    c[3][..., ::2, :] += normal(c[3][..., ::2, :].shape, 62).abs() * 0.0625
+    q = normal((b, hq, 128), 61)
+    out = sq.sq_packed_attention_q4(q, *c, None, ints(past))
+    k, v = (torch.cat(x) for x in zip(*[values_q4([t[i:i + 1] for t in c]) for i in (0, b - 2, b - 1)]))
+    pick = [0, b - 2, b - 1]
+    check_attention(out[pick], q[pick], k, v, [(1, past[i]) for i in pick])
+
+
 @pytest.mark.parametrize("fmt", ["f16", "q4"])
 def test_pass_captured(fmt):
     """A prompt, then single tokens, as a decoder makes them: the tokens' calls recorded in a graph that moves the positions
