@@ -118,7 +118,8 @@ struct Planner {
     S *= 1.f + 0x1p-16f;
     auto up = [&](float x) { return ((int)x / grain + 1) * grain; };
     const float room = (float)most - N;
-    const int hi = up(S / (room < 1.f ? 1.f : room));
+    if (room < 1.f) return;  // only where row_start lets sequences share rows
+    const int hi = up(S / room);
     span = hi;
     if (b > kWave) return;
     const int lo = up(S / (float)most - 1.f);
@@ -1110,7 +1111,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
   const int64_t stride = (int64_t)a.hkv * TQ;  // rows of the sums from one part to the next
   const int qx = blockIdx.y * 4 + wave;
-  if (qt * TQ + qx >= nq) return;
+  if (qt * TQ + qx >= nq || first + parts > a.most) return;  // (the latter as in the plan)
   const int64_t row0 = ((int64_t)first * a.hkv + g) * TQ + qx;
   if (parts <= kWave)
     join<1>(a, G, g, sr, p0, qt * TQ + qx, parts, row0, stride);

@@ -203,6 +203,22 @@ def test_bad_positions_and_rows():
             attn(q.nan_to_num(), *cache, ints(wrong), ints([3, 20]), max_rows=most)
 
 
+@pytest.mark.parametrize("most", [4, 90])
+def test_sequences_that_share_rows(most):
+    """row_start that decreases gives more tiles than the rows have: the workspace of the split keys bounds what is read,
+    and the rows behind the call's are left."""
+    b, hq, hkv, cap, rows = 300, 4, 2, 2048, most
+    k, v = normal((1, hkv, cap, 128), 51).repeat(b, 1, 1, 1), normal((1, hkv, 128, cap), 52).repeat(b, 1, 1, 1)
+    q, out = normal((rows + 8, hq, 128), 53), torch.full((rows + 8, hq, 128), 9.0, dtype=F16, device=DEV)
+    start = ints([rows * (i % 2) for i in range(b + 1)])
+    sq.sq_packed_attention_f16(q[:rows], k, v, start, ints([cap - rows] * b), max_rows=most, out=out[:rows])
+    torch.cuda.synchronize()
+    assert bool((out[rows:] == 9).all())
+    good = starts([rows] + [0] * (b - 1))
+    sq.sq_packed_attention_f16(q[:rows], k, v, good, ints([cap - rows] * b), max_rows=most, out=out[:rows])
+    check_attention(out, q, k[:1], v[:1].transpose(2, 3), [(rows, cap - rows)])
+
+
 def attention_case(seqs, hq, hkv, cap, seed, std=1.3):
     b, rows = len(seqs), sum(n for n, _ in seqs)
     q = normal((rows, hq, 128), seed, rows, std=std)
