@@ -17,6 +17,8 @@ struct Call {
 };
 
 constexpr int64_t kMaxRows = int64_t(1) << 20;
+// The prompt kernel's lanes reach seven rows of values past a scalar base with 32-bit byte offsets.
+constexpr int64_t kMaxAttnCapacity = int64_t(1) << 28;
 
 sq_status check_sizes(const Call& c) {
   if (c.max_rows < 1 || c.max_rows > kMaxRows || c.rows < 0 || c.rows > kMaxRows) return SQ_ERR_SHAPE;
@@ -76,6 +78,7 @@ sq_status attention(const Call& c, const sq::KvCache& kv, bool q4, const uint16_
                     uint16_t* out, hipStream_t stream) {
   sq_status st = check_sizes(c);
   if (st != SQ_OK) return st;
+  if (!q4 && c.capacity > kMaxAttnCapacity) return SQ_ERR_SHAPE;
   if (c.rows == 0) return SQ_OK;
   if (!q || !out) return SQ_ERR_NULL;
   st = check_arrays(c, kv, q4);

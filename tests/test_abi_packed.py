@@ -41,6 +41,12 @@ def test_sizes(call, bad):
     assert call(**bad) == SHAPE
 
 
+def test_capacity():
+    big = (1 << 28) + 64
+    assert attn_f16(cap=big) == SHAPE and attn_f16(cap=big, rows=0) == SHAPE and rope_f16(cap=big, rows=0) == OK
+    assert attn_f16(cap=1 << 28, rows=0) == OK
+
+
 def test_pointers():
     assert rope_f16(qkv=None) == NULL and rope_f16(pos=None) == NULL and rope_f16(k=None) == NULL
     assert rope_f16(q=None) == NULL and rope_f16(theta=float("inf")) == NONFINITE and rope_f16(theta=1.0) == SHAPE
