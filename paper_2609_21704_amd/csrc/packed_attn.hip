@@ -726,23 +726,25 @@ __device__ __forceinline__ void barrier_after_loads() {
 // Buffers of 32 KB: two for workgroups of four wavefronts, two of which share a CU, three for those of eight.  Where
 // keys are split and a workgroup has its CU for itself, more do not help: 20.8 us with two, 22.5 with three and 24.2 with
 // four (three sequences of 17 to 60 rows after 3000 to 9000 cached positions, 28 query heads on 4).
+constexpr int kSplitGroups = 2;
+
 constexpr int ring(bool q4, int nw) { return q4 || nw < 8 ? 2 : 3; }
 
-template <bool Q4, int NW, bool SPLIT>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
+template <bool Q4, int NW, int KW, bool SPLIT>
+__global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
                                                                                                       AttnArgs a) {
   constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW);
   constexpr int kLoads = 16 / NW;                 // fp16: loads of 1 KB of keys (and of values) per wavefront and step
   constexpr int kCodes = NW >= 8 ? 1 : 512 / NT;  // 4-bit: 16-byte cells of codes per thread
-  __shared__ __align__(16) u32x4 kb[kRing][1024], vb[kRing][1024];
+  __shared__ __align__(16) u32x4 kb[KW * kRing][1024], vb[KW * kRing][1024];
   __shared__ int odd_seen;  // a value was not finite
   const int G = a.hq / a.hkv;
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
-  const int tid = threadIdx.x, lane = tid & 63, lc = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x & (NT - 1), lane = tid & 63, lc = lane & 31, h = lane >> 5;  // in its group of wavefronts
+  const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & (NW - 1), kw = wave8 / NW;
   Unit u;
   {
-    const Planner plan(pr.b, SPLIT ? a.most : 0, 1, [&](int i) { return seq_work(pr, a, G, TQ, i); });
+    const Planner plan(pr.b, SPLIT ? a.most : 0, KW, [&](int i) { return seq_work(pr, a, G, TQ, i); });
     if (!SPLIT && a.longest ? !plan.find_longest(item, G, TQ, u) : !plan.find(item, u)) return;
   }
   const SeqRows sr = u.rows;
@@ -777,7 +779,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
   // (dimension d = 8 (wave + NW i) + lane / 8: d / 2 % 8 is 4 (wave % 2) + lane / 16, NW even)
   voff = (uint32_t)(lane >> 3) * (uint32_t)(2 * a.capacity) + 16 * ((lane & 7) ^ (4 * (wave & 1) + (lane >> 4)));
-  const uint32_t kdst = lds_address(&kb[0][64 * wave]), vdst = lds_address(&vb[0][64 * wave]);
+  const uint32_t kdst = lds_address(&kb[kw * kRing][64 * wave]), vdst = lds_address(&vb[kw * kRing][64 * wave]);
   auto issue_step = [&](int st, int buf) {
     const uint16_t* kst = k16 + (int64_t)st * (kTile * kHd);
 #pragma unroll
@@ -791,14 +793,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int i = 0; i < 1024 / NT; ++i) {
       const int c = tid + NT * i, left = klast - (st * kTile + 8 * ((c & 7) ^ ((c >> 4) & 7)));
-      u32x4 w = vb[buf][c];
+      u32x4 w = vb[kw * kRing + buf][c];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const uint32_t v = w[x] & keep_mask(2 * x, left), o = odd_halves(v);
         odd |= o;
         w[x] = without(v, o);
       }
-      vb[buf][c] = w;
+      vb[kw * kRing + buf][c] = w;
     }
     if (odd) odd_seen = 1;
   };
@@ -836,8 +838,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const int sw = swap23(key & 15);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          kb[buf][key * 16 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
-          kb[buf][key * 16 + ((8 + 2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
+          kb[kw * kRing + buf][key * 16 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
+          kb[kw * kRing + buf][key * 16 + ((8 + 2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
         }
       } else {
         const int c2 = c - 256, j = c2 >> 2, part = c2 & 3;
@@ -856,24 +858,24 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const int sw = (j >> 1) & 7;  // (of j + 64 too)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          vb[buf][j * 8 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
-          vb[buf][(j + 64) * 8 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
+          vb[kw * kRing + buf][j * 8 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, lo[x]);
+          vb[kw * kRing + buf][(j + 64) * 8 + ((2 * part + x) ^ sw)] = __builtin_bit_cast(u32x4, hi[x]);
         }
       }
     }
   };
 
-  if (tid == 0) odd_seen = 0;
+  if (threadIdx.x == 0) odd_seen = 0;
   if constexpr (Q4) {
     __syncthreads();
-    if (st0 < st1) {
-      load_step(st0);
-      store_step(st0, 0);
+    if (st0 + kw < st1) {
+      load_step(st0 + kw);
+      store_step(st0 + kw, 0);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i)
-      if (st0 + i < st1) issue_step(st0 + i, i);
+      if (st0 + kw + KW * i < st1) issue_step(st0 + kw + KW * i, i);
   }
   half8_t qf[8];
   {
@@ -892,27 +894,28 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   const int krow = swap23(lc) * 16, vrow = lc * 8, vsw = (lc >> 1) & 7;
   int buf = 0;
-  for (int st = st0; st < st1; ++st) {
-    const int key0 = st * kTile;
-    const bool past = key0 + kTile - 1 > pmin;  // uniform: some row of the workgroup may not read some key
-    // step st is in its buffer, and every wavefront is done with step st - 1
+  for (int round = st0; round < st1; round += KW) {  // (the same for all wavefronts: they meet at its barriers)
+    const int st = round + kw, key0 = st * kTile;
+    // uniform: some row of the workgroup may not read some key of the round
+    const bool past = (round + KW - 1) * (int64_t)kTile + kTile - 1 > pmin;
+    // step st is in its buffer, and every wavefront is done with step st - KW
     if constexpr (Q4) {
       __syncthreads();
-      if (st + 1 < st1) load_step(st + 1);
+      if (st + KW < st1) load_step(st + KW);
     } else {
-      if (st + kRing - 2 < st1)  // the steps st + 1 .. st + kRing - 2 may stay in flight
+      if (st + KW * (kRing - 2) < st1)  // the steps st + KW .. st + KW (kRing - 2) may stay in flight
         barrier_after_loads<(kRing - 2) * 2 * kLoads>();
       else
         barrier_after_loads<0>();
-      if (st + kRing - 1 < st1) issue_step(st + kRing - 1, buf == 0 ? kRing - 1 : buf - 1);
+      if (st + KW * (kRing - 1) < st1) issue_step(st + KW * (kRing - 1), buf == 0 ? kRing - 1 : buf - 1);
       if (past) {
-        tame_step(st, buf);
+        if (st < st1 && key0 + kTile - 1 > pmin) tame_step(st, buf);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
     }
-    if (owner && key0 <= wmax) {  // uniform in the wavefront
+    if (owner && key0 <= wmax && (KW == 1 || st < st1)) {  // uniform in the wavefront
       float16_t sc[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -921,7 +924,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       // fragment i of the keys: half i % 2 of the tile, dimensions 16 (i / 2) .. +16; kDeep of them ahead of the products
       constexpr int kDeep = Q4 ? 2 : 8;
       u32x4 f[kDeep];
-      auto key_frag = [&](int i) { return kb[buf][(i & 1) * 512 + krow + ((2 * (i >> 1) + h) ^ (lc & 15))]; };
+      auto key_frag = [&](int i) { return kb[kw * kRing + buf][(i & 1) * 512 + krow + ((2 * (i >> 1) + h) ^ (lc & 15))]; };
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) f[i] = key_frag(i);
 #pragma unroll
@@ -931,7 +934,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (i + kDeep < 16) f[i % kDeep] = key_frag(i + kDeep);
       }
       // fragment i of the values: dimensions 32 (i % 4) .. +32, keys 16 (i / 4) .. +16
-      auto val_frag = [&](int i) { return vb[buf][(i & 3) * 256 + vrow + ((2 * (i >> 2) + h) ^ vsw)]; };
+      auto val_frag = [&](int i) { return vb[kw * kRing + buf][(i & 3) * 256 + vrow + ((2 * (i >> 2) + h) ^ vsw)]; };
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) f[i] = val_frag(i);
       const bool tail = key0 + kTile - 1 > wmin;  // uniform
@@ -977,14 +980,14 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
     }
     if constexpr (Q4) {
-      if (st + 1 < st1) store_step(st + 1, buf ^ 1);
+      if (st + KW < st1) store_step(st + KW, buf ^ 1);
     }
     buf = buf + 1 == kRing ? 0 : buf + 1;
   }
-  if (!owner) return;
-  if (odd_seen) {  // (written before the last step's barrier)
+  if (KW == 1 && !owner) return;
+  if (owner && odd_seen) {  // (written before the last step's barrier)
 #pragma unroll 1
-    for (int st = st0; st < st1; ++st) {
+    for (int st = st0 + kw; st < st1; st += KW) {
       if (st * (int64_t)kTile + kTile - 1 <= pmin) continue;
 #pragma unroll 1
       for (int key = st * kTile; key < st * kTile + kTile && key <= wmax && key <= klast; ++key) {
@@ -1001,6 +1004,35 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   l = pair_fold(l, [](float x, float y) { return x + y; });
+  if constexpr (KW == 2) {  // the second group's sums to the first
+    u32x4* ob = &kb[0][1024 * wave];  // (four wavefronts of 16 KB)
+    float2* ml = reinterpret_cast<float2*>(&vb[0][64 * wave]);
+    __syncthreads();  // every wavefront is done with the keys
+    if (owner && kw == 1) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          ob[64 * (4 * d + x) + lane] =
+              __builtin_bit_cast(u32x4, float4_t{o[d][4 * x], o[d][4 * x + 1], o[d][4 * x + 2], o[d][4 * x + 3]});
+      ml[lane] = make_float2(m, l);
+    }
+    __syncthreads();
+    if (!owner || kw == 1) return;
+    const float2 other = ml[lane];
+    const float mn = fmaxf(m, other.x), mine = exp2_fast(m - mn), theirs = exp2_fast(other.x - mn);
+    m = mn;
+    l = l * mine + other.y * theirs;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const u32x4 w = ob[64 * (4 * d + x) + lane];
+        const float4_t v = __builtin_bit_cast(float4_t, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][4 * x + i] = o[d][4 * x + i] * mine + v[i] * theirs;
+      }
+  }
   if constexpr (SPLIT) {
     const int64_t at = (int64_t)blockIdx.x * TQ + 32 * wave + lc;
     float* po = a.part_o + at * kHd + 4 * h;
@@ -1149,6 +1181,7 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
     p.tiles = (int)tiles(p.tq);
     most = 256 / hkv;
     if (2 * p.tiles > most || steps <= 4) most = 0;
+    if (most) p.grain = kSplitGroups;
   }
   p.most = (int)most;
   return p;
@@ -1165,12 +1198,14 @@ void launch_few(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& 
     hipLaunchKernelGGL((few_attn_kernel<Q4, 2, 2>), grid, block, 0, stream, pr, a);
 }
 
-template <bool Q4, int NW>
+template <bool Q4>
 void launch_prompt(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
-  if (p.most)
-    hipLaunchKernelGGL((prompt_attn_kernel<Q4, NW, true>), grid, dim3(64 * NW), 0, stream, pr, a);
+  if (p.tq == 256)  // (never split: so many tiles fill the chip)
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 8, 1, false>), grid, dim3(512), 0, stream, pr, a);
+  else if (p.most)
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 4, kSplitGroups, true>), grid, dim3(256 * kSplitGroups), 0, stream, pr, a);
   else
-    hipLaunchKernelGGL((prompt_attn_kernel<Q4, NW, false>), grid, dim3(64 * NW), 0, stream, pr, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 4, 1, false>), grid, dim3(256), 0, stream, pr, a);
 }
 
 }  // namespace
@@ -1197,16 +1232,11 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
       launch_few<true>(p, grid, pr, a, stream);
     else
       launch_few<false>(p, grid, pr, a, stream);
-  } else if (p.tq == 256) {
-    if (q4)
-      launch_prompt<true, 8>(p, grid, pr, a, stream);
-    else
-      launch_prompt<false, 8>(p, grid, pr, a, stream);
   } else {
     if (q4)
-      launch_prompt<true, 4>(p, grid, pr, a, stream);
+      launch_prompt<true>(p, grid, pr, a, stream);
     else
-      launch_prompt<false, 4>(p, grid, pr, a, stream);
+      launch_prompt<false>(p, grid, pr, a, stream);
   }
   if (p.most)
     hipLaunchKernelGGL(packed_merge_kernel, dim3((unsigned)(p.tiles * hkv), (unsigned)(p.tq / 4)), dim3(256), 0, stream,
