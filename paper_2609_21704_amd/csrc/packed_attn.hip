@@ -41,6 +41,7 @@ struct AttnArgs {
   float2* part_ml;  // [unit][kv head][query]
   int most;         // parts of one kv head, 0 without splitting
   bool longest;     // the tiles with the most keys first (they do not all run at once)
+  int32_t* arrived;  // few rows: parts that are done of each (sequence, kv head), null where a merge kernel follows
 };
 
 // max / sum over the two lanes that share a column of a 32 x 32 product
@@ -109,14 +110,14 @@ struct Planner {
   __device__ __forceinline__ Planner(int b, int most, int grain, F work) : b(b), span(1 << 30), lane(threadIdx.x & 63), work(work) {
     mine = lane < b ? work(lane) : SeqWork{};
     if (most == 0) return;
-    float S = 0.f, N = 0.f;  // (sums a little off in fp32; S is taken 2^-16 larger)
+    float S = 0.f, N = 0.f;  // (up to 1024 sums in fp32: S is taken 2^-13 larger)
     for (int base = 0; base < b; base += kWave) {
       const SeqWork w = at(base);
       S += wave_total((float)w.tiles * (float)w.steps);
       N += wave_total((float)w.tiles);
     }
-    S *= 1.f + 0x1p-16f;
-    auto up = [&](float x) { return ((int)x / grain + 1) * grain; };
+    S *= 1.f + 0x1p-13f;
+    auto up = [&](float x) { return ((int)fminf(x, 0x1p29f) / grain + 1) * grain; };
     const float room = (float)most - N;
     if (room < 1.f) return;  // only where row_start lets sequences share rows
     const int hi = up(S / room);
@@ -356,6 +357,17 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
   return without(w, o);
 }
 
+// Sums for another workgroup, in stores that go through to the level that all XCDs share (so that the wait for them is all
+// that has to come before the arrival is counted), and read from there.
+__device__ __forceinline__ void publish(float2* p, float2 v) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 published(const float2* p) {
+  return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT));
+}
+
 // ---------------------------------------------------------------- few rows
 // One workgroup per (part of the keys, sequence, kv head); its wavefronts take the part's steps of 64 keys in turn, each
 // for all the queries (NQT tiles of 16), and meet in LDS.  v_mfma_f32_16x16x32_f16: lane l holds row / column li = l %
@@ -371,8 +383,10 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
                                                                                                         AttnArgs a) {
   constexpr int NW = kFewWaves / HALVES;  // wavefronts that share the keys of a half's queries
   constexpr bool kAhead = Q4 || NQT == 1;
+  constexpr bool kJoins = NQT == 1;  // (up to 16 queries: the last workgroup may join the parts)
   __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
   __shared__ float2 ml[kFewWaves][16 * NQT];
+  __shared__ bool last;
   __shared__ __align__(16) uint16_t vsb[Q4 ? kFewWaves : 1][4][64];  // a step's scales and zeros of values, per wavefront
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
@@ -646,7 +660,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     }
   }
   // the wavefronts' sums meet
-  const int nq_pad = 16 * NQT * HALVES;
+  const int nq_pad = 16 * NQT * HALVES, parts = u.steps > u.span ? (u.steps + u.span - 1) / u.span : 1;
 #pragma unroll
   for (int t = 0; t < NQT; ++t) {
     const float lt = quad_sum(l[t]);
@@ -655,6 +669,15 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     for (int d = 0; d < 8; ++d) *reinterpret_cast<float4_t*>(&ob[wave8][16 * t + li][16 * d + 4 * lg]) = o[t][d];
   }
   __syncthreads();
+  auto answer = [&](int qi, int d0, const float (&r)[8], float L) {
+    const int j = qi / G;
+    const int64_t pos = p0 + j;
+    const bool bad = pos < 0 || pos >= a.len_bound;
+    half8_t h;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) h[x] = bad ? __builtin_bit_cast(half_t, kNanF16) : (half_t)(r[x] / L);
+    *reinterpret_cast<half8_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + d0) = h;
+  };
   for (int qi = tid >> 4; qi < nq; qi += 4 * kFewWaves) {
     const int d0 = 8 * (tid & 15), half = qi / (16 * NQT), qx = qi & (16 * NQT - 1);
     float M = kNoMax, L = 0.f, r[8] = {};
@@ -673,21 +696,66 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         r[4 + i] += f * v[i];
       }
     }
-    if (a.part_o) {
+    if (parts > 1) {
       const int64_t at = (int64_t)blockIdx.x * nq_pad + qi;
-      float4_t* po = reinterpret_cast<float4_t*>(a.part_o + at * kHd + d0);
-      po[0] = float4_t{r[0], r[1], r[2], r[3]};
-      po[1] = float4_t{r[4], r[5], r[6], r[7]};
-      if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
-    } else {
-      const int j = qi / G;
-      const int64_t pos = p0 + j;
-      const bool bad = pos < 0 || pos >= a.len_bound;
-      half8_t h;
+      float* po = a.part_o + at * kHd + d0;
+      if constexpr (kJoins) {
 #pragma unroll
-      for (int x = 0; x < 8; ++x) h[x] = bad ? __builtin_bit_cast(half_t, kNanF16) : (half_t)(r[x] / L);
-      *reinterpret_cast<half8_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + d0) = h;
+        for (int x = 0; x < 4; ++x) publish(reinterpret_cast<float2*>(po) + x, make_float2(r[2 * x], r[2 * x + 1]));
+        if ((tid & 15) == 0) publish(a.part_ml + at, make_float2(M, L));
+      } else {
+        reinterpret_cast<float4_t*>(po)[0] = float4_t{r[0], r[1], r[2], r[3]};
+        reinterpret_cast<float4_t*>(po)[1] = float4_t{r[4], r[5], r[6], r[7]};
+        if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
+      }
+    } else {
+      answer(qi, d0, r, L);
     }
+  }
+  if (!kJoins || !a.arrived || parts == 1) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0)
+    last = __hip_atomic_fetch_add(a.arrived + sg, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+  __syncthreads();
+  if (!last) return;
+  if (tid == 0) __hip_atomic_store(a.arrived + sg, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // the last of a sequence's workgroups joins its parts, in their order
+  const int64_t stride = (int64_t)a.hkv * nq_pad;
+  for (int qi = tid >> 4; qi < nq; qi += 4 * kFewWaves) {
+    const int d0 = 8 * (tid & 15);
+    const int64_t at = ((int64_t)(item - u.part) * a.hkv + g) * nq_pad + qi;
+    constexpr int kFlight = 4;
+    float M = kNoMax, L = 0.f, r[8] = {};
+    for (int p0i = 0; p0i < parts; p0i += kFlight) {
+      float2 x[kFlight], v[kFlight][4];
+#pragma unroll
+      for (int i = 0; i < kFlight; ++i) {
+        const int64_t row = at + (p0i + i < parts ? p0i + i : parts - 1) * stride;
+        x[i] = published(a.part_ml + row);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) v[i][y] = published(reinterpret_cast<const float2*>(a.part_o + row * kHd + d0) + y);
+      }
+      float mn = M;
+#pragma unroll
+      for (int i = 0; i < kFlight; ++i) mn = fmaxf(mn, x[i].x);
+      const float alpha = exp2_fast(M - mn);
+      M = mn;
+      L *= alpha;
+#pragma unroll
+      for (int y = 0; y < 8; ++y) r[y] *= alpha;
+#pragma unroll
+      for (int i = 0; i < kFlight; ++i) {
+        const float f = p0i + i < parts ? exp2_fast(x[i].x - M) : 0.f;
+        L += f * x[i].y;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          r[2 * y] += p0i + i < parts ? f * v[i][y].x : 0.f;
+          r[2 * y + 1] += p0i + i < parts ? f * v[i][y].y : 0.f;
+        }
+      }
+    }
+    answer(qi, d0, r, L);
   }
 }
 
@@ -1143,7 +1211,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   const int parts = nst > u.span ? (nst + u.span - 1) / u.span : 1;
   const int64_t stride = (int64_t)a.hkv * TQ;  // rows of the sums from one part to the next
   const int qx = blockIdx.y * 4 + wave;
-  if (qt * TQ + qx >= nq || first + parts > a.most) return;  // (the latter as in the plan)
+  if (qt * TQ + qx >= nq || (few && parts == 1) || first + parts > a.most) return;  // (the latter as in the plan)
   const int64_t row0 = ((int64_t)first * a.hkv + g) * TQ + qx;
   if (parts <= kWave)
     join<1>(a, G, g, sr, p0, qt * TQ + qx, parts, row0, stride);
@@ -1155,6 +1223,7 @@ struct Plan {
   bool few;
   int tq, grain;    // queries of a tile; steps that a part's are a multiple of
   int tiles, most;  // tiles at most; parts at most (0: the keys are not split)
+  bool joins;       // a sequence's last workgroup joins its parts
 };
 
 Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
@@ -1184,6 +1253,10 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound) {
     if (most) p.grain = kSplitGroups;
   }
   p.most = (int)most;
+  // One workgroup joins eight parts of 16 queries in less time than another kernel takes to start; more wait for its CU.
+  // Both ways, without and with (4-bit entries, 28 query heads on 4, single tokens): one sequence of 4000 positions (8 parts)
+  // 11.7 and 10.3 us, of 32000 (64) 16.3 and 21.7; four of 16000 (16) 16.7 and 17.8; sixteen (4) 31.8 and 29.7.
+  p.joins = most && p.few && p.tq == 16 && (most <= 8 * b || steps <= 8 * p.grain);
   return p;
 }
 
@@ -1214,7 +1287,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
                                    int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
                                    uint16_t* out, hipStream_t stream) {
   const Plan p = make_plan(pr, hq, hkv, len_bound);
-  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most, false};
+  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most, false, nullptr};
   const int units = p.most ? p.most : p.tiles;
   if (p.most) {
     const size_t queries = (size_t)units * hkv * p.tq;
@@ -1223,6 +1296,10 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     if (e != hipSuccess) return e;
     a.part_o = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + queries * kHd);
+    if (p.joins) {
+      const hipError_t ce = zeroed_counters((size_t)pr.b * hkv, stream, &a.arrived);
+      if (ce != hipSuccess) return ce;
+    }
   }
   const bool q4 = cache.k4 != nullptr;
   const dim3 grid((unsigned)(units * hkv));
@@ -1238,7 +1315,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     else
       launch_prompt<false>(p, grid, pr, a, stream);
   }
-  if (p.most)
+  if (p.most && !p.joins)
     hipLaunchKernelGGL(packed_merge_kernel, dim3((unsigned)(p.tiles * hkv), (unsigned)(p.tq / 4)), dim3(256), 0, stream,
                        pr, a, p.tq, p.grain, p.few);
   return hipGetLastError();

@@ -481,6 +481,42 @@ def test_pass_captured(fmt):
         assert same(a, bb)
 
 
+# (rows, past), hq, hkv: the parts joined by their last workgroup, by a kernel of its own, and those of a prompt's tiles
+@pytest.mark.parametrize("seqs,hq,hkv", [([(1, 4000)], 28, 4), ([(2, 900), (0, 7), (1, 3900)] * 6, 12, 2), ([(1, 20000)], 12, 2),
+                                         ([(9, 3000), (3, 2000)], 28, 4), ([(70, 2500), (33, 700)], 14, 2)])
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_split_captured(seqs, hq, hkv, fmt):
+    """Keys split over workgroups: recorded once, on a stream of its own, and replayed with positions that move, between
+    eager calls that use the workspace too; the same bits as eager calls."""
+    most = max(n for n, _ in seqs)
+    cap = (max(n + p for n, p in seqs) + 200) // 64 * 64
+    q, k, v = attention_case(seqs, hq, hkv, cap, 81)
+    if fmt == "q4":
+        cache, attn = pack_q4(k, v), sq.sq_packed_attention_q4
+        k, v = values_q4(cache)
+    else:
+        cache, attn = (k, v.transpose(2, 3).contiguous()), sq.sq_packed_attention_f16
+    start, first = starts([n for n, _ in seqs]), ints([p for _, p in seqs])
+    eager = [attn(q, *cache, start, first + 17 * i, max_rows=most) for i in range(4)]
+    check_attention(eager[3], q, k, v, [(n, p + 51) for n, p in seqs])
+    out, pos = torch.empty_like(q), first.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            attn(q, *cache, start, pos, max_rows=most, out=out)
+            pos += 17
+    torch.cuda.synchronize()
+    for i in range(4):
+        out.fill_(9)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[i]), i
+        assert torch.equal(attn(q, *cache, start, first, max_rows=most), eager[0])
+        torch.cuda.synchronize()
+
+
 def test_strided_and_other_tensors_are_refused():
     q = normal((4, 4, 128), 41)
     k, v = normal((1, 2, 64, 128), 42), normal((1, 2, 128, 64), 43)
