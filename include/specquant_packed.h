@@ -86,8 +86,8 @@ sq_status sq_packed_kv_read_q4(const uint8_t* k_codes, const uint16_t* k_scales,
  * value.  q, out [rows][hq][128] fp16.  A row reads its sequence's positions
  * 0 .. its own, which must hold written entries; what is at later positions does
  * not matter (NaN and infinities included).  A row at a position outside [0, len_bound)
- * gets NaN.  Few workgroups for the chip: the keys are split over up to 1024
- * workgroups, whose sums take at most 33 MiB of the library workspace.
+ * gets NaN.  Few workgroups for the chip: the keys are split over up to 256
+ * workgroups, whose sums take at most 17 MiB of the library workspace.
  * capacity <= 2^28. */
 sq_status sq_packed_attention_f16(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
                                   const int32_t* row_start, int32_t b, int64_t rows, int64_t max_rows, int32_t hq,

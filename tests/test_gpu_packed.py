@@ -417,9 +417,10 @@ def test_long_cache_offsets_q4():
     assert same(ko, k[0, :, -rows:].transpose(0, 1))
 
 
-def test_many_parts_of_one_sequence():
-    """One long sequence beside 129 short ones on one kv head: its keys in more than 512 parts."""
-    b, hq, cap = 130, 64, 140032
+@pytest.mark.parametrize("b", [30, 130])
+def test_many_parts_of_one_sequence(b):
+    """One long sequence beside short ones on one kv head: its keys in many parts, and whole."""
+    hq, cap = 64, 140032
     past = [10 + i % 3 for i in range(b - 1)] + [cap - 1]
     c = (torch.randint(0, 256, (b, 1, cap, 64), dtype=torch.uint8, device=DEV), torch.zeros((b, 1, cap, 4), dtype=F16, device=DEV),
          torch.randint(0, 256, (b, 1, cap // 64, 64, 64), dtype=torch.uint8, device=DEV),
