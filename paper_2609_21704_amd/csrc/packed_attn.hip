@@ -42,7 +42,6 @@ struct AttnArgs {
   int most;         // parts of one kv head, 0 without splitting
   int grain;        // steps that a part's are a multiple of
   bool longest;     // the tiles with the most keys first (they do not all run at once)
-  int32_t* arrived;  // few rows: parts that are done of each (sequence, kv head), null where a merge kernel follows
 };
 
 // max / sum over the two lanes that share a column of a 32 x 32 product
@@ -358,17 +357,6 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
   return without(w, o);
 }
 
-// Sums for another workgroup, in stores that go through to the level that all XCDs share (so that the wait for them is all
-// that has to come before the arrival is counted), and read from there.
-__device__ __forceinline__ void publish(float2* p, float2 v) {
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED,
-                     __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 published(const float2* p) {
-  return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED,
-                                                      __HIP_MEMORY_SCOPE_AGENT));
-}
-
 // ---------------------------------------------------------------- few rows
 // One workgroup per (part of the keys, sequence, kv head); its wavefronts take the part's steps of 64 keys in turn, each
 // for all the queries (NQT tiles of 16), and meet in LDS.  v_mfma_f32_16x16x32_f16: lane l holds row / column li = l %
@@ -378,7 +366,7 @@ __device__ __forceinline__ float2 published(const float2* p) {
 // were just used (fp16 and two tiles: the registers hold only one of the two, loaded when its turn comes).  Up to
 // 32 queries: all eight wavefronts take keys; up to 64 (4-bit entries): half of them the first 32, half the rest, over the
 // same keys.  Bound by the cache's bytes: 16 tokens after 13k to 31k positions (28 heads on 4, 207 MB of 4-bit entries)
-// 43.5 us, 4.75 TB/s, what a large copy reaches; a few sequences by latency: the plan 1 us, the first loads 2, a step of 64
+// 40.5 us and 4.8 for the merge, 5.1 TB/s without it, where a large copy reaches 4.8; a few sequences by latency: the plan 1 us, the first loads 2, a step of 64
 // keys 0.7, the meeting in LDS 1, and a CU takes in fp16 entries at about 60 GB/s.
 constexpr int kFewWaves = 8;
 
@@ -387,10 +375,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
                                                                                                         AttnArgs a) {
   constexpr int NW = kFewWaves / HALVES;  // wavefronts that share the keys of a half's queries
   constexpr bool kAhead = Q4 || NQT == 1;
-  constexpr bool kJoins = NQT == 1;  // (up to 16 queries: the last workgroup may join the parts)
   __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
   __shared__ float2 ml[kFewWaves][16 * NQT];
-  __shared__ bool last;
   __shared__ __align__(16) uint16_t vsb[Q4 ? kFewWaves : 1][4][64];  // a step's scales and zeros of values, per wavefront
   const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
@@ -710,63 +696,12 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     if (parts > 1) {
       const int64_t at = (int64_t)blockIdx.x * nq_pad + qi;
       float* po = a.part_o + at * kHd + d0;
-      if constexpr (kJoins) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) publish(reinterpret_cast<float2*>(po) + x, make_float2(r[2 * x], r[2 * x + 1]));
-        if ((tid & 15) == 0) publish(a.part_ml + at, make_float2(M, L));
-      } else {
-        reinterpret_cast<float4_t*>(po)[0] = float4_t{r[0], r[1], r[2], r[3]};
-        reinterpret_cast<float4_t*>(po)[1] = float4_t{r[4], r[5], r[6], r[7]};
-        if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
-      }
+      reinterpret_cast<float4_t*>(po)[0] = float4_t{r[0], r[1], r[2], r[3]};
+      reinterpret_cast<float4_t*>(po)[1] = float4_t{r[4], r[5], r[6], r[7]};
+      if ((tid & 15) == 0) a.part_ml[at] = make_float2(M, L);
     } else {
       answer(qi, d0, r, L);
     }
-  }
-  if (!kJoins || !a.arrived || parts == 1) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (tid == 0)
-    last = __hip_atomic_fetch_add(a.arrived + sg, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
-  __syncthreads();
-  if (!last) return;
-  if (tid == 0) __hip_atomic_store(a.arrived + sg, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  // the last of a sequence's workgroups joins its parts, in their order
-  const int64_t stride = (int64_t)a.hkv * nq_pad;
-  for (int qi = tid >> 4; qi < nq; qi += 4 * kFewWaves) {
-    const int d0 = 8 * (tid & 15);
-    const int64_t at = ((int64_t)(item - u.part) * a.hkv + g) * nq_pad + qi;
-    constexpr int kFlight = 4;
-    float M = kNoMax, L = 0.f, r[8] = {};
-    for (int p0i = 0; p0i < parts; p0i += kFlight) {
-      float2 x[kFlight], v[kFlight][4];
-#pragma unroll
-      for (int i = 0; i < kFlight; ++i) {
-        const int64_t row = at + (p0i + i < parts ? p0i + i : parts - 1) * stride;
-        x[i] = published(a.part_ml + row);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) v[i][y] = published(reinterpret_cast<const float2*>(a.part_o + row * kHd + d0) + y);
-      }
-      float mn = M;
-#pragma unroll
-      for (int i = 0; i < kFlight; ++i) mn = fmaxf(mn, x[i].x);
-      const float alpha = exp2_fast(M - mn);
-      M = mn;
-      L *= alpha;
-#pragma unroll
-      for (int y = 0; y < 8; ++y) r[y] *= alpha;
-#pragma unroll
-      for (int i = 0; i < kFlight; ++i) {
-        const float f = p0i + i < parts ? exp2_fast(x[i].x - M) : 0.f;
-        L += f * x[i].y;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          r[2 * y] += p0i + i < parts ? f * v[i][y].x : 0.f;
-          r[2 * y + 1] += p0i + i < parts ? f * v[i][y].y : 0.f;
-        }
-      }
-    }
-    answer(qi, d0, r, L);
   }
 }
 
@@ -1207,7 +1142,9 @@ __device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr
   *reinterpret_cast<half2_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + 2 * lane) = r;
 }
 
-// Four queries of a tile a workgroup, one a wavefront (sixteen, in wavefronts or in turn: 7.1 and 11.2 us for 5.0).
+// Four queries of a tile a workgroup, one a wavefront (sixteen, in wavefronts or in turn: 7.1 and 11.2 us for 5.0).  A
+// sequence's last workgroup could join few parts itself (16 tokens after 22k positions 43.7 us for 45.4), with counters that
+// would have to be zero before every call: one pair of calls that overlap would leave them wrong for good.
 __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnArgs a, int TQ, int grain, bool few) {
   const int wave = threadIdx.x >> 6;
   const int G = a.hq / a.hkv;
@@ -1238,7 +1175,6 @@ struct Plan {
   bool few;
   int tq, grain;    // queries of a tile; steps that a part's are a multiple of
   int tiles, most;  // tiles at most; parts at most (0: the keys are not split)
-  bool joins;       // a sequence's last workgroup joins its parts
 };
 
 Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound, bool q4) {
@@ -1255,11 +1191,12 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound, bool q4
     p.tq = pr.max_rows * G <= 16 ? 16 : (pr.max_rows * G <= 32 ? 32 : 64);
     p.tiles = pr.b;
     // Whole sequences from half a workgroup a CU: in up to 1024 parts, 64 sequences of one row after 2000 positions took
-    // 62.7 us for 42.7 (4-bit: 36.7 for 17.1).  Parts of four steps at least (eight: one sequence after 1000 positions 19.1
-    // us for 10.7, after 4000 16.0 for 13.4).  8 steps of fp16 entries take 12.3 us whole and 10.7 in two parts, 11 of 4-bit
-    // ones 7.8 and 8.8, 16 of them 9.3 and 8.3.
+    // 62.7 us for 42.7 (4-bit: 36.7 for 17.1).  Parts of four steps at least (eight: one fp16 sequence after
+    // 1000 positions 17.2 us for 12.8, after 4000 17.2 for 13.2).  The merge has to pay: one fp16 row over 8 steps takes 12.2 us
+    // whole and 12.7 in parts, over 16 19.1 and 12.8; 4-bit, over 16 9.2 and 10.2, over 21 11.1 and 10.2; 9 rows (63 queries)
+    // over 8 13.0 and 14.4, over 16 18.4 and 14.4.
     p.grain = 4;
-    if (2 * b > most || steps <= (q4 ? 3 : 1) * p.grain) most = 0;
+    if (2 * b > most || steps <= (q4 && p.tq <= 32 ? 4 : 2) * p.grain) most = 0;
   } else {
     auto tiles = [&](int64_t tq) {
       return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq
@@ -1274,10 +1211,6 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound, bool q4
     if (2 * p.tiles > most || steps <= 4) most = 0;
   }
   p.most = (int)most;
-  // One workgroup joins eight parts of 16 queries in less time than another kernel takes to start; more wait for its CU.
-  // Without and with (4-bit entries, 28 query heads on 4, single tokens): one sequence in 8 parts 11.7 and 10.3 us, in 64
-  // 16.3 and 21.7; four in 16 each 16.7 and 17.8; sixteen in 4 each 31.8 and 29.7.
-  p.joins = most && p.few && p.tq == 16 && (most <= 8 * b || steps <= 8 * p.grain);
   return p;
 }
 
@@ -1309,7 +1242,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
                                    uint16_t* out, hipStream_t stream) {
   const bool q4 = cache.k4 != nullptr;
   const Plan p = make_plan(pr, hq, hkv, len_bound, q4);
-  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most, p.grain, false, nullptr};
+  AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most, p.grain, false};
   const int units = p.most ? p.most : p.tiles;
   if (p.most) {
     const size_t queries = (size_t)units * hkv * p.tq;
@@ -1318,10 +1251,6 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     if (e != hipSuccess) return e;
     a.part_o = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + queries * kHd);
-    if (p.joins) {
-      const hipError_t ce = zeroed_counters((size_t)pr.b * hkv, stream, &a.arrived);
-      if (ce != hipSuccess) return ce;
-    }
   }
   const dim3 grid((unsigned)(units * hkv));
   // Where not all tiles run at once: prompts of 400, 800 .. 2800 rows 189 us for 209, four of 1171 57.7 for 62.4, 29 of 64 ..
@@ -1338,7 +1267,7 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     else
       launch_prompt<false>(p, grid, pr, a, stream);
   }
-  if (p.most && !p.joins)
+  if (p.most)
     hipLaunchKernelGGL(packed_merge_kernel, dim3((unsigned)(p.tiles * hkv), (unsigned)(p.tq / 4)), dim3(256), 0, stream,
                        pr, a, p.tq, p.grain, p.few);
   return hipGetLastError();

@@ -482,7 +482,7 @@ def test_pass_captured(fmt):
         assert same(a, bb)
 
 
-# (rows, past), hq, hkv: the parts joined by their last workgroup, by a kernel of its own, and those of a prompt's tiles
+# (rows, past), hq, hkv: single tokens, blocks and a prompt's tiles whose keys are split
 @pytest.mark.parametrize("seqs,hq,hkv", [([(1, 4000)], 28, 4), ([(2, 900), (0, 7), (1, 3900)] * 6, 12, 2), ([(1, 20000)], 12, 2),
                                          ([(9, 3000), (3, 2000)], 28, 4), ([(70, 2500), (33, 700)], 14, 2)])
 @pytest.mark.parametrize("fmt", ["f16", "q4"])
