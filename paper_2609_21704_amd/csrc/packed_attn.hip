@@ -706,8 +706,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 }
 
 // -------------------------------------------------------------- many rows
-// One workgroup per (tile of 32 NW queries, kv head, part of the keys): each wavefront 32 queries, the keys in steps of
-// 64 through LDS buffers, one barrier a step.  fp16 entries go from memory to LDS directly, kRing - 1 steps ahead; 4-bit
+// One workgroup per (tile of 32 NW queries, kv head, part of the keys): each wavefront 32 queries, KW groups of NW of them the
+// keys in turn, in steps of 64 through LDS buffers, one barrier a step.  fp16 entries go from memory to LDS directly, kRing - 1 steps ahead; 4-bit
 // ones through registers, one step ahead, and become halves on the way.
 // v_mfma_f32_32x32x16_f16: lane l holds row / column lc = l % 32 and k = 8 h .. +8 (h = l / 32), and of D rows 8 (i / 4) +
 // 4 h + i % 4 of column lc.  Row r of a key tile is the key r with bits 2 and 3 exchanged, so that a lane's 16 scores
@@ -741,11 +741,8 @@ __device__ __forceinline__ void barrier_after_loads() {
   asm volatile("" ::: "memory");
 }
 
-// Buffers of 32 KB: two for workgroups of four wavefronts, two of which share a CU, three for those of eight.  Where
-// keys are split and a workgroup has its CU for itself, more do not help: 20.8 us with two, 22.5 with three and 24.2 with
-// four (three sequences of 17 to 60 rows after 3000 to 9000 cached positions, 28 query heads on 4).
-constexpr int kSplitGroups = 2;
-
+// Buffers of 32 KB a group: two for four wavefronts, two groups of which share a CU, three for those of eight.  Where keys are
+// split more did not help (one group: 20.8 us with two, 22.5 with three, 24.2 with four).
 constexpr int ring(bool q4, int nw) { return q4 || nw < 8 ? 2 : 3; }
 
 template <bool Q4, int NW, int KW, bool SPLIT>
