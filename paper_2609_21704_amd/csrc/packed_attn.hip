@@ -366,8 +366,8 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
 // were just used (fp16 and two tiles: the registers hold only one of the two, loaded when its turn comes).  Up to
 // 32 queries: all eight wavefronts take keys; up to 64 (4-bit entries): half of them the first 32, half the rest, over the
 // same keys.  Bound by the cache's bytes: 16 tokens after 13k to 31k positions (28 heads on 4, 207 MB of 4-bit entries)
-// 40.5 us and 4.8 for the merge, 5.1 TB/s without it, where a large copy reaches 4.8; a few sequences by latency: the plan 1 us, the first loads 2, a step of 64
-// keys 0.7, the meeting in LDS 1, and a CU takes in fp16 entries at about 60 GB/s.
+// 40.5 us and 4.8 for the merge, 5.1 TB/s without it, where a large copy reaches 4.8; a few sequences by latency: the plan
+// 1 us, the first loads 2, a step of 64 keys 0.7, the meeting in LDS 1, and a CU takes in fp16 entries at about 60 GB/s.
 constexpr int kFewWaves = 8;
 
 template <bool Q4, int NQT, int HALVES>
@@ -740,6 +740,10 @@ __device__ __forceinline__ void barrier_after_loads() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+
+// Where keys are split, a CU has one workgroup: two groups of four wavefronts take its steps in turn and meet in LDS (20.2 us
+// for 20.8 with one: three sequences of 20 to 57 rows after 3358 to 8773 cached positions, 28 query heads on 4).
+constexpr int kSplitGroups = 2;
 
 // Buffers of 32 KB a group: two for four wavefronts, two groups of which share a CU, three for those of eight.  Where keys are
 // split more did not help (one group: 20.8 us with two, 22.5 with three, 24.2 with four).
