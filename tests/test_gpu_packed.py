@@ -435,6 +435,23 @@ def test_many_parts_of_one_sequence(b):
     check_attention(out[pick], q[pick], k, v, [(1, past[i]) for i in pick])
 
 
+@pytest.mark.parametrize("most", [1, 40])
+def test_thousands_of_sequences(most):
+    """16000 sequences, most of them of one row, every 500th of none or of several: both kernels."""
+    b, hq, hkv, cap = 16000, 8, 4, 64
+    lens = [1 if most == 1 or i % 500 else i // 500 % 40 for i in range(b)]
+    past = [i % 24 for i in range(b)]
+    rows, st = sum(lens), starts(lens)
+    qkv = normal((rows, (hq + 2 * hkv) * 128), 91).float()
+    k, v = normal((b, hkv, cap, 128), 92), normal((b, hkv, 128, cap), 93)
+    q = sq.sq_packed_rope_kv_f16(qkv, None, st, ints(past), hq, k, v, max_rows=most)
+    out = sq.sq_packed_attention_f16(q, k, v, st, ints(past), max_rows=most)
+    for i in (0, 1, 499, 500, 7500, 8191, 8192, b - 500, b - 1):
+        a = int(st[i])
+        check_attention(out[a:a + lens[i]], q[a:a + lens[i]], k[i:i + 1], v[i:i + 1].transpose(2, 3), [(lens[i], past[i])])
+    assert bool(torch.isfinite(out).all())
+
+
 @pytest.mark.parametrize("fmt", ["f16", "q4"])
 def test_pass_captured(fmt):
     """A prompt, then single tokens, as a decoder makes them: the tokens' calls recorded in a graph that moves the positions
