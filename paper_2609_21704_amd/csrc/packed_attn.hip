@@ -169,12 +169,13 @@ struct Planner {
 
   // Unit `item` of the list of whole tiles by the number of their keys, the most first, for up to 64 sequences (the plain
   // list for more).  TQ queries are G-th as many rows, so a tile's place is its level: the sequence's tiles from its last,
-  // after as many as it is shorter than the longest sequence.  B(v), the tiles below level v, is one reduction; the search
-  // for the item's level takes three of them a turn.
+  // after as many as it is shorter than the longest sequence that has tiles (2^23 at most: with the 2^20 tiles there can be
+  // a level stays a whole number of fp32, and what lies further apart only loses its order).  B(v), the tiles below level v,
+  // is one reduction; the search for the item's level takes three of them a turn.
   __device__ __forceinline__ bool find_longest(int item, int G, int TQ, Unit& u) const {
     if (b > kWave) return find(item, u);
-    const float longest = wave_most((float)mine.steps);
-    const int off = mine.tiles > 0 ? (int)((longest - (float)mine.steps) * (float)(kTile * G) / (float)TQ) : 1 << 24;
+    const float longest = wave_most(mine.tiles > 0 ? (float)mine.steps : 0.f);
+    const int off = (int)fmaxf(fminf((longest - (float)mine.steps) * (float)(kTile * G) / (float)TQ, 0x1p23f), 0.f);
     const int levels = (int)wave_most(mine.tiles > 0 ? (float)(off + mine.tiles) : 0.f);
     auto below = [&](int v) {
       const int n = v - off;
