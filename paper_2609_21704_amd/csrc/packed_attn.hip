@@ -13,7 +13,8 @@
 // Scores, maxima, sums and O are fp32.  A weight enters the product with V as one binary16: 2^-11 of itself off, as the
 // output's own rounding is, and independent from key to key.  Weights are kept times 2^7, and the reference maximum is
 // moved only when a row's maximum passes it by 2^8, so they stay below 2^15 and a weight loses bits only
-// below 2^-21 of the row's largest.
+// below 2^-21 of the row's largest.  The reference is kept as the score it was, unscaled, and joined so: a score's scaling
+// rounds by what at 10^9 is many powers of two.
 #include <type_traits>
 
 #include "sq_internal.hpp"
@@ -26,9 +27,10 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;  // keys per step
 constexpr float kScale = 1.4426950408889634f * 0.08838834764831845f;  // log2(e) / sqrt(128)
-constexpr float kShift = 7.f, kSlack = 8.f;
+constexpr float kShift = 7.f, kSlack = 8.f / kScale;  // (the slack in unscaled scores)
+constexpr float kFar = 4096.f;  // references from which their scaling's rounding (2^-15 here) would matter
 constexpr int kMaxParts = 256;  // of one kv head's keys, all sequences
-constexpr float kNoMax = -1e30f;  // a finite start: exp2(kNoMax - m) = 0 and exp2(-inf - kNoMax) = 0
+constexpr float kNoMax = -1e30f;  // a finite start, below every score: its weights beside any other's are 0
 
 struct AttnArgs {
   const uint16_t* q;
@@ -52,6 +54,15 @@ __device__ __forceinline__ float pair_fold(float v, OP op) {
   const uint32_t p0 = p[0], p1 = p[1];
   return op(__builtin_bit_cast(float, p0), __builtin_bit_cast(float, p1));
 }
+
+// The factor from reference `from` to reference `to`.
+__device__ __forceinline__ float rescale(float from, float to) { return exp2_fast((from - to) * kScale); }
+
+// A weight is exp2(score kScale + ref).  Far from zero that would round the product and the reference each on its own, by
+// more than a weight's range at the ends of binary16's queries and keys: there the reference is taken from the scores first
+// (far: some lane of the wavefront is).
+__device__ __forceinline__ bool far_reference(float m) { return __any(fabsf(m) > kFar && m != kNoMax); }
+__device__ __forceinline__ float near_reference(float m) { return __builtin_fmaf(m, -kScale, kShift); }
 
 // How the work is laid over workgroups.  A sequence's queries are `tiles` tiles, each over the sequence's `steps` steps of
 // 64 keys, and every tile's steps are cut into parts of `span`: `span` is what keeps the number of parts of all sequences
@@ -553,15 +564,22 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) cm = fmaxf(cm, sc[t][kt][i]);
-      cm = quad_max(cm) * kScale;
+      cm = quad_max(cm);
       if (__any(cm > m[t] + kSlack)) {
-        const float mn = fmaxf(m[t], cm), alpha = exp2_fast(m[t] - mn);
+        const float mn = fmaxf(m[t], cm), alpha = rescale(m[t], mn);
         m[t] = mn;
         l[t] *= alpha;
 #pragma unroll
         for (int d = 0; d < 8; ++d) o[t][d] *= alpha;
       }
-      const float ref = kShift - m[t];
+      float ref = near_reference(m[t]);
+      if (far_reference(m[t])) {  // uniform
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[t][kt][i] -= m[t];
+        ref = kShift;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
@@ -684,7 +702,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const float2 x = ml[HALVES * w + half][qx];
-      const float f = exp2_fast(x.x - M);
+      const float f = rescale(x.x, M);
       L += f * x.y;
       const float4_t u = *reinterpret_cast<const float4_t*>(&ob[HALVES * w + half][qx][d0]);
       const float4_t v = *reinterpret_cast<const float4_t*>(&ob[HALVES * w + half][qx][d0 + 4]);
@@ -971,15 +989,22 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) cm = fmaxf(cm, sc[b][i]);
-      cm = pair_fold(cm, [](float x, float y) { return fmaxf(x, y); }) * kScale;
+      cm = pair_fold(cm, [](float x, float y) { return fmaxf(x, y); });
       if (__any(cm > m + kSlack)) {
-        const float mn = fmaxf(m, cm), alpha = exp2_fast(m - mn);
+        const float mn = fmaxf(m, cm), alpha = rescale(m, mn);
         m = mn;
         l *= alpha;
 #pragma unroll
         for (int d = 0; d < 4; ++d) o[d] *= alpha;
       }
-      const float ref = kShift - m;
+      float ref = near_reference(m);
+      if (far_reference(m)) {  // uniform
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[b][i] -= m;
+        ref = kShift;
+      }
       half8_t pf[4];
       float sum = 0.f;
 #pragma unroll
@@ -1040,7 +1065,7 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
     __syncthreads();
     if (!owner || kw == 1) return;
     const float2 other = ml[lane];
-    const float mn = fmaxf(m, other.x), mine = exp2_fast(m - mn), theirs = exp2_fast(other.x - mn);
+    const float mn = fmaxf(m, other.x), mine = rescale(m, mn), theirs = rescale(other.x, mn);
     m = mn;
     l = l * mine + other.y * theirs;
 #pragma unroll
@@ -1114,7 +1139,7 @@ __device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr
   for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, kWave));
 #pragma unroll
   for (int i = 0; i < kMost; ++i) {
-    ml[i].x = exp2_fast(ml[i].x - M);
+    ml[i].x = rescale(ml[i].x, M);
     L += ml[i].x * ml[i].y;
   }
   L = wave_sum(L);

@@ -31,3 +31,50 @@ def test_a_prompt_beside_a_sequence_of_millions(rows):
     kd, vd = values_q4([t[1:, :, :640 if i < 2 else 10] for i, t in enumerate(c)])
     check_attention(out, q, kd, vd, [(n, 0)], lead=rows)
     assert bool((out[:rows] == 0).all())  # (its values are zeros)
+
+
+@pytest.mark.parametrize("rows,past", [(1, 700), (4, 700), (9, 700), (150, 600), (30, 9000)])
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_scores_past_whole_numbers_of_fp32(rows, past, fmt):
+    """Scores up to 2.7e11, where neighbours in fp32 lie thousands apart.  Queries and keys of equal elements: a score is 128
+    equal terms of at most 11 bits and a power of two, exact in fp32, so that the row's largest keys share the weight
+    evenly and no other has any.  Then keys at random: the largest score takes all, wherever it leads by more than
+    twice what 128 fp32 terms may be off (2^-24 each of the largest sum, and eight more roundings)."""
+    hq, hkv, cap = 7, 1, 9088
+    n = past + rows
+    v = normal((1, hkv, cap, 128), 121)
+
+    def run(q, k):
+        if fmt == "f16":
+            return sq.sq_packed_attention_f16(q, k, v.transpose(2, 3).contiguous(), starts([rows]), ints([past])), k, v
+        cache = pack_q4(k, v)
+        return sq.sq_packed_attention_q4(q, *cache, starts([rows]), ints([past])), *values_q4(cache)
+
+    at = torch.arange(cap, device=DEV)
+    for shape in ("up", "down", "steps"):
+        c = {"up": at // 3, "down": (n - at).clamp(min=0) // 3, "steps": at * 37 % 11 * 100}[shape]
+        c = (c.float() / c[:n].max() * 65504).clamp(max=65504).half()
+        q = torch.full((rows, hq, 128), 32768.0, dtype=F16, device=DEV)
+        out, kk, vv = run(q, c.view(1, 1, cap, 1).expand(1, hkv, cap, 128).contiguous())
+        assert bool((kk == kk[..., :1]).all())
+        seen = at[None, :n] <= past + torch.arange(rows, device=DEV)[:, None]
+        s = torch.where(seen, kk[0, 0, :n, 0].double()[None], -math.inf)
+        w = (s == s.amax(1, keepdim=True)).double()
+        ref = (w @ vv[0, 0, :n].double()) / w.sum(1, keepdim=True)
+        mag = (w @ vv[0, 0, :n].double().abs()) / w.sum(1, keepdim=True)
+        # equal weights of 2^7 or a power of two below 2^15, sums of them in fp32, the output's rounding
+        bound = ref.abs() * 2.0 ** -11 + mag * (n * 2.0 ** -24 + 2.0 ** -18) + 2.0 ** -25
+        err = (out.double() - ref[:, None]).abs()
+        assert bool((err <= bound[:, None]).all()), (shape, float(err.max()))
+    q, k = normal((rows, hq, 128), 122, std=3000.0), normal((1, hkv, cap, 128), 123, std=3000.0)
+    out, kk, vv = run(q, k)
+    assert bool(torch.isfinite(out).all())
+    s = torch.matmul(q.double().view(rows * hq, 128), kk[0, 0, :n].double().t().contiguous())
+    s = s.masked_fill(at[None, :n] > (past + torch.arange(rows, device=DEV).repeat_interleave(hq))[:, None], -math.inf)
+    top = s.topk(2, 1)
+    dot = torch.matmul(q.double().abs().view(rows * hq, 128), kk[0, 0, :n].double().abs().t().contiguous()).amax(1)
+    clear = top.values[:, 0] - top.values[:, 1] > 2 * dot * 136 * 2.0 ** -24 + 1000
+    assert int(clear.sum()) > rows * hq // 2
+    want = vv[0, 0, top.indices[:, 0][clear]].double()
+    # a weight's binary16, the output's
+    assert bool(((out.view(-1, 128)[clear].double() - want).abs() <= want.abs() * (2.0 ** -10 + 2.0 ** -18) + 2.0 ** -25).all())
