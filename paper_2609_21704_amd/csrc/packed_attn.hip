@@ -745,7 +745,8 @@ typedef __attribute__((address_space(3))) void lds_void;
 // assembly, because the compiler waits for all loads of the builtin before any read of LDS, whichever buffer it reads;
 // the waits are barrier_after_loads.  There is no result register, and the addresses are read when the load is issued.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(dst)
+               : "memory", "m0");
 }
 template <class T>
 __device__ __forceinline__ uint32_t lds_address(T* p) {
