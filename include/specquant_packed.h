@@ -82,8 +82,8 @@ sq_status sq_packed_kv_read_q4(const uint8_t* k_codes, const uint16_t* k_scales,
 
 /* Causal grouped-query attention of packed rows over the cache: out[r][h] as
  * sq_attention_f16 has it, for any number of rows per sequence; scores, softmax
- * sums and outputs in fp32, each weight rounded to fp16 for its product with the
- * value.  q, out [rows][hq][128] fp16.  A row reads its sequence's positions
+ * sums and outputs in fp32, a weight rounded for its product with the value to two fp16
+ * terms (2^-20 of it) where max_rows hq / hkv <= 32, to one (2^-11) above.  q, out [rows][hq][128] fp16.  A row reads its sequence's positions
  * 0 .. its own, which must hold written entries; what is at later positions does
  * not matter (NaN and infinities included).  A row at a position outside [0, len_bound)
  * gets NaN.  Few workgroups for the chip: the keys are split over up to 256
@@ -94,7 +94,7 @@ sq_status sq_packed_attention_f16(const uint16_t* q, const uint16_t* k_cache, co
                                   int32_t hkv, const int32_t* pos_base, int32_t pos_offset, int64_t len_bound,
                                   int64_t capacity, uint16_t* out, hipStream_t stream);
 /* The same over a 4-bit cache: the attention over the fp16 values its entries
- * stand for. */
+ * stand for, each weight as one fp16 term. */
 sq_status sq_packed_attention_q4(const uint16_t* q, const uint8_t* k_codes, const uint16_t* k_scales,
                                  const uint8_t* v_codes, const uint16_t* v_scales, const int32_t* row_start, int32_t b,
                                  int64_t rows, int64_t max_rows, int32_t hq, int32_t hkv, const int32_t* pos_base,

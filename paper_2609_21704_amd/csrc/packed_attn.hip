@@ -10,8 +10,14 @@
 // and the rescaling of O need no exchange but a fold over the lanes of one column.  The keys enter S^T in an order that
 // makes a lane's scores consecutive keys, which is the order that P^T's fragments take: P goes from one product to the
 // next in registers.
-// Scores, maxima, sums and O are fp32.  A weight enters the product with V as one binary16: 2^-11 of itself off, as the
-// output's own rounding is, and independent from key to key.  Weights are kept times 2^7, and the reference maximum is
+// Scores, maxima, sums and O are fp32.  A weight enters the product with V as two binary16 terms (2^-20 of itself off at
+// most) in few rows over fp16 entries, whose bytes bound them: the second product costs nothing there (64 tokens after 2000
+// positions 54.9 us for 54.8, 32 blocks of 4 rows 37.7 for 37.1).  It enters as one (2^-11 of itself off, as the output's own
+// rounding is, and independent from key to key) where the products bound the kernel, in prompts (16001 rows would take
+// 2527 us for 1832, four of about 1170 81 for 65), and over 4-bit entries, whose own steps are a fifteenth of a group's
+// range and whose dequantisation fills the rest (64 tokens after 2000 positions 18.6 for 17.5, 16 after 13k to 31k 53 for 49).
+// Against 64 bits, relative in the 2-norm, one term is 2.0e-4 to 2.2e-4 off where the output's rounding alone is 2.0e-4 to
+// 2.1e-4.  Weights are kept times 2^7, and the reference maximum is
 // moved only when a row's maximum passes it by 2^8, so they stay below 2^15 and a weight loses bits only
 // below 2^-21 of the row's largest.  The reference is kept as the score it was, unscaled, and joined so: a score's scaling
 // rounds by what at 10^9 is many powers of two.
@@ -63,6 +69,12 @@ __device__ __forceinline__ float rescale(float from, float to) { return exp2_fas
 // (far: some lane of the wavefront is).
 __device__ __forceinline__ bool far_reference(float m) { return __any(fabsf(m) > kFar && m != kNoMax); }
 __device__ __forceinline__ float near_reference(float m) { return __builtin_fmaf(m, -kScale, kShift); }
+
+// Two weights as two binary16 terms each: truncated, and what that leaves (exact in fp32), truncated.
+__device__ __forceinline__ void two_terms(float p0, float p1, half2_t& hi, half2_t& lo) {
+  hi = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0, p1));
+  lo = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0 - (float)hi[0], p1 - (float)hi[1]));
+}
 
 // How the work is laid over workgroups.  A sequence's queries are `tiles` tiles, each over the sequence's `steps` steps of
 // 64 keys, and every tile's steps are cut into parts of `span`: `span` is what keeps the number of parts of all sequences
@@ -387,6 +399,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
                                                                                                         AttnArgs a) {
   constexpr int NW = kFewWaves / HALVES;  // wavefronts that share the keys of a half's queries
   constexpr bool kAhead = Q4 || NQT == 1;
+  constexpr bool kTwoTerms = !Q4;
   __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
   __shared__ float2 ml[kFewWaves][16 * NQT];
   __shared__ __align__(16) uint16_t vsb[Q4 ? kFewWaves : 1][4][64];  // a step's scales and zeros of values, per wavefront
@@ -426,7 +439,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   }
   float m[NQT], l[NQT];
   float4_t o[NQT][8];
-  half8_t pf[NQT][2];
+  half8_t pf[NQT][2], pl[kTwoTerms ? NQT : 1][2];  // the weights, and their second terms
 #pragma unroll
   for (int t = 0; t < NQT; ++t) {
     m[t] = kNoMax;
@@ -505,6 +518,10 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   auto product = [&](int d, half8_t v0, half8_t v1) {
 #pragma unroll
     for (int t = 0; t < NQT; ++t) {
+      if constexpr (kTwoTerms) {
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pl[t][0], o[t][d], 0, 0, 0);
+        o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pl[t][1], o[t][d], 0, 0, 0);
+      }
       o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[t][0], o[t][d], 0, 0, 0);
       o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[t][1], o[t][d], 0, 0, 0);
     }
@@ -584,10 +601,19 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = exp2_fast(__builtin_fmaf(sc[t][kt][i], kScale, ref));
-          sum += p;
-          pf[t][kt >> 1][4 * (kt & 1) + i] = (half_t)p;
+        for (int i = 0; i < 4; i += 2) {
+          const float p0 = exp2_fast(__builtin_fmaf(sc[t][kt][i], kScale, ref));
+          const float p1 = exp2_fast(__builtin_fmaf(sc[t][kt][i + 1], kScale, ref));
+          sum += p0;
+          sum += p1;
+          half2_t hi = {(half_t)p0, (half_t)p1}, lo;
+          if constexpr (kTwoTerms) {
+            two_terms(p0, p1, hi, lo);
+            pl[t][kt >> 1][4 * (kt & 1) + i] = lo[0];
+            pl[t][kt >> 1][4 * (kt & 1) + i + 1] = lo[1];
+          }
+          pf[t][kt >> 1][4 * (kt & 1) + i] = hi[0];
+          pf[t][kt >> 1][4 * (kt & 1) + i + 1] = hi[1];
         }
       l[t] += sum;
     }

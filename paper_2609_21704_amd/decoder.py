@@ -345,7 +345,8 @@ class SpecDecoder:
     def prefill_packed(self, prompts, models=(True, False)):
         """prefill() of prompts given as one list of token ids per sequence (2 .. capacity of them), their tokens packed
         one after the other: no padding is computed, and prompts longer than a pass (PREFILL_ROWS rows over all
-        sequences) continue in the next."""
+        sequences) continue in the next.  The attention rounds its weights to one binary16 (prefill() to two), which is
+        up to 5 % on top of the rounding of its outputs."""
         if len(prompts) != self.B or any(not 2 <= len(p) <= self.capacity for p in prompts):
             raise ValueError("one prompt of 2 .. capacity tokens per sequence")
         if not all(self.w.stack.prefill_takes(draft, self.w.layers) for draft in models):

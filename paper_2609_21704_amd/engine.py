@@ -104,7 +104,8 @@ class Engine:
                  packed: bool = False):
         """`draft_cache`: "q4" keeps the drafts' caches in 4 bits.  `packed`: the
         prompts of a batch go through the models packed, without padding and
-        without copies of a prompt for idle rows.  `parent`: existing FP16 parent
+        without copies of a prompt for idle rows (`SpecDecoder.prefill_packed`, whose
+        attention rounds its weights to one binary16).  `parent`: existing FP16 parent
         weights (with one draft copy) to serve from instead of building new ones.  `timed`: synchronise around each
         batch's prefill and rounds and add their wall time to `seconds`."""
         self.cfg = cfg

@@ -78,3 +78,39 @@ def test_scores_past_whole_numbers_of_fp32(rows, past, fmt):
     want = vv[0, 0, top.indices[:, 0][clear]].double()
     # a weight's binary16, the output's
     assert bool(((out.view(-1, 128)[clear].double() - want).abs() <= want.abs() * (2.0 ** -10 + 2.0 ** -18) + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("rows", [1, 4])
+@pytest.mark.parametrize("past", [30, 5000])
+def test_weights_of_few_rows_to_two_terms(rows, past):
+    """Values whose weighted sum all but vanishes, so that the weights' roundings are seen beside the output's.  Scores are
+    one product each, exact in fp32; the scale, the exponent's argument (below 32: 2^-20), the exponential and the
+    sums come to 2^-18 of every weight, its two binary16 terms to 2^-20.  One binary16 would be 2^-12 off."""
+    hq, hkv, cap = 7, 1, (past + rows + 63) // 64 * 64
+    n = past + rows
+    g = torch.Generator(device=DEV).manual_seed(131)
+    k0 = torch.rand(n, generator=g, device=DEV) * 4 - 2
+    k0[past:] = -30  # the block's own keys: hardly any weight, the same sum for all rows
+    k0[:past][torch.arange(past, device=DEV) % (past // 30) != 0] = -30  # thirty keys have some
+    k = torch.zeros((1, hkv, cap, 128), dtype=F16, device=DEV)
+    k[0, 0, :n, 0] = k0.half()
+    q = torch.zeros((rows, hq, 128), dtype=F16, device=DEV)
+    q[..., 0] = 11.3125
+    sign = torch.where(torch.rand(n, generator=g, device=DEV) < 0.5, 1.0, -1.0).double()
+    w = torch.softmax(q[0, 0, 0].double() * k[0, 0, :past, 0].double() / math.sqrt(128), 0)
+    value = (sign * (torch.rand(n, generator=g, device=DEV) * 0.7 + 0.35)).half()
+    # some of the largest take away what is left of the sum, until it is about a rounding
+    for i in torch.argsort(w, descending=True)[:6].tolist():
+        left = float((w * value[:past].double()).sum() - w[i] * value[i].double())
+        value[i] = -left / float(w[i])
+    v = torch.zeros_like(k)
+    v[0, 0, :n] = value[:, None]
+    out = sq.sq_packed_attention_f16(q, k, v.transpose(2, 3).contiguous(), starts([rows]), ints([past]))
+    kd, vd = k[0, 0, :n, 0].double(), v[0, 0, :n].double()
+    s = q[0, 0, 0].double() * kd / math.sqrt(128)
+    s = s.masked_fill(torch.arange(n, device=DEV)[None] > past + torch.arange(rows, device=DEV)[:, None], -math.inf)
+    w = torch.softmax(s, 1)
+    ref, mag = w @ vd, w @ vd.abs()
+    bound = mag * (2.0 ** -18 + 2.0 ** -20) + n * 2.0 ** -32 * vd.abs().amax() + ref.abs() * 2.0 ** -11 + 2.0 ** -25
+    err = (out.double() - ref[:, None]).abs()
+    assert bool((err <= bound[:, None]).all()), float((err / bound[:, None]).max())
