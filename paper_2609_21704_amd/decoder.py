@@ -342,6 +342,10 @@ class SpecDecoder:
             w.stack.prefill_linear(draft, (l, "down"), t, h, sq.PREFILL_ADD)
         return True
 
+    def takes_packed(self, models=(True, False)) -> bool:
+        """Whether every projection of these models has a kernel for packed prompts."""
+        return all(self.w.stack.prefill_takes(draft, self.w.layers) for draft in models)
+
     def prefill_packed(self, prompts, models=(True, False)):
         """prefill() of prompts given as one list of token ids per sequence (2 .. capacity of them), their tokens packed
         one after the other: no padding is computed, and prompts longer than a pass (PREFILL_ROWS rows over all
@@ -349,7 +353,7 @@ class SpecDecoder:
         up to 5 % on top of the rounding of its outputs."""
         if len(prompts) != self.B or any(not 2 <= len(p) <= self.capacity for p in prompts):
             raise ValueError("one prompt of 2 .. capacity tokens per sequence")
-        if not all(self.w.stack.prefill_takes(draft, self.w.layers) for draft in models):
+        if not self.takes_packed(models):
             raise ValueError("a projection of this model has no kernel for packed prompts: use prefill()")
         prompts = [list(p) for p in prompts for _ in range(self.c)]
         i32 = torch.int32
@@ -526,6 +530,9 @@ class DirectDecoder(SpecDecoder):
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(False,), lengths=None):
         super().prefill(prompt, chunk, models=models, lengths=lengths)
+
+    def takes_packed(self, models=(False,)) -> bool:
+        return super().takes_packed(models)
 
     def prefill_packed(self, prompts, models=(False,)):
         super().prefill_packed(prompts, models=models)

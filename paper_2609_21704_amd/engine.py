@@ -105,7 +105,8 @@ class Engine:
         """`draft_cache`: "q4" keeps the drafts' caches in 4 bits.  `packed`: the
         prompts of a batch go through the models packed, without padding and
         without copies of a prompt for idle rows (`SpecDecoder.prefill_packed`, whose
-        attention rounds its weights to one binary16).  `parent`: existing FP16 parent
+        attention rounds its weights to one binary16); padded where a projection
+        has no kernel for them.  `parent`: existing FP16 parent
         weights (with one draft copy) to serve from instead of building new ones.  `timed`: synchronise around each
         batch's prefill and rounds and add their wall time to `seconds`."""
         self.cfg = cfg
@@ -197,7 +198,7 @@ class Engine:
     def _run_batch(self, variant: str, toks: list, max_new: int) -> list:
         dec = self.decoder(variant)
         n = len(toks)
-        if self.packed:
+        if self.packed and dec.takes_packed():
             t0 = self._clock()
             dec.prefill_packed(toks + [toks[0][:2]] * (self.batch - n))  # idle rows: two tokens of the first prompt
         else:

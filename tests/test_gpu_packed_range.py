@@ -6,6 +6,9 @@ import pytest
 import torch
 
 import paper_2609_21704_amd as sq
+from paper_2609_21704_amd.configs import Config
+from paper_2609_21704_amd.decoder import DecoderWeights, SpecDecoder
+from paper_2609_21704_amd.engine import Engine, weight_bytes
 from test_gpu_packed import check_attention, ints, normal, pack_q4, starts, values_q4
 
 pytestmark = pytest.mark.gpu
@@ -114,3 +117,20 @@ def test_weights_of_few_rows_to_two_terms(rows, past):
     bound = mag * (2.0 ** -18 + 2.0 ** -20) + n * 2.0 ** -32 * vd.abs().amax() + ref.abs() * 2.0 ** -11 + 2.0 ** -25
     err = (out.double() - ref[:, None]).abs()
     assert bool((err <= bound[:, None]).all()), float((err / bound[:, None]).max())
+
+
+def test_engine_pads_where_no_projection_takes_packed_prompts():
+    """Rows of 1184 elements, which no projection of many rows takes: the engine's packed prompts go padded, in blocks."""
+    cfg = Config(0, "odd", 2, 512, 1184, 4, 2, 1000, "fp8", 2, 2, 5)
+    tokens = []
+    for packed in (True, False):
+        w = DecoderWeights(cfg, DEV, variant="fp8")
+        eng = Engine(cfg, DEV, batch=2, capacity=128, temperature=0.0, parent=w, packed=packed,
+                     free_bytes=int(weight_bytes(cfg)["f16"] * 1.4) + (1 << 20))
+        assert eng.plan["resident"] == ["f16"] and not eng.decoder("f16").takes_packed()
+        tokens.append([r.tokens for r in eng.generate([[5, 6, 7], list(range(40)), [9, 1]], 6)])
+    assert tokens[0] == tokens[1]
+    d = SpecDecoder(w, batch=2, k=2, capacity=128)
+    assert not d.takes_packed()
+    with pytest.raises(ValueError, match="use prefill"):
+        d.prefill_packed([[1, 2], [3, 4]])
