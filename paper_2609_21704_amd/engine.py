@@ -52,6 +52,8 @@ def weight_bytes(cfg: Config, layers: int | None = None) -> dict:
 def cache_bytes(cfg: Config, layers: int, rows: int, capacity: int, fmt: str = "f16") -> int:
     """Keys and values of one model's cache, per layer, row, kv head and position: fp16, or ("q4") 4-bit codes with a
     scale and a zero per 64."""
+    if fmt not in ("f16", "q4"):
+        raise ValueError("a cache is 'f16' or 'q4'")
     return 2 * layers * rows * cfg.kv_heads * capacity * (HEAD_DIM * 2 if fmt == "f16" else HEAD_DIM // 2 + 8)
 
 
@@ -116,6 +118,8 @@ class Engine:
         self.router = router or Router()
         self.seed = cfg.seed if seed is None else seed
         L = cfg.layers if layers is None else layers
+        if draft_cache not in ("f16", "q4"):
+            raise ValueError("draft_cache must be 'f16' or 'q4'")
         if free_bytes is None:
             free_bytes = torch.cuda.mem_get_info(self.device)[0]
         if draft_cache == "q4" and chains != 1:
