@@ -13,8 +13,15 @@
  *
  * Packed rows.  row_start [b + 1] (device, int32): sequence s has the rows
  * row_start[s] .. row_start[s + 1] - 1 of `rows` rows, none where the two are equal.
- * max_rows is a bound on one sequence's rows, known on the host (it chooses the
- * kernels).  Row row_start[s] + j is at position pos_base[s] + pos_offset + j.
+ * max_rows is a bound on one sequence's rows, known on the host.  It chooses the
+ * attention's kernel, and with the rows whether keys are split, for all sequences
+ * alike: single tokens after long caches packed with a prompt get the prompt's, one
+ * workgroup each (16 tokens after 31000 positions and a prompt of 512 rows, 28 query
+ * heads on 4: 557 us, 751 over 4-bit entries).  Two calls over the same packed rows
+ * take 196 and 78: the tokens' sequences first, then one call whose row_start is
+ * clipped to at most their number of rows, with max_rows 1, and one whose row_start
+ * is clipped to at least that (the other sequences are empty, their rows are left).
+ * Row row_start[s] + j is at position pos_base[s] + pos_offset + j.
  * Rows before the first and after the last sequence's are left as they were.
  * row_start NULL: max_rows rows for every sequence (rows = b max_rows).
  * Entries of row_start that decrease or lie outside [0, rows], or a sequence of more

@@ -683,7 +683,9 @@ def sq_prefill_attention_f16(q, k_cache, v_cache, pos_base, pos_offset: int, row
 
 # ------------------------------------------------- packed rows, 4-bit cache
 # The calls of include/specquant_packed.h.  row_start: int32 [b + 1] on the GPU, or None for max_rows rows of every
-# sequence; max_rows: a bound on one sequence's rows (by default all rows, which suits one sequence or long prompts).
+# sequence; max_rows: a bound on one sequence's rows, which chooses the kernels for all of them (by default all rows, which
+# suits one sequence or long prompts: for blocks and single tokens give theirs, and beside prompts make two calls, with
+# row_start.clamp(max=r) and row_start.clamp(min=r), r the first prompt's row).
 
 
 def _launch(entry: str, tensors, *args):

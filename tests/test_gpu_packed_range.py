@@ -134,3 +134,49 @@ def test_engine_pads_where_no_projection_takes_packed_prompts():
     assert not d.takes_packed()
     with pytest.raises(ValueError, match="use prefill"):
         d.prefill_packed([[1, 2], [3, 4]])
+
+
+# (rows, past) of more than 64 sequences on one kv head whose keys are split: single tokens with long caches below and above
+# the 64th, empty ones between; few sequences with rows, of up to 70, among a hundred
+MANY = [[((i % 5 != 2) * (1 + (i == 90)), 1100 * (i // 3 % 9) if i in (3, 70, 90, 119) else i % 60) for i in range(120)],
+        [((40, 3000) if i == 2 else (33, 5000) if i == 66 else (70, 2000) if i == 99 else (0, 17 * i)) for i in range(100)]]
+
+
+@pytest.mark.parametrize("seqs", MANY)
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_split_keys_of_many_sequences(seqs, fmt):
+    hq, hkv = 8, 1
+    cap = (max(n + p for n, p in seqs) + 63) // 64 * 64
+    b, rows, most = len(seqs), sum(n for n, _ in seqs), max(n for n, _ in seqs)
+    q, k, v = normal((rows, hq, 128), 141, std=1.3), normal((b, hkv, cap, 128), 142), normal((b, hkv, cap, 128), 143)
+    args = starts([n for n, _ in seqs]), ints([p for _, p in seqs])
+    if fmt == "f16":
+        out = sq.sq_packed_attention_f16(q, k, v.transpose(2, 3).contiguous(), *args, max_rows=most)
+    else:
+        cache = pack_q4(k, v)
+        out = sq.sq_packed_attention_q4(q, *cache, *args, max_rows=most)
+        k, v = values_q4(cache)
+    check_attention(out, q, k, v, seqs)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_prompts_and_single_tokens_in_one_call(fmt):
+    """A prompt packed beside single tokens after long caches; and the same in two calls over the same packed rows, whose
+    row_start leaves the other sequences empty, each with a bound of its own."""
+    hq, hkv, tokens = 28, 4, 9
+    seqs = [(1, 700 + 450 * i) for i in range(tokens)] + [(500, 0), (60, 333)]
+    cap = 4352
+    b, rows = len(seqs), sum(n for n, _ in seqs)
+    q, k, v = normal((rows, hq, 128), 151, std=1.3), normal((b, hkv, cap, 128), 152), normal((b, hkv, cap, 128), 153)
+    start, pos = starts([n for n, _ in seqs]), ints([p for _, p in seqs])
+    if fmt == "f16":
+        cache, attn = (k, v.transpose(2, 3).contiguous()), sq.sq_packed_attention_f16
+    else:
+        cache, attn = pack_q4(k, v), sq.sq_packed_attention_q4
+        k, v = values_q4(cache)
+    check_attention(attn(q, *cache, start, pos, max_rows=500), q, k, v, seqs)
+    out = torch.full_like(q, 9.0)
+    attn(q, *cache, start.clamp(max=tokens), pos, max_rows=1, out=out)
+    assert bool((out[tokens:] == 9).all())
+    attn(q, *cache, start.clamp(min=tokens), pos, max_rows=500, out=out)
+    check_attention(out, q, k, v, seqs)
