@@ -1256,8 +1256,10 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound, bool q4
       return pr.start ? ((int64_t)pr.rows * G + b * (tq - 1)) / tq
                       : (int64_t)pr.b * (((int64_t)pr.max_rows * G + tq - 1) / tq);
     };
-    // Tiles of 256 queries read the keys half as often, and leave more CUs idle at the end: one prompt of 12000 rows 1015 us
-    // for 1028 with 128 (28 query heads on 4), of 4000 188 for 180 (40 on 8), of 2000 60 for 53, 40 of 200 52 for 45.
+    // Tiles of 256 queries read the keys (and dequantise 4-bit ones) half as often, and leave more CUs idle at the end.  256
+    // and 128 over fp16, then 4-bit entries, 28 query heads on 4: one prompt of 12000 rows 996 and 1000 us, 1090 and 1122;
+    // eight of 2000 273 and 275, 293 and 308; sixteen of 1000 173 and 171, 188 and 186; one of 2000 55.7 and 49.2, 69.7 and
+    // 58.9; forty of 200 49.9 and 46.9, both formats; four of 2000, 40 heads on 8, 204 and 200, 214 and 225.
     p.tq = tiles(256) * hkv >= 1536 ? 256 : 128;
     p.tiles = (int)tiles(p.tq);
     // Split: one sequence of 40 rows after 4000 positions 20.6 us for 76.  Tiles on half of the CUs or more stay whole.
@@ -1307,9 +1309,14 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     a.part_ml = reinterpret_cast<float2*>(a.part_o + queries * kHd);
   }
   const dim3 grid((unsigned)(units * hkv));
-  // Where not all tiles run at once: prompts of 400, 800 .. 2800 rows 189 us for 209, four of 1171 57.7 for 62.4, 29 of 64 ..
-  // 1856 350 for 341 (the level of a tile is found by search).
-  a.longest = !p.few && (int64_t)units * hkv > (p.tq == 256 ? 256 : 512);
+  // Longest first where not all tiles run at once, for a few (sequence, kv head) pairs: tiles of more of them side by side
+  // no longer find their keys in the L2s, and a tile's level is found by search, which one sequence (in this order as it
+  // is) need not pay.  fp16 and 4-bit entries, 28 heads on 4: four prompts of 1171 rows 58.9 us for 61.2 and 63.9 for 69.2,
+  // seven of 400, 800 .. 2800 209 for 213 and 223 for 232, eight of up to 2500 42.7 for 45.1 and 81.4 for 95.8; eight of 700
+  // 54.3 for 52.1 and 55.5 for 57.9; ten of up to 2500 110 for 105 and 95.0 for 97.1; 29 of 64 .. 1856 360 for 350 and 374 for
+  // 366; 40 heads on 8, four of up to 3000 72.3 for 75.6 and 128.4 for 126.5, eight 282 for 275 and 220 for 217.
+  const int64_t seqs = pr.b < pr.rows ? pr.b : pr.rows;
+  a.longest = !p.few && seqs > 1 && seqs * hkv <= 32 && (int64_t)units * hkv > (p.tq == 256 ? 256 : 512);
   if (p.few) {
     if (q4)
       launch_few<true>(p, grid, pr, a, stream);
