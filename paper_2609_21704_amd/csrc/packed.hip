@@ -5,8 +5,8 @@
 //                              positions, [64 bytes][64 positions]
 //   packed_read_kernel         4-bit entries of the packed rows' positions as fp16 rows
 // All three are bound by memory: fp32 projections in, 16-bit queries and the entries out.  fp16, 13128 rows of 40 heads on
-// 8 (565 MB): 128 us, 4.4 TB/s; a copy of 1 GiB reaches 4.8.  4-bit, 3091 rows of 28 heads on 4 (89 MB with the read): 18.2 us
-// and 5.4 us for the read.  A few rows: 5.4 us, the launch, the list of tiles and two dependent loads.
+// 8 (565 MB): 128 us, 4.4 TB/s; a copy of 1 GiB reaches 4.8.  4-bit, 3091 rows of 28 heads on 4 (89 MB with the read): 20.2 us
+// and 5.0 us for the read.  A few rows: 5.5 us, the launch, the list of tiles and two dependent loads.
 #include "sq_internal.hpp"
 #include "sq_packed.hpp"
 #include "sq_quant.hpp"

@@ -389,8 +389,9 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
 // A step's keys are loaded while the step before takes its values, and the other way round, each into the registers that
 // were just used (fp16 and two tiles: the registers hold only one of the two, loaded when its turn comes).  Up to
 // 32 queries: all eight wavefronts take keys; up to 64 (4-bit entries): half of them the first 32, half the rest, over the
-// same keys.  Bound by the cache's bytes: 16 tokens after 13k to 31k positions (28 heads on 4, 207 MB of 4-bit entries)
-// 40.5 us and 4.8 for the merge, 5.1 TB/s without it, where a large copy reaches 4.8; a few sequences by latency: the plan
+// same keys.  fp16 entries: bound by the cache's bytes, 64 tokens after 2000 positions (28 heads on 4, 262 MB) 54.9 us, 4.8 TB/s.
+// 4-bit: by reads and arithmetic together, 16 tokens after 13k to 31k positions (207 MB, three caches in turn) 44.0 us and 4.8
+// for the merge, 4.7 TB/s without it where a streaming read reaches 6.2 to 6.5.  A few sequences by latency: the plan
 // 1 us, the first loads 2, a step of 64 keys 0.7, the meeting in LDS 1, and a CU takes in fp16 entries at about 60 GB/s.
 constexpr int kFewWaves = 8;
 

@@ -180,3 +180,19 @@ def test_prompts_and_single_tokens_in_one_call(fmt):
     assert bool((out[tokens:] == 9).all())
     attn(q, *cache, start.clamp(min=tokens), pos, max_rows=500, out=out)
     check_attention(out, q, k, v, seqs)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_tiles_in_the_order_of_their_keys(fmt):
+    """Eight sequences whose tiles do not run at once, two of them empty, some after cached positions: every row is there."""
+    hq, hkv, seqs = 28, 4, [(1500, 0), (0, 900), (330, 40), (900, 0), (611, 200), (1203, 64), (0, 0), (1, 1700)]
+    cap, b, rows = 1728, len(seqs), sum(n for n, _ in seqs)
+    q, k, v = normal((rows, hq, 128), 161, std=1.3), normal((b, hkv, cap, 128), 162), normal((b, hkv, cap, 128), 163)
+    args = starts([n for n, _ in seqs]), ints([p for _, p in seqs])
+    if fmt == "f16":
+        out = sq.sq_packed_attention_f16(q, k, v.transpose(2, 3).contiguous(), *args, max_rows=1500)
+    else:
+        cache = pack_q4(k, v)
+        out = sq.sq_packed_attention_q4(q, *cache, *args, max_rows=1500)
+        k, v = values_q4(cache)
+    check_attention(out, q, k, v, seqs)
