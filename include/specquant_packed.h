@@ -92,7 +92,8 @@ sq_status sq_packed_kv_read_q4(const uint8_t* k_codes, const uint16_t* k_scales,
  * sums and outputs in fp32, a weight rounded for its product with the value to two
  * fp16 terms (2^-20 of it) where max_rows hq / hkv <= 32, to one (2^-11) above.
  * q, out [rows][hq][128] fp16.  A row reads its sequence's positions 0 .. its own, which must hold written entries; what is at later positions does
- * not matter (NaN and infinities included).  A row at a position outside [0, len_bound)
+ * not matter (NaN and infinities included); an infinite value it reads with a weight
+ * below 2^-31 of its largest may give NaN.  A row at a position outside [0, len_bound)
  * gets NaN.  Few workgroups for the chip: the keys are split over up to 256
  * workgroups, whose sums take at most 17 MiB of the library workspace.
  * capacity <= 2^28. */

@@ -70,10 +70,12 @@ __device__ __forceinline__ float rescale(float from, float to) { return exp2_fas
 __device__ __forceinline__ bool far_reference(float m) { return __any(fabsf(m) > kFar && m != kNoMax); }
 __device__ __forceinline__ float near_reference(float m) { return __builtin_fmaf(m, -kScale, kShift); }
 
-// Two weights as two binary16 terms each: truncated, and what that leaves (exact in fp32), truncated.
+// Two weights as two binary16 terms each: truncated, and what that leaves (exact in fp32), truncated.  Where it leaves
+// nothing of a weight, the second term is the least there is: a zero would make an infinite value NaN.
 __device__ __forceinline__ void two_terms(float p0, float p1, half2_t& hi, half2_t& lo) {
   hi = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0, p1));
   lo = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0 - (float)hi[0], p1 - (float)hi[1]));
+  lo = __builtin_elementwise_max(lo, __builtin_elementwise_min(hi, half2_t{(half_t)0x1p-24f, (half_t)0x1p-24f}));
 }
 
 // How the work is laid over workgroups.  A sequence's queries are `tiles` tiles, each over the sequence's `steps` steps of

@@ -196,3 +196,36 @@ def test_tiles_in_the_order_of_their_keys(fmt):
         out = sq.sq_packed_attention_q4(q, *cache, *args, max_rows=1500)
         k, v = values_q4(cache)
     check_attention(out, q, k, v, seqs)
+
+
+@pytest.mark.parametrize("rows,past", [(1, 90), (4, 200), (40, 300)])
+@pytest.mark.parametrize("fmt", ["f16", "q4"])
+def test_infinite_values_that_every_row_reads(rows, past, fmt):
+    """An infinite value below every row's position, at the key of the largest score (a weight that is one binary16 alone)
+    and at others: the outputs are infinite in its dimension, and nowhere else."""
+    hq, hkv, cap = 7, 1, 384
+    q, k, v = normal((rows, hq, 128), 171), normal((1, hkv, cap, 128), 172), normal((1, hkv, cap, 128), 173)
+    k[..., 0] = 0
+    q[..., 0] = 8.0
+    k[0, 0, 7, 0] = 10.0
+    for key in (7, 3):
+        if fmt == "f16":
+            args = starts([rows]), ints([past])
+            clean = sq.sq_packed_attention_f16(q, k, v.transpose(2, 3).contiguous(), *args)
+            w = v.clone()
+            w[0, 0, key, 5], w[0, 0, key, 70] = math.inf, -math.inf
+            out = sq.sq_packed_attention_f16(q, k, w.transpose(2, 3).contiguous(), *args)
+            hit = torch.zeros(128, device=DEV)
+            hit[5], hit[70] = math.inf, -math.inf
+        else:
+            cache = pack_q4(k, v)
+            clean = sq.sq_packed_attention_q4(q, *cache, starts([rows]), ints([past]))
+            vs = cache[3].clone()
+            vs[0, 0, 0, 2, key] = math.inf  # elements 64 .. 127 of one value: a zero of 7.5 lies between codes
+            vs[0, 0, 0, 3, key] = 7.5
+            out = sq.sq_packed_attention_q4(q, *cache[:3], vs, starts([rows]), ints([past]))
+            hit = torch.zeros(128, device=DEV)
+            c = cache[2][0, 0, 0, :, (key & ~3) | ((key & 1) << 1) | ((key >> 1) & 1)] >> 4
+            hit[64:] = torch.where(c > 7, math.inf, -math.inf)
+        want = torch.where(hit == 0, clean.float(), hit.expand_as(clean))
+        assert torch.equal(out.float(), want), key
