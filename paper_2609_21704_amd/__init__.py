@@ -24,6 +24,16 @@ from ._lib import (  # noqa: F401
     sq_packed_kv_read_q4,
     sq_packed_rope_kv_f16,
     sq_packed_rope_kv_q4,
+    sq_page_copy,
+    sq_paged_attention_f16,
+    sq_paged_attention_q4,
+    sq_paged_kv_read_q4,
+    sq_paged_rope_kv_f16,
+    sq_paged_rope_kv_q4,
+    sq_pages_compact,
+    sq_pages_fork,
+    sq_pages_reserve,
+    sq_pages_trim,
     sq_qgemv_w4a16,
     sq_qgemv_w4a16_acc,
     sq_qgemv_w4a16_rmsnorm,

@@ -81,6 +81,18 @@ def load() -> ctypes.CDLL:
             "sq_packed_kv_read_q4": ([P, P, P, P, P, I32, I64, I64, I32, P, I32, I64, I64, P, P, P], S),
             "sq_packed_attention_f16": ([P, P, P, P, I32, I64, I64, I32, I32, P, I32, I64, I64, P, P], S),
             "sq_packed_attention_q4": ([P, P, P, P, P, P, I32, I64, I64, I32, I32, P, I32, I64, I64, P, P], S),
+            "sq_pages_reserve": ([P, P, P, I32, I64, I64, P, I32, P, P], S),
+            "sq_pages_trim": ([P, P, P, I32, I64, I64, P, P, P], S),
+            "sq_pages_fork": ([P, P, P, I32, I64, I64, P, P, P, I32, P, P, P, P, P], S),
+            "sq_pages_compact": ([P, P, P, I32, I64, I64, P, P, P, P, P, P], S),
+            "sq_page_copy": ([P, I32, I64, I64, P, P, P, I64, P, P], S),
+            "sq_paged_rope_kv_f16": ([P, P, P, I32, I64, I64, I32, I32, P, I32, I64, P, I64, I64, ctypes.c_double, P, P, P,
+                                      P, P], S),
+            "sq_paged_rope_kv_q4": ([P, P, P, I32, I64, I64, I32, I32, P, I32, I64, P, I64, I64, ctypes.c_double, P, P, P,
+                                     P, P, P, P], S),
+            "sq_paged_kv_read_q4": ([P, P, P, P, P, I64, I64, P, I32, I64, I64, I32, P, I32, I64, P, P, P], S),
+            "sq_paged_attention_f16": ([P, P, P, P, I64, I64, P, I32, I64, I64, I32, I32, P, I32, I64, P, P], S),
+            "sq_paged_attention_q4": ([P, P, P, P, P, P, I64, I64, P, I32, I64, I64, I32, I32, P, I32, I64, P, P], S),
             "sq_kv_adopt_f16": ([P, P, I32, I32, I32, I32, I64, P, P, P, I32, I32, P], S),
             "sq_spec_commit_multi": ([P, P, P, P, I32, I32, I32, P, P, P, P, I64, P, P, P], S),
         }
@@ -103,6 +115,7 @@ EXPORTED = ("sq_abi_version", "sq_status_str", "sq_quantize_int4_g128", "sq_quan
 # device status bits (SQ_DEV_* of include/specquant.h)
 DEV_BAD_TOKEN, DEV_BAD_POS, DEV_OVERFLOW, DEV_NO_DIST = 1, 2, 4, 8
 DEV_BAD_ROWS = 16  # of include/specquant_packed.h
+DEV_NO_PAGES, DEV_BAD_PAGE, DEV_BAD_FORK = 32, 64, 128  # of include/specquant_paged.h
 
 
 def _ptr(t):
@@ -820,3 +833,185 @@ def sq_packed_attention_q4(q, k_codes, k_scales, v_codes, v_scales, row_start, p
     cache = (k_codes, k_scales, v_codes, v_scales)
     return _packed_attention("sq_packed_attention_q4", q, cache, _q4_cache(*cache), row_start, pos_base, max_rows,
                              pos_offset, len_bound, out)
+
+
+# ------------------------------------------------------------- paged caches
+# The calls of include/specquant_paged.h.  table: int32 [b][width] page ids (-1 past the held ones), held: int32 [b],
+# refs: int32 [pages]; the arrays of a layer's pool start with [pages][hkv].
+PAGE = 64  # positions of a page
+
+
+def _page_state(table, held, refs):
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise ValueError("table must be int32 [b][width]")
+    _expect(held, torch.int32, (table.shape[0],), "held")
+    if refs.dtype != torch.int32 or refs.dim() != 1:
+        raise ValueError("refs must be int32 [pages]")
+    return (table.data_ptr(), held.data_ptr(), refs.data_ptr(), table.shape[0], table.shape[1], refs.shape[0])
+
+
+def _status_word(status):
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise ValueError("status must be int32")
+    return _ptr(status)
+
+
+def _ints(t, n: int, name: str):
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] < n:
+        raise ValueError(f"{name} must be int32 with at least {n} elements")
+    return t.data_ptr()
+
+
+def sq_pages_reserve(table, held, refs, pos_base, ahead: int = 1, status=None):
+    """Pages for the positions below pos_base[s] + ahead of every row, lowest free ids first, as long as they last."""
+    state = _page_state(table, held, refs)
+    _expect(pos_base, torch.int32, (table.shape[0],), "pos_base")
+    _launch("sq_pages_reserve", (table, held, refs, pos_base, status), *state, pos_base.data_ptr(), ahead,
+            _status_word(status))
+
+
+def sq_pages_trim(table, held, refs, keep, status=None):
+    """Give back the pages past position keep[s] of every row (0: all; below 0: the row is left alone)."""
+    state = _page_state(table, held, refs)
+    _expect(keep, torch.int32, (table.shape[0],), "keep")
+    _launch("sq_pages_trim", (table, held, refs, keep, status), *state, keep.data_ptr(), _status_word(status))
+
+
+def sq_pages_fork(table, held, refs, parent, child, length, src, dst, count, status=None):
+    """Rows child[i] share the pages of the first length[i] positions of rows parent[i]; src, dst, count: the partly filled
+    last pages, for sq_page_copy."""
+    state = _page_state(table, held, refs)
+    n = parent.shape[0]
+    args = [_ints(t, n, name) for t, name in ((parent, "parent"), (child, "child"), (length, "length"))]
+    args += [n, _ints(src, n, "src"), _ints(dst, n, "dst"), _ints(count, 1, "count")]
+    _launch("sq_pages_fork", (table, held, refs, parent, child, length, src, dst, count, status), *state, *args,
+            _status_word(status))
+
+
+def sq_pages_compact(table, held, refs, src, dst, count, used, status=None):
+    """Move the used pages to the ids 0 .. used[0] - 1 in refs and table; src, dst (pages / 2 at least), count: the moves,
+    for sq_page_copy."""
+    state = _page_state(table, held, refs)
+    half = refs.shape[0] // 2
+    _launch("sq_pages_compact", (table, held, refs, src, dst, count, used, status), *state, _ints(src, half, "src"),
+            _ints(dst, half, "dst"), _ints(count, 1, "count"), _ints(used, 1, "used"), _status_word(status))
+
+
+def sq_page_copy(pool, src, dst, count, status=None):
+    """Page dst[i] = page src[i] for i < count[0], in every layer of pool [layers][pages][..] (any type)."""
+    if pool.dim() < 3:
+        raise ValueError("pool must be [layers][pages][..]")
+    layers, pages = pool.shape[:2]
+    n = min(src.shape[0], dst.shape[0], 1 << 20)
+    _launch("sq_page_copy", (pool, src, dst, count, status), pool.data_ptr(), layers, pages,
+            pool[0, 0].numel() * pool.element_size(), _ints(src, n, "src"), _ints(dst, n, "dst"), _ints(count, 1, "count"),
+            n, _status_word(status))
+
+
+def _pool_f16(k_pages, v_pages):
+    """(hkv, pages) of a layer's fp16 pool."""
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages must be float16 [pages][hkv][64][128]")
+    pages, hkv = k_pages.shape[:2]
+    _expect(k_pages, torch.float16, (pages, hkv, PAGE, HEAD_DIM), "k_pages")
+    _expect(v_pages, torch.float16, (pages, hkv, HEAD_DIM, PAGE), "v_pages")
+    return hkv, pages
+
+
+def _pool_q4(k_codes, k_scales, v_codes, v_scales):
+    if k_codes.dim() != 4:
+        raise ValueError("k_codes must be uint8 [pages][hkv][64][64]")
+    pages, hkv = k_codes.shape[:2]
+    _expect(k_codes, torch.uint8, (pages, hkv, PAGE, HEAD_DIM // 2), "k_codes")
+    _expect(k_scales, torch.float16, (pages, hkv, PAGE, 4), "k_scales")
+    _expect(v_codes, torch.uint8, (pages, hkv, HEAD_DIM // 2, PAGE), "v_codes")
+    _expect(v_scales, torch.float16, (pages, hkv, 4, PAGE), "v_scales")
+    return hkv, pages
+
+
+def _table_dims(table):
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise ValueError("table must be int32 [b][width]")
+    return table.shape[0], table.shape[1]
+
+
+def _paged_rope(entry, qkv, bias, row_start, pos_base, hq, cache, dims, table, max_rows, pos_offset, len_bound, theta,
+                q_out, status):
+    (hkv, pages), (b, width) = dims, _table_dims(table)
+    nh = hq + 2 * hkv
+    if qkv.dtype != torch.float32 or qkv.numel() % (nh * HEAD_DIM):
+        raise ValueError("qkv must be float32 [rows][(hq + 2 hkv) * 128]")
+    rows = qkv.numel() // (nh * HEAD_DIM)
+    max_rows, len_bound = _packed(b, width * PAGE, rows, row_start, pos_base, max_rows, len_bound)
+    q_out = torch.empty((rows, hq, HEAD_DIM), dtype=torch.float16, device=qkv.device) if q_out is None else q_out
+    _expect(q_out, torch.float16, (rows, hq, HEAD_DIM), "q_out")
+    if bias is not None:
+        _expect(bias, torch.float16, (nh * HEAD_DIM,), "bias")
+    _launch(entry, (qkv, bias, row_start, pos_base, table, q_out, *cache, status), qkv.data_ptr(), _ptr(bias),
+            _ptr(row_start), b, rows, max_rows, hq, hkv, pos_base.data_ptr(), pos_offset, len_bound, table.data_ptr(),
+            width, pages, theta, q_out.data_ptr(), *[c.data_ptr() for c in cache], _status_word(status))
+    return q_out
+
+
+def sq_paged_rope_kv_f16(qkv, bias, row_start, pos_base, hq: int, k_pages, v_pages, table, max_rows: int | None = None,
+                         pos_offset: int = 0, len_bound: int | None = None, theta: float = 1e6, q_out=None, status=None):
+    """sq_packed_rope_kv_f16 into pages (k_pages fp16 [pages][hkv][64][128], v_pages fp16 [pages][hkv][128][64])."""
+    return _paged_rope("sq_paged_rope_kv_f16", qkv, bias, row_start, pos_base, hq, (k_pages, v_pages),
+                       _pool_f16(k_pages, v_pages), table, max_rows, pos_offset, len_bound, theta, q_out, status)
+
+
+def sq_paged_rope_kv_q4(qkv, bias, row_start, pos_base, hq: int, k_codes, k_scales, v_codes, v_scales, table,
+                        max_rows: int | None = None, pos_offset: int = 0, len_bound: int | None = None,
+                        theta: float = 1e6, q_out=None, status=None):
+    """The same into 4-bit pages (k_codes, v_codes u8 [pages][hkv][64][64], k_scales fp16 [pages][hkv][64][4], v_scales
+    fp16 [pages][hkv][4][64])."""
+    cache = (k_codes, k_scales, v_codes, v_scales)
+    return _paged_rope("sq_paged_rope_kv_q4", qkv, bias, row_start, pos_base, hq, cache, _pool_q4(*cache), table, max_rows,
+                       pos_offset, len_bound, theta, q_out, status)
+
+
+def sq_paged_kv_read_q4(k_codes, k_scales, v_codes, v_scales, table, row_start, pos_base, rows: int,
+                        max_rows: int | None = None, pos_offset: int = 0, len_bound: int | None = None, k_out=None,
+                        v_out=None):
+    """(k_out, v_out) [rows][hkv][128] fp16: what the 4-bit entries at the packed rows' positions stand for."""
+    cache = (k_codes, k_scales, v_codes, v_scales)
+    (hkv, pages), (b, width) = _pool_q4(*cache), _table_dims(table)
+    max_rows, len_bound = _packed(b, width * PAGE, rows, row_start, pos_base, max_rows, len_bound)
+    shape = (rows, hkv, HEAD_DIM)
+    k_out = torch.empty(shape, dtype=torch.float16, device=k_codes.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=torch.float16, device=k_codes.device) if v_out is None else v_out
+    _expect(k_out, torch.float16, shape, "k_out")
+    _expect(v_out, torch.float16, shape, "v_out")
+    _launch("sq_paged_kv_read_q4", (*cache, table, row_start, pos_base, k_out, v_out), *[c.data_ptr() for c in cache],
+            table.data_ptr(), width, pages, _ptr(row_start), b, rows, max_rows, hkv, pos_base.data_ptr(), pos_offset,
+            len_bound, k_out.data_ptr(), v_out.data_ptr())
+    return k_out, v_out
+
+
+def _paged_attention(entry, q, cache, dims, table, row_start, pos_base, max_rows, pos_offset, len_bound, out):
+    (hkv, pages), (b, width) = dims, _table_dims(table)
+    if q.dtype != torch.float16 or q.dim() != 3 or q.shape[2] != HEAD_DIM:
+        raise ValueError("q must be float16 [rows][hq][128]")
+    rows, hq, _ = q.shape
+    max_rows, len_bound = _packed(b, width * PAGE, rows, row_start, pos_base, max_rows, len_bound)
+    out = torch.empty((rows, hq, HEAD_DIM), dtype=torch.float16, device=q.device) if out is None else out
+    _expect(out, torch.float16, (rows, hq, HEAD_DIM), "out")
+    _launch(entry, (q, *cache, table, row_start, pos_base, out), q.data_ptr(), *[c.data_ptr() for c in cache],
+            table.data_ptr(), width, pages, _ptr(row_start), b, rows, max_rows, hq, hkv, pos_base.data_ptr(), pos_offset,
+            len_bound, out.data_ptr())
+    return out
+
+
+def sq_paged_attention_f16(q, k_pages, v_pages, table, row_start, pos_base, max_rows: int | None = None,
+                           pos_offset: int = 0, len_bound: int | None = None, out=None):
+    """Causal GQA attention of packed rows over pages; returns out [rows][hq][128] fp16."""
+    return _paged_attention("sq_paged_attention_f16", q, (k_pages, v_pages), _pool_f16(k_pages, v_pages), table, row_start,
+                            pos_base, max_rows, pos_offset, len_bound, out)
+
+
+def sq_paged_attention_q4(q, k_codes, k_scales, v_codes, v_scales, table, row_start, pos_base,
+                          max_rows: int | None = None, pos_offset: int = 0, len_bound: int | None = None, out=None):
+    """sq_paged_attention_f16 over 4-bit pages."""
+    cache = (k_codes, k_scales, v_codes, v_scales)
+    return _paged_attention("sq_paged_attention_q4", q, cache, _pool_q4(*cache), table, row_start, pos_base, max_rows,
+                            pos_offset, len_bound, out)

@@ -13,7 +13,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libspecquant.so")
 
 SOURCES = ["quant.hip", "gemv.hip", "gemm.hip", "linear.hip", "prefill.hip", "accept.hip", "decoder.hip", "packed.hip",
-           "packed_attn.hip", "probe.hip", "abi.cpp", "abi_prefill.cpp", "abi_packed.cpp"]
+           "packed_attn.hip", "pages.hip", "probe.hip", "abi.cpp", "abi_prefill.cpp", "abi_packed.cpp", "abi_paged.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

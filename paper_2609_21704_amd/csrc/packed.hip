@@ -15,7 +15,7 @@
 namespace sq {
 namespace {
 
-constexpr int32_t kBadPos = 2, kBadRows = 16;  // the SQ_DEV_* values of the C headers
+constexpr int32_t kBadPos = 2, kBadRows = 16, kBadPage = 64;  // the SQ_DEV_* values of the C headers
 
 // A workgroup takes the rows of one sequence at 16 positions that start at a multiple of 16 (so that a run of values
 // is whole words of memory), and the heads h with h % gridDim.y == blockIdx.y.
@@ -103,6 +103,11 @@ __device__ __forceinline__ Q4Group quantize_group(const half_t (&w)[4]) {
   return r;
 }
 
+// Whether the page of a tile's 16 positions from `base` on lies in the pool (no table is read outside the bound).
+__device__ __forceinline__ bool tile_page_ok(const KvCache& c, int s, int64_t base, int64_t len_bound) {
+  return base >= 0 && base < len_bound && page_ok(c, page_id(c, s, (int)(base >> 6)));
+}
+
 struct RopeArgs {
   const float* qkv;
   const uint16_t* bias;
@@ -119,7 +124,7 @@ struct RopeArgs {
 // rotation and one word of codes.  The 16 such groups of a workgroup take a row each and walk its heads, whose rows of
 // the projection follow one another in memory, one load ahead; where a tile has fewer rows (blocks, single tokens),
 // several groups share a row's heads.
-template <bool Q4>
+template <bool Q4, bool Paged>
 __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArgs a) {
   __shared__ float2 tab[kTileRows][64];                             // cosine, sine of (row, pair)
   __shared__ __align__(16) uint16_t vt[Q4 ? 1 : kTileRows][kHd + 4];  // one head's values
@@ -170,8 +175,21 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
   if (busy && hh < head1) next = load(r, hh);
   for (int i = tid >> 6; i < rt.nr; i += 4) tab[i][tid & 63] = rope_cos_sin(rt.pos0 + i, freq);
   __syncthreads();
-  auto valid = [&](int row) { return rt.pos0 + row >= 0 && rt.pos0 + row < a.len_bound; };
-  if (share == 0 && tid < rt.nr && !valid(tid)) flag(a.status, kBadPos);
+  const int64_t base = rt.pos0 - rt.shift;  // a multiple of 16
+  auto in_bounds = [&](int row) { return rt.pos0 + row >= 0 && rt.pos0 + row < a.len_bound; };
+  bool page_good = true;  // (a tile lies in one page)
+  if constexpr (Paged) page_good = tile_page_ok(a.c, rt.s, base, a.len_bound);
+  auto valid = [&](int row) { return in_bounds(row) && page_good; };
+  if (share == 0 && tid < rt.nr) {
+    if (!in_bounds(tid))
+      flag(a.status, kBadPos);
+    else if (!page_good)
+      flag(a.status, kBadPage);
+  }
+  // the first entry of the tile's 64 positions, of kv head g (not used where no row is valid)
+  auto block = [&](int g) {
+    return block64<Paged>(a.c, a.hkv, a.capacity, rt.s, g, Paged && !page_good ? 0 : (int)(base >> 6)).e;
+  };
   if (busy) {
     const bool ok = valid(r);
     for (; hh < head1; hh += step) {
@@ -196,7 +214,7 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
         const half_t wl[4] = {ol[0], ol[1], ol[2], ol[3]}, wh[4] = {oh[0], oh[1], oh[2], oh[3]};
         const Q4Group gl = quantize_group(wl), gh = quantize_group(wh);
         if (ok) {
-          const int64_t e = ((int64_t)rt.s * a.hkv + (hh - a.hq)) * a.capacity + rt.pos0 + r;
+          const int64_t e = block(hh - a.hq) + ((rt.pos0 + r) & 63);
           uint32_t c = 0;
 #pragma unroll
           for (int x = 0; x < 4; ++x) c |= (gl.code[x] | gh.code[x] << 4) << (8 * swap01(x));
@@ -206,20 +224,18 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
                                                              gh.scale | (uint32_t)gh.zero << 16);
         }
       } else if (ok) {
-        uint16_t* dst = a.c.k + (((int64_t)rt.s * a.hkv + (hh - a.hq)) * a.capacity + rt.pos0 + r) * kHd + t0;
+        uint16_t* dst = a.c.k + (block(hh - a.hq) + ((rt.pos0 + r) & 63)) * kHd + t0;
         *reinterpret_cast<half4_t*>(dst) = ol;
         *reinterpret_cast<half4_t*>(dst + 64) = oh;
       }
     }
   }
   // values: a group a row; each head's rows meet in LDS and leave as runs of positions
-  const int64_t base = rt.pos0 - rt.shift;  // a multiple of 16
   auto inside = [&](int c) { return c >= rt.shift && c < rt.shift + rt.nr && valid(c - rt.shift); };
   const bool mine = unit < rt.nr;
   const int c = rt.shift + unit;  // the row's place among the 16 positions
   if (mine && share < a.hkv) next = load(unit, turned + share);
   for (int g = share; g < a.hkv; g += shares) {
-    const int64_t sg = (int64_t)rt.s * a.hkv + g;
     if (g != share) __syncthreads();
     if (mine) {
       Raw w = next;
@@ -252,7 +268,7 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
     if constexpr (Q4) {
       // thread: byte row j, four positions, whose bytes lie exchanged
       const int j = tid & 63, p = 4 * (tid >> 6);
-      uint8_t* dst = a.c.v4 + sg * a.capacity * 64 + (base >> 6) * 4096 + j * 64 + (base & 63) + p;
+      uint8_t* dst = a.c.v4 + block(g) * 64 + j * 64 + (base & 63) + p;
       if (inside(p) && inside(p + 1) && inside(p + 2) && inside(p + 3)) {
         *reinterpret_cast<uint32_t*>(dst) =
             vc4[p][j] | vc4[p + 2][j] << 8 | vc4[p + 1][j] << 16 | (uint32_t)vc4[p + 3][j] << 24;
@@ -262,12 +278,13 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
           if (inside(p + i)) dst[swap01(i)] = vc4[p + i][j];
       }
       if (tid < 64 && inside(tid & 15))
-        a.c.vs[sg * a.capacity * 4 + (base >> 6) * 256 + (base & 63) + (tid >> 4) * 64 + (tid & 15)] =
+        a.c.vs[block(g) * 4 + (base & 63) + (tid >> 4) * 64 + (tid & 15)] =
             vs4[tid >> 4][tid & 15];
     } else {
       // thread: dimension d, eight positions
       const int d = tid & 127, p = 8 * (tid >> 7);
-      uint16_t* dst = a.c.v + (sg * kHd + d) * a.capacity + base + p;
+      uint16_t* dst = Paged ? a.c.v + block(g) * kHd + d * kPage + (base & 63) + p
+                            : a.c.v + (((int64_t)rt.s * a.hkv + g) * kHd + d) * a.capacity + base + p;
       uint16_t e[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) e[i] = vt[p + i][d];
@@ -288,7 +305,8 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
   }
 }
 
-// The values f16((q - z) s) of the entries at the packed rows' positions; rows at bad positions: NaN.
+// The values f16((q - z) s) of the entries at the packed rows' positions; rows at bad positions (or pages): NaN.
+template <bool Paged>
 __global__ __launch_bounds__(256) void packed_read_kernel(PackedRows pr, const int32_t* __restrict__ pos_base,
                                                           int pos_offset, int hkv, int64_t len_bound, int64_t capacity,
                                                           KvCache c, uint16_t* __restrict__ k_out,
@@ -298,27 +316,28 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedRows pr, const i
   RowTile rt;
   if (!row_tile(pr, pos_base, pos_offset, tile_of_block(), rt)) return;  // uniform
   const int64_t base = rt.pos0 - rt.shift;
+  bool page_good = true;
+  if constexpr (Paged) page_good = tile_page_ok(c, rt.s, base, len_bound);
   const CodeConsts kc;
   for (int g = blockIdx.y; g < hkv; g += gridDim.y) {
-    const int64_t sg = (int64_t)rt.s * hkv + g;
+    const int64_t blk = block64<Paged>(c, hkv, capacity, rt.s, g, Paged && !page_good ? 0 : (int)(base >> 6)).e;
     __syncthreads();
-    if (tid < 64 && base >= 0 && base < len_bound)
-      *reinterpret_cast<u32x4*>(vb[tid]) = *reinterpret_cast<const u32x4*>(c.v4 + sg * capacity * 64 +
-                                                                           (base >> 6) * 4096 + tid * 64 + (base & 63));
+    if (tid < 64 && base >= 0 && base < len_bound && page_good)
+      *reinterpret_cast<u32x4*>(vb[tid]) = *reinterpret_cast<const u32x4*>(c.v4 + blk * 64 + tid * 64 + (base & 63));
     __syncthreads();
     for (int r = unit; r < rt.nr; r += 16) {
       const int64_t pos = rt.pos0 + r;
-      const bool ok = pos >= 0 && pos < len_bound;
+      const bool ok = pos >= 0 && pos < len_bound && page_good;
       const int64_t o = ((int64_t)(rt.row0 + r) * hkv + g) * kHd + 4 * t;
       uint32_t kw = 0, vw = 0;
       uint16_t sz[2][4];
       if (ok) {
-        kw = reinterpret_cast<const uint32_t*>(c.k4)[(sg * capacity + pos) * 16 + t];
+        kw = reinterpret_cast<const uint32_t*>(c.k4)[(blk + (pos & 63)) * 16 + t];
         const int cc = swap01(rt.shift + r);
 #pragma unroll
         for (int x = 0; x < 4; ++x) vw |= (uint32_t)vb[4 * t + x][cc] << (8 * swap01(x));
-        const uint16_t* ks = c.ks + (sg * capacity + pos) * 4;
-        const uint16_t* vs = c.vs + sg * capacity * 4 + (pos >> 6) * 256 + (pos & 63);
+        const uint16_t* ks = c.ks + (blk + (pos & 63)) * 4;
+        const uint16_t* vs = c.vs + blk * 4 + (pos & 63);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           sz[0][x] = ks[x];
@@ -372,10 +391,14 @@ hipError_t launch_packed_rope_kv(const float* qkv, const uint16_t* bias, const P
   const int64_t tiles = tile_bound(pr);
   const dim3 grid((unsigned)tiles, head_shares(pr, tiles, hq + hkv));
   const RopeArgs a{qkv, bias, pos_base, pos_offset, hq, hkv, len_bound, capacity, rope_base(theta), q_out, cache, status};
-  if (cache.k4)
-    hipLaunchKernelGGL(packed_rope_kernel<true>, grid, dim3(256), 0, stream, pr, a);
+  if (cache.table && cache.k4)
+    hipLaunchKernelGGL((packed_rope_kernel<true, true>), grid, dim3(256), 0, stream, pr, a);
+  else if (cache.table)
+    hipLaunchKernelGGL((packed_rope_kernel<false, true>), grid, dim3(256), 0, stream, pr, a);
+  else if (cache.k4)
+    hipLaunchKernelGGL((packed_rope_kernel<true, false>), grid, dim3(256), 0, stream, pr, a);
   else
-    hipLaunchKernelGGL(packed_rope_kernel<false>, grid, dim3(256), 0, stream, pr, a);
+    hipLaunchKernelGGL((packed_rope_kernel<false, false>), grid, dim3(256), 0, stream, pr, a);
   return hipGetLastError();
 }
 
@@ -384,8 +407,9 @@ hipError_t launch_packed_kv_read(const PackedRows& pr, int hkv, const int32_t* p
                                  uint16_t* v_out, hipStream_t stream) {
   const int64_t tiles = tile_bound(pr);
   const dim3 grid((unsigned)tiles, head_shares(pr, tiles, hkv));
-  hipLaunchKernelGGL(packed_read_kernel, grid, dim3(256), 0, stream, pr, pos_base, pos_offset, hkv, len_bound, capacity,
-                     cache, k_out, v_out);
+  auto* kernel = cache.table ? packed_read_kernel<true> : packed_read_kernel<false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, pr, pos_base, pos_offset, hkv, len_bound, capacity, cache, k_out,
+                     v_out);
   return hipGetLastError();
 }
 

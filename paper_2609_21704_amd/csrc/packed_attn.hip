@@ -335,11 +335,12 @@ __device__ __forceinline__ void dequant_val(const CodeConsts& k, u32x4 w, const 
       o);
 }
 
-// Element `dim` of the value at position `key` of (sequence, kv head) sg.
-template <bool Q4>
-__device__ __forceinline__ float value_at(const AttnArgs& a, int64_t sg, int64_t key, int dim) {
-  if constexpr (!Q4) return f16_bits_to_f32(a.c.v[(sg * kHd + dim) * a.capacity + key]);
-  const int64_t blk = sg * a.capacity + (key & ~63);
+// Element `dim` of the value at position `key` of (sequence, kv head) (s, g).
+template <bool Q4, bool Paged>
+__device__ __forceinline__ float value_at(const AttnArgs& a, int s, int g, int64_t key, int dim) {
+  if constexpr (!Q4 && !Paged) return f16_bits_to_f32(a.c.v[(((int64_t)s * a.hkv + g) * kHd + dim) * a.capacity + key]);
+  const int64_t blk = block64<Paged>(a.c, a.hkv, a.capacity, s, g, (int)(key >> 6)).e;
+  if constexpr (!Q4) return f16_bits_to_f32(a.c.v[blk * kHd + dim * kPage + ((int)key & 63)]);
   const int j = dim & 63, t = (int)key & 63, hi = dim >> 6;
   const uint32_t c = a.c.v4[blk * 64 + j * 64 + swap01(t)] >> (4 * hi) & 15;
   const uint16_t* p = a.c.vs + blk * 4 + 128 * hi + t;
@@ -351,13 +352,13 @@ __device__ __forceinline__ float value_at(const AttnArgs& a, int64_t sg, int64_t
 struct OddValue {
   float v[2];
 };
-template <bool Q4>
-__device__ __forceinline__ OddValue odd_value(const AttnArgs& a, int64_t sg, int64_t key) {
+template <bool Q4, bool Paged>
+__device__ __forceinline__ OddValue odd_value(const AttnArgs& a, int s, int g, int64_t key) {
   OddValue r;
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float v = value_at<Q4>(a, sg, key, 64 * i + lane);
+    const float v = value_at<Q4, Paged>(a, s, g, key, 64 * i + lane);
     r.v[i] = fabsf(v) <= 65504.f ? 0.f : v;
   }
   return r;
@@ -397,7 +398,7 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
 // 1 us, the first loads 2, a step of 64 keys 0.7, the meeting in LDS 1, and a CU takes in fp16 entries at about 60 GB/s.
 constexpr int kFewWaves = 8;
 
-template <bool Q4, int NQT, int HALVES>
+template <bool Q4, int NQT, int HALVES, bool Paged>
 __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2))) void few_attn_kernel(PackedRows pr,
                                                                                                         AttnArgs a) {
   constexpr int NW = kFewWaves / HALVES;  // wavefronts that share the keys of a half's queries
@@ -460,18 +461,14 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   uint2 ksz[4];                            // .. +8 of a key, positions 8 lg .. +8 and 32 + 8 lg .. +8 of dim 16 d + li
   uint2 vsr;  // 4-bit: this lane's 8 of the 512 bytes of a step's scales and zeros of values
   // uniform bases and 32-bit lane offsets: the addresses stay out of the vector registers
-  const uint8_t* k4 = a.c.k4 + sg * a.capacity * 64;
-  const uint16_t* ks = a.c.ks + sg * a.capacity * 4;
-  const uint8_t* v4 = a.c.v4 + sg * a.capacity * 64;
-  const uint16_t* vs4 = a.c.vs + sg * a.capacity * 4;
-  const uint16_t* k16 = a.c.k + sg * a.capacity * kHd;
   const uint16_t* v16 = a.c.v + sg * kHd * a.capacity;
-  const int64_t vlane = (int64_t)li * a.capacity + 8 * lg;
-  // `live`: all ones; 0 for loads that nothing will use, which all take one lane's
-  auto load_k = [&](int st, uint32_t live) {
+  const int64_t vlane = (int64_t)li * (Paged ? kPage : a.capacity) + 8 * lg;
+  auto block = [&](int st) { return block64<Paged>(a.c, a.hkv, a.capacity, u.s, g, st); };
+  // `e`: the step's first entry; `live`: all ones; 0 for loads that nothing will use, which all take one lane's
+  auto load_k = [&](int64_t e, uint32_t live) {
     if constexpr (Q4) {
-      const uint8_t* kst = k4 + (int64_t)st * (kTile * 64);
-      const uint16_t* sst = ks + (int64_t)st * (kTile * 4);
+      const uint8_t* kst = a.c.k4 + e * 64;
+      const uint16_t* sst = a.c.ks + e * 4;
       const uint32_t at = (krow * 64 + 16 * lg) & live, as = krow * 8 & live;
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
@@ -479,7 +476,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         ksz[kt] = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(sst) + (as + 32 * kt));
       }
     } else {
-      const uint8_t* kst = reinterpret_cast<const uint8_t*>(k16 + (int64_t)st * (kTile * kHd));
+      const uint8_t* kst = reinterpret_cast<const uint8_t*>(a.c.k + e * kHd);
       const uint32_t at = (krow * 256 + 16 * lg) & live;
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
@@ -487,10 +484,10 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         for (int x = 0; x < 4; ++x) kw[4 * kt + x] = *reinterpret_cast<const u32x4*>(kst + (at + 256 * kt_at(kt) + 64 * x));
     }
   };
-  auto load_v = [&](int st, uint32_t live) {
+  auto load_v = [&](int64_t e, int st, uint32_t live) {
     if constexpr (Q4) {
-      vsr = reinterpret_cast<const uint2*>(vs4 + (int64_t)st * 256)[(uint32_t)lane & live];
-      const uint8_t* vst = v4 + (int64_t)st * 4096;
+      vsr = reinterpret_cast<const uint2*>(a.c.vs + e * 4)[(uint32_t)lane & live];
+      const uint8_t* vst = a.c.v4 + e * 64;
       const uint32_t at = (li * 64 + 16 * lg) & live;
 #pragma unroll
       for (int j = 0; j < 4; ++j) vw[j] = *reinterpret_cast<const u32x4*>(vst + (at + 1024 * j));
@@ -498,7 +495,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
         const int64_t vl = live ? vlane : 0;
-        const uint16_t* vst = v16 + (int64_t)16 * d * a.capacity + (int64_t)st * kTile;
+        const uint16_t* vst = Paged ? a.c.v + e * kHd + 16 * d * kPage
+                                    : v16 + (int64_t)16 * d * a.capacity + (int64_t)st * kTile;
         vw[2 * d] = *reinterpret_cast<const u32x4*>(vst + vl);
         vw[2 * d + 1] = *reinterpret_cast<const u32x4*>(vst + vl + 32);
       }
@@ -514,9 +512,11 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     turn = turn == (older ? 2 : 1) ? 0 : turn + 1;
     return st + gap;
   };
+  Block64 here = {};
+  if (st0 + wave < end) here = block(st0 + wave);
   if (kAhead && st0 + wave < end) {
-    load_k(st0 + wave, ~0u);
-    load_v(st0 + wave, ~0u);
+    load_k(here.e, ~0u);
+    load_v(here.e, st0 + wave, ~0u);
   }
   auto product = [&](int d, half8_t v0, half8_t v1) {
 #pragma unroll
@@ -535,8 +535,9 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     following = advance(st);
     const int next = following < end ? following : st;  // (loads after the last step, too: no branch around loads)
     const uint32_t live = following < end ? ~0u : 0u;
+    const Block64 ahead = block(next);
     float4_t sc[NQT][4];
-    if constexpr (!kAhead) load_k(st, ~0u);
+    if constexpr (!kAhead) load_k(here.e, ~0u);
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
       half8_t kf[4];
@@ -556,7 +557,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       }
 #pragma unroll
       for (int t = 0; t < NQT; ++t) {
-        float4_t acc = {0.f, 0.f, 0.f, 0.f};
+        float4_t acc = {here.odd, here.odd, here.odd, here.odd};
 #pragma unroll
         for (int x = 0; x < 4; ++x) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[x], qf[t][x], acc, 0, 0, 0);
         sc[t][kt] = acc;
@@ -564,9 +565,9 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       if constexpr (NQT > 1) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (kAhead)
-      load_k(next, live);
+      load_k(ahead.e, live);
     else
-      load_v(st, ~0u);
+      load_v(here.e, st, ~0u);
     __builtin_amdgcn_sched_barrier(0);
     // only a step past the first row's position holds keys that some row may not read
     const bool tail = key0 + kTile - 1 > p0;  // uniform
@@ -680,7 +681,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         product(d, __builtin_bit_cast(half8_t, w0), __builtin_bit_cast(half8_t, w1));
       }
     }
-    if constexpr (kAhead) load_v(next, live);
+    if constexpr (kAhead) load_v(ahead.e, next, live);
+    here = ahead;
     __builtin_amdgcn_sched_barrier(0);
   }
   if (odd_seen) {
@@ -691,7 +693,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
       if (key0 + kTile - 1 <= p0) continue;
 #pragma unroll 1
       for (int64_t key = key0; key < key0 + kTile && key <= klast; ++key) {
-        const OddValue ov = odd_value<Q4>(a, sg, key);
+        const OddValue ov = odd_value<Q4, Paged>(a, u.s, g, key);
         if (!__any(ov.v[0] != 0.f || ov.v[1] != 0.f)) continue;
 #pragma unroll
         for (int d = 0; d < 8; ++d)
@@ -798,7 +800,7 @@ constexpr int kSplitGroups = 2;
 // split more did not help (one group: 20.8 us with two, 22.5 with three, 24.2 with four).
 constexpr int ring(bool q4, int nw) { return q4 || nw < 8 ? 2 : 3; }
 
-template <bool Q4, int NW, int KW, bool SPLIT>
+template <bool Q4, int NW, int KW, bool SPLIT, bool Paged>
 __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_attn_kernel(PackedRows pr,
                                                                                                       AttnArgs a) {
   constexpr int NT = 64 * NW, TQ = 32 * NW, kRing = ring(Q4, NW);
@@ -825,7 +827,8 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
   const int st0 = SPLIT ? __builtin_amdgcn_readfirstlane(u.part * u.span) : 0;
   const int st1 = SPLIT && st0 + u.span < nst ? st0 + u.span : nst;
   if (SPLIT && u.part > 0 && st0 >= st1) return;  // (part 0 always answers: rows without any key)
-  const int64_t sg = (int64_t)__builtin_amdgcn_readfirstlane(u.s) * a.hkv + g;
+  const int seq = __builtin_amdgcn_readfirstlane(u.s);
+  const int64_t sg = (int64_t)seq * a.hkv + g;
   const int wq = qt * TQ + 32 * wave;                       // the wavefront's first query
   const bool owner = wq < nq;
   const int qi = wq + lc < nq ? wq + lc : nq - 1, qj = qi / G;
@@ -843,18 +846,20 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
   for (int i = 0; i < kLoads; ++i) {
     const int row = 4 * (wave + NW * i) + (lane >> 4);
     koff[i] = row * 256 + 16 * ((lane & 15) ^ swap23(row & 15));
-    v16[i] = a.c.v + (sg * kHd + 8 * (wave + NW * i)) * a.capacity;
+    v16[i] = Paged ? a.c.v + 8 * (wave + NW * i) * kPage : a.c.v + (sg * kHd + 8 * (wave + NW * i)) * a.capacity;
   }
   // (dimension d = 8 (wave + NW i) + lane / 8: d / 2 % 8 is 4 (wave % 2) + lane / 16, NW even)
-  voff = (uint32_t)(lane >> 3) * (uint32_t)(2 * a.capacity) + 16 * ((lane & 7) ^ (4 * (wave & 1) + (lane >> 4)));
+  voff = (uint32_t)(lane >> 3) * (uint32_t)(2 * (Paged ? kPage : a.capacity)) + 16 * ((lane & 7) ^ (4 * (wave & 1) + (lane >> 4)));
   const uint32_t kdst = lds_address(&kb[kw * kRing][64 * wave]), vdst = lds_address(&vb[kw * kRing][64 * wave]);
-  auto issue_step = [&](int st, int buf) {
-    const uint16_t* kst = k16 + (int64_t)st * (kTile * kHd);
+  auto issue_step = [&](int st, int64_t e, int buf) {  // (e: of a paged cache, the step's first entry)
+    const uint16_t* kst = Paged ? a.c.k + e * kHd : k16 + (int64_t)st * (kTile * kHd);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_to_lds(kst, koff[i], kdst + 16384 * buf + 1024 * NW * i);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds(v16[i] + (int64_t)st * kTile, voff, vdst + 16384 * buf + 1024 * NW * i);
+    for (int i = 0; i < kLoads; ++i)
+      load_to_lds(v16[i] + (Paged ? e * kHd : (int64_t)st * kTile), voff, vdst + 16384 * buf + 1024 * NW * i);
   };
+  auto block = [&](int st) { return block64<Paged>(a.c, a.hkv, a.capacity, seq, g, st); };
   // ... and in a step past the tile's first position the values are tamed where they lie
   auto tame_step = [&](int st, int buf) {
     uint32_t odd = 0;
@@ -879,19 +884,18 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
   ValScales pre_vs;
   // 4-bit cell c: key c / 4, part c % 4 of it (c < 256), byte (c - 256) / 4 of the block of values, positions 16 (c % 4)
   // .. +16; which of the two is uniform across a wavefront
-  auto load_step = [&](int st) {
-    const int64_t key0 = (int64_t)st * kTile;
+  auto load_step = [&](int64_t first) {  // (the step's first entry)
 #pragma unroll
     for (int i = 0; i < kCodes; ++i) {
       const int c = tid + NT * i;
       if (c < 256) {
-        const int64_t e = sg * a.capacity + key0 + (c >> 2);
+        const int64_t e = first + (c >> 2);
         pre[i] = reinterpret_cast<const u32x4*>(a.c.k4)[e * 4 + (c & 3)];
         pre_ks[i] = reinterpret_cast<const uint2*>(a.c.ks)[e];
       } else {
         const int c2 = c - 256;
-        pre[i] = *reinterpret_cast<const u32x4*>(a.c.v4 + sg * a.capacity * 64 + (int64_t)st * 4096 + 16 * c2);
-        pre_vs = load_val_scales(a.c.vs + sg * a.capacity * 4 + (int64_t)st * 256 + 16 * (c2 & 3));
+        pre[i] = *reinterpret_cast<const u32x4*>(a.c.v4 + first * 64 + 16 * c2);
+        pre_vs = load_val_scales(a.c.vs + first * 4 + 16 * (c2 & 3));
       }
     }
   };
@@ -937,13 +941,13 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
   if constexpr (Q4) {
     __syncthreads();
     if (st0 + kw < st1) {
-      load_step(st0 + kw);
+      load_step(block(st0 + kw).e);
       store_step(st0 + kw, 0);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i)
-      if (st0 + kw + KW * i < st1) issue_step(st0 + kw + KW * i, i);
+      if (st0 + kw + KW * i < st1) issue_step(st0 + kw + KW * i, Paged ? block(st0 + kw + KW * i).e : 0, i);
   }
   half8_t qf[8];
   {
@@ -966,16 +970,18 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
     const int st = round + kw, key0 = st * kTile;
     // uniform: some row of the workgroup may not read some key of the round
     const bool past = (round + KW - 1) * (int64_t)kTile + kTile - 1 > pmin;
+    int64_t ahead = 0;  // the first entry of the step to be issued, whose page is read before the wait
+    if constexpr (Paged && !Q4) ahead = block(st + KW * (kRing - 1) < st1 ? st + KW * (kRing - 1) : st1 - 1).e;
     // step st is in its buffer, and every wavefront is done with step st - KW
     if constexpr (Q4) {
       __syncthreads();
-      if (st + KW < st1) load_step(st + KW);
+      if (st + KW < st1) load_step(block(st + KW).e);
     } else {
       if (st + KW * (kRing - 2) < st1)  // the steps st + KW .. st + KW (kRing - 2) may stay in flight
         barrier_after_loads<(kRing - 2) * 2 * kLoads>();
       else
         barrier_after_loads<0>();
-      if (st + KW * (kRing - 1) < st1) issue_step(st + KW * (kRing - 1), buf == 0 ? kRing - 1 : buf - 1);
+      if (st + KW * (kRing - 1) < st1) issue_step(st + KW * (kRing - 1), ahead, buf == 0 ? kRing - 1 : buf - 1);
       if (past) {
         if (st < st1 && key0 + kTile - 1 > pmin) tame_step(st, buf);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -984,11 +990,12 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
       }
     }
     if (owner && key0 <= wmax && (KW == 1 || st < st1)) {  // uniform in the wavefront
+      const float odd = Paged ? block(st).odd : 0.f;
       float16_t sc[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) sc[b][i] = odd;
       // fragment i of the keys: half i % 2 of the tile, dimensions 16 (i / 2) .. +16; kDeep of them ahead of the products
       constexpr int kDeep = Q4 ? 2 : 8;
       u32x4 f[kDeep];
@@ -1066,7 +1073,7 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
       if (st * (int64_t)kTile + kTile - 1 <= pmin) continue;
 #pragma unroll 1
       for (int key = st * kTile; key < st * kTile + kTile && key <= wmax && key <= klast; ++key) {
-        const OddValue ov = odd_value<Q4>(a, sg, key);
+        const OddValue ov = odd_value<Q4, Paged>(a, seq, g, key);
         if (!__any(ov.v[0] != 0.f || ov.v[1] != 0.f)) continue;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
@@ -1273,25 +1280,25 @@ Plan make_plan(const PackedRows& pr, int hq, int hkv, int64_t len_bound, bool q4
   return p;
 }
 
-template <bool Q4>
+template <bool Q4, bool Paged>
 void launch_few(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
   const dim3 block(64 * kFewWaves);
   if (p.tq == 16)
-    hipLaunchKernelGGL((few_attn_kernel<Q4, 1, 1>), grid, block, 0, stream, pr, a);
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 1, 1, Paged>), grid, block, 0, stream, pr, a);
   else if (p.tq == 32)
-    hipLaunchKernelGGL((few_attn_kernel<Q4, 2, 1>), grid, block, 0, stream, pr, a);
+    hipLaunchKernelGGL((few_attn_kernel<Q4, 2, 1, Paged>), grid, block, 0, stream, pr, a);
   else if constexpr (Q4)
-    hipLaunchKernelGGL((few_attn_kernel<true, 2, 2>), grid, block, 0, stream, pr, a);
+    hipLaunchKernelGGL((few_attn_kernel<true, 2, 2, Paged>), grid, block, 0, stream, pr, a);
 }
 
-template <bool Q4>
+template <bool Q4, bool Paged>
 void launch_prompt(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
   if (p.tq == 256)  // (never split: so many tiles fill the chip)
-    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 8, 1, false>), grid, dim3(512), 0, stream, pr, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 8, 1, false, Paged>), grid, dim3(512), 0, stream, pr, a);
   else if (p.most)
-    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 4, kSplitGroups, true>), grid, dim3(256 * kSplitGroups), 0, stream, pr, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 4, kSplitGroups, true, Paged>), grid, dim3(256 * kSplitGroups), 0, stream, pr, a);
   else
-    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 4, 1, false>), grid, dim3(256), 0, stream, pr, a);
+    hipLaunchKernelGGL((prompt_attn_kernel<Q4, 4, 1, false, Paged>), grid, dim3(256), 0, stream, pr, a);
 }
 
 }  // namespace
@@ -1320,17 +1327,17 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
   // 366; 40 heads on 8, four of up to 3000 72.3 for 75.6 and 128.4 for 126.5, eight 282 for 275 and 220 for 217.
   const int64_t seqs = pr.b < pr.rows ? pr.b : pr.rows;
   a.longest = !p.few && seqs > 1 && seqs * hkv <= 32 && (int64_t)units * hkv > (p.tq == 256 ? 256 : 512);
-  if (p.few) {
-    if (q4)
-      launch_few<true>(p, grid, pr, a, stream);
+  const bool paged = cache.table != nullptr;
+  auto launch = [&](auto is_q4, auto is_paged) {
+    if (p.few)
+      launch_few<is_q4.value, is_paged.value>(p, grid, pr, a, stream);
     else
-      launch_few<false>(p, grid, pr, a, stream);
-  } else {
-    if (q4)
-      launch_prompt<true>(p, grid, pr, a, stream);
-    else
-      launch_prompt<false>(p, grid, pr, a, stream);
-  }
+      launch_prompt<is_q4.value, is_paged.value>(p, grid, pr, a, stream);
+  };
+  if (paged)
+    q4 ? launch(std::true_type{}, std::true_type{}) : launch(std::false_type{}, std::true_type{});
+  else
+    q4 ? launch(std::true_type{}, std::false_type{}) : launch(std::false_type{}, std::false_type{});
   if (p.most)
     hipLaunchKernelGGL(packed_merge_kernel, dim3((unsigned)(p.tiles * hkv), (unsigned)(p.tq / 4)), dim3(256), 0, stream,
                        pr, a, p.tq, p.grain, p.few);

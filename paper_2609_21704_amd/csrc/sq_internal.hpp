@@ -208,14 +208,18 @@ struct PackedRows {
   const int32_t* start;
   int b, rows, max_rows;
 };
-// The caches of one layer: fp16 (k, v) or 4-bit (k4, ks, v4, vs; k4 null: fp16).
+// The caches of one layer: fp16 (k, v) or 4-bit (k4, ks, v4, vs; k4 null: fp16); with a table, pools of `pages` pages of 64
+// positions, [pages][hkv][..] each, and the pages of sequence s in table[s * width ..].
 struct KvCache {
   uint16_t *k, *v;
   uint8_t* k4;
   uint16_t* ks;
   uint8_t* v4;
   uint16_t* vs;
+  const int32_t* table = nullptr;
+  int width = 0, pages = 0;
 };
+constexpr int kPage = 64;  // positions of a page: a step of the attention kernels, a block of 4-bit values
 hipError_t launch_packed_rope_kv(const float* qkv, const uint16_t* bias, const PackedRows& pr, int hq, int hkv,
                                  const int32_t* pos_base, int pos_offset, int64_t len_bound, int64_t capacity,
                                  double theta, uint16_t* q_out, const KvCache& cache, int32_t* status,
@@ -226,5 +230,20 @@ hipError_t launch_packed_kv_read(const PackedRows& pr, int hkv, const int32_t* p
 hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int hq, int hkv, const int32_t* pos_base,
                                    int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
                                    uint16_t* out, hipStream_t stream);
+
+// Which rows hold which pages of a paged cache (pages.hip).
+struct PageState {
+  int32_t *table, *held, *refs;  // [b][width], [b], [pages]
+  int b, width, pages;
+};
+hipError_t launch_pages_reserve(const PageState& p, const int32_t* pos_base, int ahead, int32_t* status,
+                                hipStream_t stream);
+hipError_t launch_pages_trim(const PageState& p, const int32_t* keep, int32_t* status, hipStream_t stream);
+hipError_t launch_pages_fork(const PageState& p, const int32_t* parent, const int32_t* child, const int32_t* length, int n,
+                             int32_t* src, int32_t* dst, int32_t* count, int32_t* status, hipStream_t stream);
+hipError_t launch_pages_compact(const PageState& p, int32_t* src, int32_t* dst, int32_t* count, int32_t* used,
+                                int32_t* status, hipStream_t stream);
+hipError_t launch_page_copy(void* pool, int layers, int pages, int64_t page_bytes, const int32_t* src, const int32_t* dst,
+                            const int32_t* count, int n, int32_t* status, hipStream_t stream);
 
 }  // namespace sq

@@ -46,6 +46,30 @@ __device__ __forceinline__ bool find_tile(int b, int item, F tiles, int& s, int&
   return false;
 }
 
+// ------------------------------------------------------------------- pages
+// Page `i` of sequence s, the same for the whole wavefront.  Through the constant address space, for a scalar load
+// (prompt_attn_kernel counts its vector loads); the table is written by earlier launches only.
+__device__ __forceinline__ int page_id(const KvCache& c, int s, int i) {
+  typedef const __attribute__((address_space(4))) int32_t* table_t;
+  const int64_t row = (int64_t)__builtin_amdgcn_readfirstlane(s) * c.width;
+  return ((table_t)(uintptr_t)c.table)[row + __builtin_amdgcn_readfirstlane(i)];
+}
+__device__ __forceinline__ bool page_ok(const KvCache& c, int page) { return (uint32_t)page < (uint32_t)c.pages; }
+
+// The first entry of the 64 positions 64 i .. +64 of (sequence s, kv head g): entries of a kv head follow one another.
+// A table entry outside the pool is not followed: its keys are those of page 0, and `odd` is NaN for their scores (else 0).
+struct Block64 {
+  int64_t e;
+  float odd;
+};
+template <bool Paged>
+__device__ __forceinline__ Block64 block64(const KvCache& c, int hkv, int64_t capacity, int s, int g, int i) {
+  if constexpr (!Paged) return {((int64_t)s * hkv + g) * capacity + (int64_t)i * kPage, 0.f};
+  const int page = page_id(c, s, i);
+  const bool ok = page_ok(c, page);
+  return {((int64_t)(ok ? page : 0) * hkv + g) * kPage, ok ? 0.f : __builtin_nanf("")};
+}
+
 // ------------------------------------------------------------ 4-bit entries
 // An entry of 128 elements is two groups of 64 with a scale and a zero each; byte j holds the codes of elements j (low
 // nibble) and j + 64 (high).  Four consecutive bytes (of a key: elements; of a block of values: positions) lie in the
