@@ -18,6 +18,7 @@ from ._lib import (  # noqa: F401
     sq_add_rmsnorm_f16,
     sq_attention_f16,
     sq_embed_block_f16,
+    sq_filter_logits_f32,
     sq_kv_adopt_f16,
     sq_packed_attention_f16,
     sq_packed_attention_q4,
@@ -44,6 +45,7 @@ from ._lib import (  # noqa: F401
     sq_probe_stream_read,
     sq_rope_attention_f16,
     sq_rope_kv_f16,
+    sq_sample_f32,
     sq_silu_mul_f16,
     sq_spec_accept,
     sq_spec_accept_multi,

@@ -93,6 +93,8 @@ def load() -> ctypes.CDLL:
             "sq_paged_kv_read_q4": ([P, P, P, P, P, I64, I64, P, I32, I64, I64, I32, P, I32, I64, P, P, P], S),
             "sq_paged_attention_f16": ([P, P, P, P, I64, I64, P, I32, I64, I64, I32, I32, P, I32, I64, P, P], S),
             "sq_paged_attention_q4": ([P, P, P, P, P, P, I64, I64, P, I32, I64, I64, I32, I32, P, I32, I64, P, P], S),
+            "sq_sample_f32": ([P, I32, I64, I64, P, P, P, P, P, P, P, P], S),
+            "sq_filter_logits_f32": ([P, I32, I64, I64, P, P, P, P, P, P, P], S),
             "sq_kv_adopt_f16": ([P, P, I32, I32, I32, I32, I64, P, P, P, I32, I32, P], S),
             "sq_spec_commit_multi": ([P, P, P, P, I32, I32, I32, P, P, P, P, I64, P, P, P], S),
         }
@@ -116,6 +118,7 @@ EXPORTED = ("sq_abi_version", "sq_status_str", "sq_quantize_int4_g128", "sq_quan
 DEV_BAD_TOKEN, DEV_BAD_POS, DEV_OVERFLOW, DEV_NO_DIST = 1, 2, 4, 8
 DEV_BAD_ROWS = 16  # of include/specquant_packed.h
 DEV_NO_PAGES, DEV_BAD_PAGE, DEV_BAD_FORK = 32, 64, 128  # of include/specquant_paged.h
+DEV_BAD_PARAM = 256  # of include/specquant_sample.h
 
 
 def _ptr(t):
@@ -1015,3 +1018,46 @@ def sq_paged_attention_q4(q, k_codes, k_scales, v_codes, v_scales, table, row_st
     cache = (k_codes, k_scales, v_codes, v_scales)
     return _paged_attention("sq_paged_attention_q4", q, cache, _pool_q4(*cache), table, row_start, pos_base, max_rows,
                             pos_offset, len_bound, out)
+
+
+# ----------------------------------------------------------------- sampling
+# The calls of include/specquant_sample.h.  temperature, top_p, min_p: float32 [m], top_k: int32 [m], on the GPU; None
+# leaves them out (temperature 1).
+
+
+def _sample_args(logits, temperature, top_k, top_p, min_p, vocab):
+    if logits.dtype != torch.float32 or logits.dim() != 2:
+        raise ValueError("logits must be float32 [m][ld]")
+    m, ld = logits.shape
+    for t, dtype, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        if t is not None:
+            _expect(t, dtype, (m,), name)
+    return (logits.data_ptr(), m, ld if vocab is None else int(vocab), ld, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+            _ptr(min_p))
+
+
+def sq_sample_f32(logits, u24, temperature=None, top_k=None, top_p=None, min_p=None, vocab: int | None = None, token=None,
+                  status=None):
+    """A token of every row of logits [m][ld] (its first `vocab`), drawn with u24 int32 [m] from what the filters leave of
+    softmax(logits / temperature); returns token int32 [m]."""
+    args = _sample_args(logits, temperature, top_k, top_p, min_p, vocab)
+    m = logits.shape[0]
+    _expect(u24, torch.int32, (m,), "u24")
+    token = torch.empty((m,), dtype=torch.int32, device=logits.device) if token is None else token
+    _expect(token, torch.int32, (m,), "token")
+    _launch("sq_sample_f32", (logits, u24, temperature, top_k, top_p, min_p, token, status), *args, u24.data_ptr(),
+            token.data_ptr(), _status_word(status))
+    return token
+
+
+def sq_filter_logits_f32(logits, temperature=None, top_k=None, top_p=None, min_p=None, vocab: int | None = None, out=None,
+                         status=None):
+    """The first `vocab` logits of every row, those of tokens that the filters drop as -inf; returns out [m][ld] (logits
+    itself to filter in place; what lies behind `vocab` is not written)."""
+    args = _sample_args(logits, temperature, top_k, top_p, min_p, vocab)
+    out = torch.empty_like(logits) if out is None else out
+    _expect(out, torch.float32, tuple(logits.shape), "out")
+    _launch("sq_filter_logits_f32", (logits, temperature, top_k, top_p, min_p, out, status), *args, out.data_ptr(),
+            _status_word(status))
+    return out

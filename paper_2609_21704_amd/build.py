@@ -13,7 +13,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libspecquant.so")
 
 SOURCES = ["quant.hip", "gemv.hip", "gemm.hip", "linear.hip", "prefill.hip", "accept.hip", "decoder.hip", "packed.hip",
-           "packed_attn.hip", "pages.hip", "probe.hip", "abi.cpp", "abi_prefill.cpp", "abi_packed.cpp", "abi_paged.cpp"]
+           "packed_attn.hip", "pages.hip", "sample.hip", "probe.hip", "abi.cpp", "abi_prefill.cpp", "abi_packed.cpp", "abi_paged.cpp",
+           "abi_sample.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -246,4 +246,9 @@ hipError_t launch_pages_compact(const PageState& p, int32_t* src, int32_t* dst, 
 hipError_t launch_page_copy(void* pool, int layers, int pages, int64_t page_bytes, const int32_t* src, const int32_t* dst,
                             const int32_t* count, int n, int32_t* status, hipStream_t stream);
 
+// Draws (token), or filtered logits (out), of m rows of v logits (sample.hip).
+hipError_t launch_sample(const float* logits, int m, int v, int64_t ld, const float* temperature, const int32_t* top_k,
+                         const float* top_p, const float* min_p, const uint32_t* u24, int32_t* token, float* out,
+                         int32_t* status, hipStream_t stream);
+
 }  // namespace sq
