@@ -25,7 +25,7 @@
  *
  * logits [m][ld] f32, of which the first v of each row count; 1 <= m <= 2^20, 1 <= v <= 2^26, v <= ld < 2^31.
  * temperature, top_k, top_p, min_p [m] (f32, int32, f32, f32), each NULL: 1, 0, 1 and 0 for every row.
- * Workspace: at most 40 MB.
+ * Workspace: at most 32 MB.
  */
 #ifndef SPECQUANT_SAMPLE_H
 #define SPECQUANT_SAMPLE_H

@@ -4,14 +4,15 @@
 //   1. range_kernel   per (row, segment) the largest and smallest logit
 //   2. bins_kernel    per (row, segment) the weights' sums and counts in 1024 bins of the distance from the maximum;
 //                     the row's last workgroup finds the bins that the cuts go through
-//   3. cut_kernel     gathers the tokens of those bins (a few) and sums the weights that are kept for sure; the row's
-//                     last workgroup ranks the gathered tokens against each other, which gives the cuts, and draws
+//   3. cut_kernel     gathers the tokens of those bins and sums the weights that are kept for sure; the row's last
+//                     workgroup finds the cuts among the gathered tokens (1024 bins of the bin, then ranks) and draws
 //   4. filter_kernel  writes the kept logits
-// A row without top-k and top-p is drawn from by step 2.  Where the bins of the cuts hold too many tokens to rank (ties,
-// rows whose logits lie close together but for a few), the last workgroup finds the cuts by a radix selection over the
-// row (11 bits of the logit's key a pass).
+// A row without top-k and top-p is drawn from by step 2.  Where the bins of the cuts hold too many tokens (ties, rows
+// whose logits lie close together but for a few), the last workgroup finds the cuts by a radix selection over the row
+// (11 bits of the logit's key a pass).
 // Weights are whole numbers, so their sums do not depend on any order.  Rows are cut into segments so that a call fills
-// the chip from one row on; last workgroups are found by counting arrivals (counters that step 1 clears).
+// the chip from one row on, and a segment into runs, one a wavefront, whose sums say where a draw has to look.  Last
+// workgroups are found by counting arrivals (counters that step 1 clears).
 // Bound by latency in few rows, by fp64 instructions in many (a weight is about 30 of them).
 #include <limits.h>
 
@@ -26,8 +27,11 @@ namespace {
 constexpr int32_t kNoDist = 8, kBadParam = 256;  // the SQ_DEV_* values of the C headers
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = kThreads;   // one a thread where they are scanned
-constexpr int kMost = 2048;       // gathered tokens of a row that are ranked
+constexpr int kHeld = 4;          // gathered tokens a thread holds
+constexpr int kMost = kHeld * kThreads;
+constexpr int kFew = 512;         // tokens that are ranked against each other
 constexpr int kMaxSegments = 16;  // of a row
+constexpr int kMaxRuns = kMaxSegments * kWaves;
 constexpr int kMinSegment = 4096; // tokens
 constexpr double kSpan = 32.0;    // nats below the maximum that the bins cover (e^-32 < 2^-46)
 
@@ -41,7 +45,7 @@ struct SampleArgs {
   int32_t* token;  // null: filter
   float* out;
   int32_t* status;
-  int segments, len;  // of a row; tokens of a segment
+  int segments, run;  // of a row, of kWaves runs each; tokens of a run
   int shift;          // log2 of the largest weight
 };
 
@@ -66,9 +70,9 @@ enum : int { kDone = 0, kAll = 1, kCut = 2, kNan = 3, kSame = 4 };
 
 struct Scratch {
   Cell* cells;       // [m][segments]
-  int64_t* sums;     // [m][segments][kBins], then [m][segments] of step 3
-  int64_t* kept;
-  int64_t* counts;   // [m][segments][kBins]
+  int64_t* sums;     // [m][segments][kBins]
+  int64_t* kept;     // [m][segments * kWaves]: of the runs
+  int32_t* counts;   // [m][segments][kBins]
   int64_t* list;     // [m][kMost]: logit in the low half, index in the high one
   Cut* cuts;         // [m]
   int32_t* counters; // [m][4]: arrivals of steps 2 and 3, gathered tokens
@@ -96,10 +100,19 @@ struct Params {
 // The weight of a logit, and on the grid.
 struct Weight {
   Soft<false> sf;
-  double zmax, grid;
-  __device__ __forceinline__ Weight(float t, float hi, int shift) : sf(t), zmax(sf.z(hi)), grid(ldexp(1.0, shift)) {}
+  double zmax;
+  int shift;
+  __device__ __forceinline__ Weight(float t, float hi, int shift) : sf(t), zmax(sf.z(hi)), shift(shift) {}
   __device__ __forceinline__ float w(float l) const { return (float)sf.exp(sf.z(l) - zmax); }
-  __device__ __forceinline__ int64_t r(float w) const { return llrint((double)w * grid); }
+  // rint(w 2^shift), ties to even, from the bits of w in [0, 1]
+  __device__ __forceinline__ int64_t r(float w) const {
+    const uint32_t u = __builtin_bit_cast(uint32_t, w);
+    const int e = (int)(u >> 23) - 150 + shift;
+    const uint32_t m = u < 0x00800000u ? 0u : (u & 0x7FFFFFu) | 0x800000u;  // (below 2^-126: 0 on every grid)
+    if (e >= 0) return (int64_t)m << e;
+    const int k = -e < 26 ? -e : 26;
+    return (m + ((1u << (k - 1)) - 1) + ((m >> k) & 1)) >> k;
+  }
 };
 
 // Bins of the distance from the maximum, in the order of the logits: differences, products and minima round monotonically.
@@ -116,20 +129,39 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 // `last`, `at` in (and everything before it in the order) against (l, j)
 __device__ __forceinline__ bool up_to(float l, int j, float last, int at) { return l > last || (l == last && j <= at); }
 
-// Tokens of a segment in steps of kBatch a thread, their loads in flight together; f(l, j) for every one.
-constexpr int kBatch = 8;
+// f(l, j) for the tokens from .. to, of which a wavefront (stride 64) or the workgroup takes every stride-th; kBatch loads
+// a thread in flight while the batch before is worked on.
+constexpr int kBatch = 4;
 template <class F>
-__device__ __forceinline__ void each_token(const float* row, int from, int to, F f) {
-  for (int base = from; base < to; base += kThreads * kBatch) {  // uniform
-    float x[kBatch];
+__device__ __forceinline__ void each_token(const float* row, int from, int to, int first, int stride, F f) {
+  if (from >= to) return;
+  float x[kBatch], y[kBatch];
+  auto load = [&](int base, float (&v)[kBatch]) {
 #pragma unroll
-    for (int e = 0; e < kBatch; ++e) x[e] = row[min(base + e * kThreads + (int)threadIdx.x, to - 1)];
+    for (int e = 0; e < kBatch; ++e) v[e] = row[min(base + e * stride + first, to - 1)];
+  };
+  load(from, x);
+  for (int base = from; base < to; base += stride * kBatch) {  // uniform
+    if (base + stride * kBatch < to) load(base + stride * kBatch, y);
 #pragma unroll
     for (int e = 0; e < kBatch; ++e) {
-      const int j = base + e * kThreads + (int)threadIdx.x;
+      const int j = base + e * stride + first;
       if (j < to) f(x[e], j);
     }
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) x[e] = y[e];
   }
+}
+// ... of this wavefront's run of a segment
+template <class F>
+__device__ __forceinline__ void each_of_run(const SampleArgs& a, const float* row, int run, F f) {
+  const int from = (int)min((int64_t)run * a.run, (int64_t)a.v), to = (int)min((int64_t)from + a.run, (int64_t)a.v);
+  each_token(row, from, to, threadIdx.x & 63, kWave, f);
+}
+// ... and of the whole row
+template <class F>
+__device__ __forceinline__ void each_of_row(const SampleArgs& a, const float* row, F f) {
+  each_token(row, 0, a.v, threadIdx.x, kThreads, f);
 }
 
 // True in every thread of the row's last workgroup to arrive, after whose return it sees what all of them published.
@@ -142,13 +174,24 @@ __device__ __forceinline__ bool last_of_row(int32_t* counter, int n, int* sh) {
 }
 
 // ------------------------------------------------------------------- step 1
+__device__ __forceinline__ Cell merge(Cell x, Cell y) {
+  const bool other = y.hi > x.hi || (y.hi == x.hi && y.at < x.at);
+  return Cell{other ? y.hi : x.hi, fminf(x.lo, y.lo), other ? y.at : x.at, x.bad | y.bad};
+}
+template <int kLanes>
+__device__ __forceinline__ Cell merge_lanes(Cell c) {
+#pragma unroll
+  for (int d = kLanes / 2; d >= 1; d >>= 1)
+    c = merge(c, Cell{__shfl_xor(c.hi, d), __shfl_xor(c.lo, d), __shfl_xor(c.at, d), __shfl_xor(c.bad, d)});
+  return c;
+}
+
 __global__ __launch_bounds__(kThreads) void range_kernel(SampleArgs a, Scratch sc) {
   __shared__ Cell sh[kWaves];
-  const int row = blockIdx.x / a.segments, seg = blockIdx.x - row * a.segments;
-  const int from = seg * a.len, to = min(from + a.len, a.v);
+  const int row = blockIdx.x / a.segments, seg = blockIdx.x - row * a.segments, w = threadIdx.x >> 6;
   if (seg == 0 && threadIdx.x < 4) sc.counters[4 * (int64_t)row + threadIdx.x] = 0;
   Cell c = {-INFINITY, INFINITY, INT_MAX, 0};
-  each_token(a.logits + row * a.ld, from, to, [&](float l, int j) {
+  each_of_run(a, a.logits + row * a.ld, seg * kWaves + w, [&](float l, int j) {
     c.bad |= isnan(l) || l == INFINITY ? 1 : 0;
     if (l > c.hi) {
       c.hi = l;
@@ -156,77 +199,33 @@ __global__ __launch_bounds__(kThreads) void range_kernel(SampleArgs a, Scratch s
     }
     if (l > -INFINITY) c.lo = fminf(c.lo, l);
   });
-  auto merge = [](Cell x, Cell y) {
-    const bool other = y.hi > x.hi || (y.hi == x.hi && y.at < x.at);
-    return Cell{other ? y.hi : x.hi, fminf(x.lo, y.lo), other ? y.at : x.at, x.bad | y.bad};
-  };
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1)
-    c = merge(c, Cell{__shfl_xor(c.hi, d), __shfl_xor(c.lo, d), __shfl_xor(c.at, d), __shfl_xor(c.bad, d)});
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = c;
+  c = merge_lanes<kWave>(c);
+  if ((threadIdx.x & 63) == 0) sh[w] = c;
   __syncthreads();
-  if (threadIdx.x == 0) {
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) c = merge(c, sh[w]);
-    sc.cells[(int64_t)row * a.segments + seg] = c;
+  if (threadIdx.x < kWaves) {
+    c = merge_lanes<kWaves>(sh[threadIdx.x]);
+    if (threadIdx.x == 0) sc.cells[(int64_t)row * a.segments + seg] = c;
   }
 }
 
+// Of the whole row, by every wavefront for itself.
 __device__ __forceinline__ Cell row_cell(const SampleArgs& a, const Scratch& sc, int row) {
-  Cell c = sc.cells[(int64_t)row * a.segments];
-  for (int s = 1; s < a.segments; ++s) {
-    const Cell y = sc.cells[(int64_t)row * a.segments + s];
-    if (y.hi > c.hi) {  // (the first of equal ones stays)
-      c.hi = y.hi;
-      c.at = y.at;
-    }
-    c.lo = fminf(c.lo, y.lo);
-    c.bad |= y.bad;
-  }
-  return c;
+  static_assert(kMaxSegments == 16, "four steps over the lanes");
+  const int s = min((int)threadIdx.x & (kMaxSegments - 1), a.segments - 1);
+  return merge_lanes<kMaxSegments>(sc.cells[(int64_t)row * a.segments + s]);
 }
 
 // ------------------------------------------------------------------ drawing
-// The smallest j in [from, to) whose running sum of f(l, j) exceeds t (from <= every j; t < the sum of all): the wavefronts
-// sum a run each, then the workgroup the one that holds it.
+// The smallest j in [from, to) at which base + the running sum of f(l, j) exceeds t (base <= t < base + the sum).
 template <class F>
-__device__ __forceinline__ int locate(const float* row, int from, int to, int64_t t, F f, int64_t* sh, int* shi) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int run = (to - from + kWaves - 1) / kWaves;
-  const int r0 = from + min(w * run, to - from), r1 = min(r0 + run, to);
-  int64_t s = 0;
-  for (int base = r0; base < r1; base += kWave * kBatch) {
-    float x[kBatch];
-#pragma unroll
-    for (int e = 0; e < kBatch; ++e) x[e] = row[min(base + e * kWave + lane, r1 - 1)];
-#pragma unroll
-    for (int e = 0; e < kBatch; ++e) {
-      const int j = base + e * kWave + lane;
-      if (j < r1) s += f(x[e], j);
-    }
-  }
-  s = wave_sum_i64(s);
-  __syncthreads();
-  if (lane == 0) sh[w] = s;
-  __syncthreads();
-  int mine = kWaves - 1;
-  int64_t before = 0;
-  for (int i = 0; i < kWaves; ++i) {
-    if (t < before + sh[i]) {
-      mine = i;
-      break;
-    }
-    before += sh[i];
-  }
-  const int b0 = from + min(mine * run, to - from), b1 = min(b0 + run, to);
-  __syncthreads();
-  // every thread a few consecutive tokens
-  const int per = (b1 - b0 + kThreads - 1) / kThreads;
-  const int p0 = b0 + min((int)threadIdx.x * per, b1 - b0), p1 = min(p0 + per, b1);
+__device__ __forceinline__ int locate_in(const float* row, int from, int to, int64_t base, int64_t t, F f, int64_t* sh,
+                                         int* shi) {
+  const int per = (to - from + kThreads - 1) / kThreads;  // consecutive tokens of a thread
+  const int p0 = from + min((int)threadIdx.x * per, to - from), p1 = min(p0 + per, to);
   int64_t part = 0;
   for (int j = p0; j < p1; ++j) part += f(row[j], j);
   int64_t total;
-  int64_t at = before + block_exclusive_scan_i64<kWaves>(part, sh, total);
+  int64_t at = base + block_exclusive_scan_i64<kWaves>(part, sh, total);
   if (part > 0 && at <= t && t < at + part) {
     int j = p0;
     for (; j < p1 - 1; ++j) {
@@ -239,21 +238,50 @@ __device__ __forceinline__ int locate(const float* row, int from, int to, int64_
   return *shi;
 }
 
+// The same over a row whose runs' sums are in LDS.
+template <class F>
+__device__ __forceinline__ int locate(const SampleArgs& a, const float* row, const int64_t* runs, int64_t t, F f, int64_t* sh,
+                                      int* shi) {
+  __shared__ int64_t base;
+  const int n = a.segments * kWaves;  // at most a thread each
+  const int64_t mine = (int)threadIdx.x < n ? runs[threadIdx.x] : 0;
+  int64_t total;
+  const int64_t at = block_exclusive_scan_i64<kWaves>(mine, sh, total);
+  if (mine > 0 && at <= t && t < at + mine) {
+    *shi = threadIdx.x;
+    base = at;
+  }
+  __syncthreads();
+  const int from = (int)min((int64_t)*shi * a.run, (int64_t)a.v), to = (int)min((int64_t)from + a.run, (int64_t)a.v);
+  const int64_t b = base;
+  __syncthreads();
+  return locate_in(row, from, to, b, t, f, sh, shi);
+}
+
+// Sums of f over the runs, to LDS; the wavefronts take them in turn.
+template <class F>
+__device__ __forceinline__ void sum_runs(const SampleArgs& a, const float* row, int64_t* runs, F f) {
+  __syncthreads();
+  for (int r = threadIdx.x >> 6; r < a.segments * kWaves; r += kWaves) {
+    int64_t s = 0;
+    each_of_run(a, row, r, [&](float l, int j) { s += f(l, j); });
+    s = wave_sum_i64(s);
+    if ((threadIdx.x & 63) == 0) runs[r] = s;
+  }
+  __syncthreads();
+}
+
 __device__ __forceinline__ int64_t draw_at(uint32_t u24, int64_t z) {  // floor(u z / 2^24)
   const int64_t u = u24 & 0xFFFFFF;
   return u * (z >> 24) + ((u * (z & 0xFFFFFF)) >> 24);
 }
 
-// A token of a row with the sums of R of its segments in seg_sum (LDS) and the weight f of a kept token.
+// A token of a row with the runs' sums in LDS and the weight f of a kept token.
 template <class F>
-__device__ __forceinline__ void draw(const SampleArgs& a, int row, const int64_t* seg_sum, F f, int64_t* sh, int* shi) {
-  int64_t z = 0;
-  for (int s = 0; s < a.segments; ++s) z += seg_sum[s];
-  int64_t t = draw_at(a.u24[row], z);
-  int seg = 0;
-  while (seg + 1 < a.segments && t >= seg_sum[seg]) t -= seg_sum[seg++];
-  const int from = seg * a.len, to = min(from + a.len, a.v);
-  const int j = locate(a.logits + row * a.ld, from, to, t, f, sh, shi);
+__device__ __forceinline__ void draw(const SampleArgs& a, int row, const int64_t* runs, F f, int64_t* sh, int* shi) {
+  const uint32_t u = a.u24[row];
+  const int64_t z = block_sum_i64<kWaves>((int)threadIdx.x < a.segments * kWaves ? runs[threadIdx.x] : 0, sh);
+  const int j = locate(a, a.logits + row * a.ld, runs, draw_at(u, z), f, sh, shi);
   if (threadIdx.x == 0) a.token[row] = j;
 }
 
@@ -266,7 +294,7 @@ __device__ __forceinline__ int64_t need_of(float top_p, int64_t z) {
 __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc) {
   __shared__ int64_t sums[kBins];
   __shared__ uint32_t counts[kBins];
-  __shared__ int64_t sh[kWaves], seg_sum[kMaxSegments];
+  __shared__ int64_t sh[kWaves], runs[kMaxRuns];
   __shared__ int shi;
   __shared__ Cut cut;
   const int row = blockIdx.x / a.segments, seg = blockIdx.x - row * a.segments, tid = threadIdx.x;
@@ -290,7 +318,6 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
     return;
   }
   const Weight wt(p.t, c.hi, a.shift);
-  const int from = seg * a.len, to = min(from + a.len, a.v);
   const bool by_count = p.top_k > 0, by_mass = p.top_p < 1.f;
   if (!by_count && !by_mass) {  // uniform: nothing to cut
     if (!a.token) {
@@ -302,19 +329,20 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
       }
       return;
     }
-    auto weight = [&](float l, int) {
+    auto weight = [&](float l, int) -> int64_t {
       const float w = wt.w(l);
       return w >= p.min_p ? wt.r(w) : 0;
     };
     int64_t s = 0;
-    each_token(logits, from, to, [&](float l, int j) { s += weight(l, j); });
-    s = block_sum_i64<kWaves>(s, sh);
-    if (tid == 0) publish(&sc.kept[(int64_t)row * a.segments + seg], s);
+    each_of_run(a, logits, seg * kWaves + (tid >> 6), [&](float l, int j) { s += weight(l, j); });
+    s = wave_sum_i64(s);
+    int64_t* kept = sc.kept + (int64_t)row * a.segments * kWaves;
+    if ((tid & 63) == 0) publish(&kept[seg * kWaves + (tid >> 6)], s);
     if (!last_of_row(&sc.counters[4 * (int64_t)row], a.segments, &shi)) return;
-    if (tid < a.segments) seg_sum[tid] = published(&sc.kept[(int64_t)row * a.segments + tid]);
+    if (tid < a.segments * kWaves) runs[tid] = published(&kept[tid]);
     if (tid == 0) sc.cuts[row].mode = kDone;
     __syncthreads();
-    draw(a, row, seg_sum, weight, sh, &shi);
+    draw(a, row, runs, weight, sh, &shi);
     return;
   }
   sums[tid] = 0;
@@ -322,7 +350,7 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
   __syncthreads();
   const double span = fmin((double)c.hi - (double)c.lo, kSpan * (double)p.t);
   const float scale = span > 0.0 ? (float)((double)kBins / span) : 0.f;
-  each_token(logits, from, to, [&](float l, int) {
+  each_of_run(a, logits, seg * kWaves + (tid >> 6), [&](float l, int) {
     const int b = bin_of(c.hi, scale, l);
     if (by_count) atomicAdd(&counts[b], 1u);
     if (by_mass) {
@@ -333,14 +361,17 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
   __syncthreads();
   const int64_t slice = (int64_t)row * a.segments * kBins;
   if (by_mass) publish(&sc.sums[slice + seg * kBins + tid], sums[tid]);
-  if (by_count) publish(&sc.counts[slice + seg * kBins + tid], counts[tid]);
+  if (by_count)
+    __hip_atomic_store(&sc.counts[slice + seg * kBins + tid], (int32_t)counts[tid], __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
   if (!last_of_row(&sc.counters[4 * (int64_t)row], a.segments, &shi)) return;
   // the row's last workgroup: a thread a bin
   int64_t mass = 0, n = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int s = 0; s < a.segments; ++s) {
     if (by_mass) mass += published(&sc.sums[slice + s * kBins + tid]);
-    if (by_count) n += published(&sc.counts[slice + s * kBins + tid]);
+    if (by_count)
+      n += __hip_atomic_load(&sc.counts[slice + s * kBins + tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   int64_t all, tokens;
   const int64_t m0 = block_exclusive_scan_i64<kWaves>(mass, sh, all);
@@ -390,16 +421,10 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
 }
 
 // ------------------------------------------------------------------- step 3
-// The cuts of a whole row by radix selection, one workgroup.
-struct RadixCut {
-  float last;
-  int last_at;
-};
-
 // The key K (descending order) where the running sum of f over keys passes `target` (>= 1): before K it is less, with K's
 // own tokens it is not.  `passed`: the sum before K.
 template <class F>
-__device__ uint32_t radix_key(const float* row, int v, int64_t target, F f, int64_t* hist, int64_t* sh, int* shi,
+__device__ uint32_t radix_key(const SampleArgs& a, const float* row, int64_t target, F f, int64_t* hist, int64_t* sh, int* shi,
                               int64_t& passed) {
   uint32_t prefix = 0;
   passed = 0;
@@ -409,7 +434,7 @@ __device__ uint32_t radix_key(const float* row, int v, int64_t target, F f, int6
     __syncthreads();
     for (int i = threadIdx.x; i < 2048; i += kThreads) hist[i] = 0;
     __syncthreads();
-    each_token(row, 0, v, [&](float l, int j) {
+    each_of_row(a, row, [&](float l, int j) {
       const uint32_t k = key_of(l);
       if (pass > 0 && (k >> (low + bits)) != prefix) return;
       const int64_t x = f(l, j);
@@ -435,22 +460,75 @@ __device__ uint32_t radix_key(const float* row, int v, int64_t target, F f, int6
   return prefix;
 }
 
+// The token of those that the threads hold at which base + the running sum of val, in the order, reaches `target`: their
+// bins (-1: not in question) are a monotone function of the order, so the sum is followed through the bins and then through
+// the tokens of one.  False where those are too many.
+struct Picked {
+  int64_t val[kFew], sum;
+  float l[kFew], last;
+  int j[kFew], bin, n, at;
+};
+__device__ __forceinline__ bool pick(const float (&l)[kHeld], const int (&j)[kHeld], const int (&bin)[kHeld],
+                                     const int64_t (&val)[kHeld], int64_t base, int64_t target, int64_t* hist, int64_t* sh,
+                                     Picked& p) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  hist[tid] = 0;
+  if (tid == 0) p.n = 0;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kHeld; ++e)
+    if (bin[e] >= 0) atomicAdd((unsigned long long*)&hist[bin[e]], (unsigned long long)val[e]);
+  __syncthreads();
+  const int64_t h = hist[tid];
+  int64_t total;
+  const int64_t at = base + block_exclusive_scan_i64<kWaves>(h, sh, total);
+  if (at < target && target <= at + h) {
+    p.bin = tid;
+    p.sum = at;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kHeld; ++e) {
+    if (bin[e] != p.bin) continue;
+    const int slot = atomicAdd(&p.n, 1);
+    if (slot < kFew) {
+      p.l[slot] = l[e];
+      p.j[slot] = j[e];
+      p.val[slot] = val[e];
+    }
+  }
+  __syncthreads();
+  const int n = p.n;
+  if (n > kFew) return false;  // uniform
+  if (tid < n) {
+    int64_t before = p.sum;
+    for (int i = 0; i < n; ++i)
+      if (i != tid && up_to(p.l[i], p.j[i], p.l[tid], p.j[tid])) before += p.val[i];
+    if (before < target && target <= before + p.val[tid]) {
+      p.last = p.l[tid];
+      p.at = p.j[tid];
+    }
+  }
+  __syncthreads();
+  return true;
+}
+
 __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc) {
-  __shared__ __align__(16) int64_t lr[kMost];  // weights of the gathered tokens; the histogram of a radix pass
-  __shared__ float ll[kMost];
-  __shared__ int lj[kMost], lkeep[kMost];
-  __shared__ int64_t sh[kWaves], seg_sum[kMaxSegments], z1;
-  __shared__ int shi, most_at;
+  __shared__ __align__(16) int64_t list[kMost];  // gathered by this workgroup; then histograms
+  __shared__ Picked pk;
+  __shared__ int64_t sh[kWaves], runs[kMaxRuns];
+  __shared__ int shi, found;
   const int row = blockIdx.x / a.segments, seg = blockIdx.x - row * a.segments, tid = threadIdx.x;
   const Cut cut = sc.cuts[row];
   const Params p(a, row);
   if (cut.mode != kCut || p.t == 0.f || p.bad) return;  // uniform
   const float* logits = a.logits + row * a.ld;
   const Weight wt(p.t, cut.hi, a.shift);
-  const int from = seg * a.len, to = min(from + a.len, a.v);
-  int32_t* gathered = &sc.counters[4 * (int64_t)row + 2];
+  if (tid == 0) found = 0;
+  __syncthreads();
   int64_t s = 0;
-  each_token(logits, from, to, [&](float l, int j) {
+  each_of_run(a, logits, seg * kWaves + (tid >> 6), [&](float l, int j) {
     const int b = bin_of(cut.hi, cut.scale, l);
     if (b < cut.sure) {
       if (a.token) {
@@ -458,100 +536,140 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
         s += w >= p.min_p ? wt.r(w) : 0;
       }
     } else if (b == cut.bk || (b >= cut.g0 && b <= cut.g1)) {
-      const int at = __hip_atomic_fetch_add(gathered, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (at < kMost)
-        publish(&sc.list[(int64_t)row * kMost + at], (int64_t)j << 32 | __builtin_bit_cast(uint32_t, l));
+      const int at = atomicAdd(&found, 1);
+      if (at < kMost) list[at] = (int64_t)j << 32 | __builtin_bit_cast(uint32_t, l);
     }
   });
-  s = block_sum_i64<kWaves>(s, sh);
-  if (tid == 0) publish(&sc.kept[(int64_t)row * a.segments + seg], s);
+  s = wave_sum_i64(s);
+  int64_t* kept = sc.kept + (int64_t)row * a.segments * kWaves;
+  if ((tid & 63) == 0) publish(&kept[seg * kWaves + (tid >> 6)], s);
+  __syncthreads();
+  int32_t* gathered = &sc.counters[4 * (int64_t)row + 2];
+  const int mine = found;
+  if (tid == 0 && mine > 0) shi = __hip_atomic_fetch_add(gathered, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  for (int i = tid; i < mine && shi + i < kMost; i += kThreads) publish(&sc.list[(int64_t)row * kMost + shi + i], list[i]);
+  __syncthreads();
   if (!last_of_row(&sc.counters[4 * (int64_t)row + 1], a.segments, &shi)) return;
-  if (tid < a.segments) seg_sum[tid] = published(&sc.kept[(int64_t)row * a.segments + tid]);
+  if (tid < a.segments * kWaves) runs[tid] = published(&kept[tid]);
   const int n = __hip_atomic_load(gathered, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const bool by_mass = p.top_p < 1.f;
-  float last = INFINITY;
+  float last = INFINITY;  // the last kept token; of the bins below `sure` alone where none of the gathered ones is
   int last_at = -1;
-  int sure = cut.sure;
-  if (n <= kMost) {  // uniform: rank them
-    for (int i = tid; i < n; i += kThreads) {
-      const int64_t x = published(&sc.list[(int64_t)row * kMost + i]);
-      ll[i] = __builtin_bit_cast(float, (uint32_t)x);
-      lj[i] = (int)(x >> 32);
-      lr[i] = wt.r(wt.w(ll[i]));
-    }
-    __syncthreads();
-    auto ahead = [&](int i, int j) { return i != j && up_to(ll[j], lj[j], ll[i], lj[i]); };
-    auto bin = [&](int i) { return bin_of(cut.hi, cut.scale, ll[i]); };
-    // top-k: what it keeps of its bin, and their weights
-    int64_t part = 0;
-    for (int i = tid; i < n; i += kThreads) {
-      int keep = 1;
-      if (cut.bk >= 0 && bin(i) == cut.bk) {
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += bin(j) == cut.bk && ahead(i, j) ? 1 : 0;
-        keep = rank < cut.rk;
-        if (keep) part += lr[i];
-      }
-      lkeep[i] = keep;
-    }
-    part = block_sum_i64<kWaves>(part, sh);
-    if (tid == 0) z1 = cut.before_k + part;
-    __syncthreads();
-    if (by_mass) {
-      const int64_t need = need_of(p.top_p, z1);
-      bool in[kMost / kThreads];
+  bool settled = n <= kMost;
+  if (settled) {
+    float l[kHeld];
+    int j[kHeld], b[kHeld], bin[kHeld];
+    int64_t r[kHeld], val[kHeld];
 #pragma unroll
-      for (int x = 0; x < kMost / kThreads; ++x) {
-        const int i = tid + x * kThreads;
-        in[x] = false;
-        if (i >= n || !lkeep[i] || bin(i) > cut.g1) continue;
-        int64_t before = cut.before;
-        for (int j = 0; j < n; ++j) before += lkeep[j] && ahead(i, j) ? lr[j] : 0;
-        in[x] = before < need;
+    for (int e = 0; e < kHeld; ++e) {
+      const int i = tid + e * kThreads;
+      b[e] = -1;
+      l[e] = -INFINITY;
+      j[e] = 0;
+      r[e] = 0;
+      if (i < n) {
+        const int64_t x = published(&sc.list[(int64_t)row * kMost + i]);
+        l[e] = __builtin_bit_cast(float, (uint32_t)x);
+        j[e] = (int)(x >> 32);
+        b[e] = bin_of(cut.hi, cut.scale, l[e]);
+        r[e] = wt.r(wt.w(l[e]));
       }
+    }
+    // the place of a token in its bin, in kBins steps
+    auto place = [&](int e) {
+      const float x = ((cut.hi - l[e]) * cut.scale - (float)b[e]) * (float)kBins;
+      return (int)fminf(fmaxf(x, 0.f), (float)(kBins - 1));
+    };
+    if (cut.bk >= 0) {
+#pragma unroll
+      for (int e = 0; e < kHeld; ++e) {
+        bin[e] = b[e] == cut.bk ? place(e) : -1;
+        val[e] = 1;
+      }
+      settled = pick(l, j, bin, val, 0, cut.rk, list, sh, pk);
+      if (settled) {
+        last = pk.last;
+        last_at = pk.at;
+      }
+    }
+    if (settled && by_mass) {
+      int64_t part = 0;
+#pragma unroll
+      for (int e = 0; e < kHeld; ++e) {
+        if (cut.bk >= 0 && b[e] == cut.bk) {
+          if (up_to(l[e], j[e], last, last_at))
+            part += r[e];
+          else
+            b[e] = -1;  // dropped by top-k
+        }
+      }
+      part = block_sum_i64<kWaves>(part, sh);
+      const int64_t need = need_of(p.top_p, cut.before_k + part);
+      // its bin, where it may be one of several: the sums of the gathered bins
+      int at_bin = cut.g0;
+      int64_t base = cut.before;
+      if (cut.g1 > cut.g0) {
+        list[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e)
+          if (b[e] >= cut.g0 && b[e] <= cut.g1) atomicAdd((unsigned long long*)&list[b[e]], (unsigned long long)r[e]);
+        __syncthreads();
+        const int64_t h = list[tid];
+        int64_t total;
+        const int64_t at = base + block_exclusive_scan_i64<kWaves>(h, sh, total);
+        if (at < need && need <= at + h) {
+          shi = tid;
+          pk.sum = at;
+        }
+        __syncthreads();
+        at_bin = shi;
+        base = pk.sum;
+      }
+#pragma unroll
+      for (int e = 0; e < kHeld; ++e) bin[e] = b[e] == at_bin ? place(e) : -1;
+      settled = pick(l, j, bin, r, base, need, list, sh, pk);
+      if (settled) {
+        last = pk.last;
+        last_at = pk.at;
+      }
+    }
+    if (settled && a.token) {  // the kept ones' weights to their runs
       __syncthreads();
 #pragma unroll
-      for (int x = 0; x < kMost / kThreads; ++x)
-        if (tid + x * kThreads < n) lkeep[tid + x * kThreads] = in[x];
+      for (int e = 0; e < kHeld; ++e) {
+        if (tid + e * kThreads < n && up_to(l[e], j[e], last, last_at) && wt.w(l[e]) >= p.min_p)
+          atomicAdd((unsigned long long*)&runs[j[e] / a.run], (unsigned long long)r[e]);
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    // the last one kept, and the kept weights by segment
-    if (tid == 0) most_at = -1;
-    __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      if (!lkeep[i]) continue;
-      bool final = true;
-      for (int j = 0; j < n; ++j) final = final && !(lkeep[j] && ahead(j, i));
-      if (final) most_at = i;
-      const float w = wt.w(ll[i]);
-      if (w >= p.min_p) atomicAdd((unsigned long long*)&seg_sum[lj[i] / a.len], (unsigned long long)lr[i]);
-    }
-    __syncthreads();
-    if (most_at >= 0) {
-      last = ll[most_at];
-      last_at = lj[most_at];
-    }
-  } else {
-    // too many to rank: the cuts from the whole row
+  }
+  int sure = cut.sure;
+  if (!settled) {  // uniform: the cuts from the whole row
     sure = 0;
     int64_t passed;
     uint32_t key = 0xFFFFFFFFu;
     int at = INT_MAX;
     if (p.top_k > 0) {
-      key = radix_key(logits, a.v, p.top_k, [](float, int) { return (int64_t)1; }, lr, sh, &shi, passed);
-      at = locate(logits, 0, a.v, p.top_k - passed - 1, [&](float l, int) { return (int64_t)(key_of(l) == key); }, sh, &shi);
+      key = radix_key(a, logits, p.top_k, [](float, int) { return (int64_t)1; }, list, sh, &shi, passed);
+      auto tie = [&](float l, int) { return (int64_t)(key_of(l) == key); };
+      sum_runs(a, logits, runs, tie);
+      at = locate(a, logits, runs, p.top_k - passed - 1, tie, sh, &shi);
     }
-    auto by_k = [&](float l, int j) { return key_of(l) < key || (key_of(l) == key && j <= at); };
     if (by_mass) {
-      auto weight = [&](float l, int j) { return by_k(l, j) ? wt.r(wt.w(l)) : 0; };
+      auto weight = [&](float l, int j) -> int64_t {
+        const uint32_t k = key_of(l);
+        return k < key || (k == key && j <= at) ? wt.r(wt.w(l)) : 0;
+      };
       int64_t z = 0;
-      each_token(logits, 0, a.v, [&](float l, int j) { z += weight(l, j); });
+      each_of_row(a, logits, [&](float l, int j) { z += weight(l, j); });
       z = block_sum_i64<kWaves>(z, sh);
       const int64_t need = need_of(p.top_p, z);
-      const uint32_t kp = radix_key(logits, a.v, need, weight, lr, sh, &shi, passed);
-      // tokens of one key weigh the same: the sum passes need with the first of them at which (running sum) >= need
-      at = locate(logits, 0, a.v, need - passed - 1,
-                  [&](float l, int j) { return key_of(l) == kp ? weight(l, j) : 0; }, sh, &shi);
+      const uint32_t kp = radix_key(a, logits, need, weight, list, sh, &shi, passed);
+      auto tie = [&](float l, int j) { return key_of(l) == kp ? weight(l, j) : 0; };
+      sum_runs(a, logits, runs, tie);
+      at = locate(a, logits, runs, need - passed - 1, tie, sh, &shi);
       key = kp;
     }
     last = __builtin_bit_cast(float, (key >> 31) ? key : ~(key | 0x80000000u));
@@ -570,16 +688,8 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
     const float w = wt.w(l);
     return w >= p.min_p ? wt.r(w) : 0;
   };
-  if (n > kMost) {  // the segments' sums anew
-    for (int g = 0; g < a.segments; ++g) {
-      int64_t z = 0;
-      each_token(logits, g * a.len, min((g + 1) * a.len, a.v), [&](float l, int j) { z += weight(l, j); });
-      z = block_sum_i64<kWaves>(z, sh);
-      if (tid == 0) seg_sum[g] = z;
-    }
-    __syncthreads();
-  }
-  draw(a, row, seg_sum, weight, sh, &shi);
+  if (!settled) sum_runs(a, logits, runs, weight);
+  draw(a, row, runs, weight, sh, &shi);
 }
 
 // ------------------------------------------------------------------- step 4
@@ -587,11 +697,10 @@ __global__ __launch_bounds__(kThreads) void filter_kernel(SampleArgs a, Scratch 
   const int row = blockIdx.x / a.segments, seg = blockIdx.x - row * a.segments;
   const Cut cut = sc.cuts[row];
   const Params p(a, row);
-  const int from = seg * a.len, to = min(from + a.len, a.v);
   float* out = a.out + row * a.ld;
   const bool greedy = p.t == 0.f;
   const Weight wt(greedy ? 1.f : p.t, cut.hi, a.shift);
-  each_token(a.logits + row * a.ld, from, to, [&](float l, int j) {
+  each_of_run(a, a.logits + row * a.ld, seg * kWaves + (threadIdx.x >> 6), [&](float l, int j) {
     bool keep = true;
     if (cut.mode == kCut) keep = greedy ? j == cut.last_at
                                         : bin_of(cut.hi, cut.scale, l) < cut.sure || up_to(l, j, cut.last, cut.last_at);
@@ -600,7 +709,7 @@ __global__ __launch_bounds__(kThreads) void filter_kernel(SampleArgs a, Scratch 
   });
 }
 
-constexpr int kRowsAtOnce = 1024;  // rows whose scratch is held at once
+constexpr int kRowsAtOnce = 512;  // rows whose scratch is held at once
 
 size_t rounded(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -612,15 +721,14 @@ hipError_t launch_sample(const float* logits, int m, int v, int64_t ld, const fl
   const int rows = m < kRowsAtOnce ? m : kRowsAtOnce;
   SampleArgs a{logits, v, ld, temperature, top_p, min_p, top_k, u24, token, out, status, 1, v, 62};
   while (a.shift > 0 && (int64_t(1) << (62 - a.shift)) < v) --a.shift;
-  // segments: a workgroup a CU over all rows, none shorter than pays
-  int segments = (cu_count() + rows - 1) / rows;
+  // segments: two workgroups a CU over all rows, none shorter than pays
+  int segments = (2 * cu_count() + rows - 1) / rows;
   const int most = (v + kMinSegment - 1) / kMinSegment;
   segments = segments > kMaxSegments ? kMaxSegments : segments;
   a.segments = segments > most ? most : segments;
-  a.len = (v + a.segments - 1) / a.segments;
-  a.segments = (v + a.len - 1) / a.len;
+  a.run = (v + a.segments * kWaves - 1) / (a.segments * kWaves);
   const size_t rs = (size_t)rows * a.segments;
-  const size_t bytes[] = {rs * sizeof(Cell),      rs * kBins * 8,         rs * 8,          rs * kBins * 8,
+  const size_t bytes[] = {rs * sizeof(Cell),        rs * kBins * 8,             rs * kWaves * 8,  rs * kBins * 4,
                           (size_t)rows * kMost * 8, (size_t)rows * sizeof(Cut), (size_t)rows * 16};
   size_t total = 0;
   for (size_t n : bytes) total += rounded(n);
@@ -637,7 +745,7 @@ hipError_t launch_sample(const float* logits, int m, int v, int64_t ld, const fl
   sc.cells = reinterpret_cast<Cell*>(take(0));
   sc.sums = reinterpret_cast<int64_t*>(take(1));
   sc.kept = reinterpret_cast<int64_t*>(take(2));
-  sc.counts = reinterpret_cast<int64_t*>(take(3));
+  sc.counts = reinterpret_cast<int32_t*>(take(3));
   sc.list = reinterpret_cast<int64_t*>(take(4));
   sc.cuts = reinterpret_cast<Cut*>(take(5));
   sc.counters = reinterpret_cast<int32_t*>(take(6));
