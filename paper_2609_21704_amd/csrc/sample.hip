@@ -30,7 +30,8 @@ constexpr int kBins = kThreads;   // one a thread where they are scanned
 constexpr int kHeld = 4;          // gathered tokens a thread holds
 constexpr int kMost = kHeld * kThreads;
 constexpr int kFew = 512;         // tokens that are ranked against each other
-constexpr int kMaxSegments = 16;  // of a row
+constexpr int kDirect = 96;       // gathered ones that are, without bins of theirs
+constexpr int kMaxSegments = 32;  // of a row
 constexpr int kMaxRuns = kMaxSegments * kWaves;
 constexpr int kMinSegment = 4096; // tokens
 constexpr double kSpan = 32.0;    // nats below the maximum that the bins cover (e^-32 < 2^-46)
@@ -210,7 +211,6 @@ __global__ __launch_bounds__(kThreads) void range_kernel(SampleArgs a, Scratch s
 
 // Of the whole row, by every wavefront for itself.
 __device__ __forceinline__ Cell row_cell(const SampleArgs& a, const Scratch& sc, int row) {
-  static_assert(kMaxSegments == 16, "four steps over the lanes");
   const int s = min((int)threadIdx.x & (kMaxSegments - 1), a.segments - 1);
   return merge_lanes<kMaxSegments>(sc.cells[(int64_t)row * a.segments + s]);
 }
@@ -291,6 +291,20 @@ __device__ __forceinline__ int64_t need_of(float top_p, int64_t z) {
   return n < 1 ? 1 : n;
 }
 
+// The sum of part(s) over the segments, sixteen loads in flight.
+template <class F>
+__device__ __forceinline__ int64_t slices(int segments, F part) {
+  int64_t sum = 0;
+  for (int s0 = 0; s0 < segments; s0 += 16) {
+    int64_t x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = part(min(s0 + i, segments - 1));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += s0 + i < segments ? x[i] : 0;
+  }
+  return sum;
+}
+
 __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc) {
   __shared__ int64_t sums[kBins];
   __shared__ uint32_t counts[kBins];
@@ -367,11 +381,13 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
   if (!last_of_row(&sc.counters[4 * (int64_t)row], a.segments, &shi)) return;
   // the row's last workgroup: a thread a bin
   int64_t mass = 0, n = 0;
-#pragma unroll 8
-  for (int s = 0; s < a.segments; ++s) {
-    if (by_mass) mass += published(&sc.sums[slice + s * kBins + tid]);
-    if (by_count)
-      n += __hip_atomic_load(&sc.counts[slice + s * kBins + tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (by_mass) {
+    mass = slices(a.segments, [&](int s) { return published(&sc.sums[slice + s * kBins + tid]); });
+  }
+  if (by_count) {
+    n = slices(a.segments, [&](int s) -> int64_t {
+      return __hip_atomic_load(&sc.counts[slice + s * kBins + tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
   }
   int64_t all, tokens;
   const int64_t m0 = block_exclusive_scan_i64<kWaves>(mass, sh, all);
@@ -469,28 +485,34 @@ struct Picked {
   int j[kFew], bin, n, at;
 };
 __device__ __forceinline__ bool pick(const float (&l)[kHeld], const int (&j)[kHeld], const int (&bin)[kHeld],
-                                     const int64_t (&val)[kHeld], int64_t base, int64_t target, int64_t* hist, int64_t* sh,
-                                     Picked& p) {
+                                     const int64_t (&val)[kHeld], int held, int64_t base, int64_t target, int64_t* hist,
+                                     int64_t* sh, Picked& p) {
   const int tid = threadIdx.x;
   __syncthreads();
-  hist[tid] = 0;
-  if (tid == 0) p.n = 0;
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < kHeld; ++e)
-    if (bin[e] >= 0) atomicAdd((unsigned long long*)&hist[bin[e]], (unsigned long long)val[e]);
-  __syncthreads();
-  const int64_t h = hist[tid];
-  int64_t total;
-  const int64_t at = base + block_exclusive_scan_i64<kWaves>(h, sh, total);
-  if (at < target && target <= at + h) {
-    p.bin = tid;
-    p.sum = at;
+  const bool few = held <= kDirect;  // uniform: all of them are ranked
+  if (!few) hist[tid] = 0;
+  if (tid == 0) {
+    p.n = 0;
+    p.sum = base;
   }
   __syncthreads();
+  if (!few) {
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+      if (bin[e] >= 0) atomicAdd((unsigned long long*)&hist[bin[e]], (unsigned long long)val[e]);
+    __syncthreads();
+    const int64_t h = hist[tid];
+    int64_t total;
+    const int64_t at = base + block_exclusive_scan_i64<kWaves>(h, sh, total);
+    if (at < target && target <= at + h) {
+      p.bin = tid;
+      p.sum = at;
+    }
+    __syncthreads();
+  }
 #pragma unroll
   for (int e = 0; e < kHeld; ++e) {
-    if (bin[e] != p.bin) continue;
+    if (few ? bin[e] < 0 : bin[e] != p.bin) continue;
     const int slot = atomicAdd(&p.n, 1);
     if (slot < kFew) {
       p.l[slot] = l[e];
@@ -587,7 +609,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
         bin[e] = b[e] == cut.bk ? place(e) : -1;
         val[e] = 1;
       }
-      settled = pick(l, j, bin, val, 0, cut.rk, list, sh, pk);
+      settled = pick(l, j, bin, val, n, 0, cut.rk, list, sh, pk);
       if (settled) {
         last = pk.last;
         last_at = pk.at;
@@ -629,7 +651,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
       }
 #pragma unroll
       for (int e = 0; e < kHeld; ++e) bin[e] = b[e] == at_bin ? place(e) : -1;
-      settled = pick(l, j, bin, r, base, need, list, sh, pk);
+      settled = pick(l, j, bin, r, n, base, need, list, sh, pk);
       if (settled) {
         last = pk.last;
         last_at = pk.at;
