@@ -98,13 +98,32 @@ struct Params {
   }
 };
 
-// The weight of a logit, and on the grid.
+// The weight of a logit, and on the grid: exp((l - hi) / T) = 2^y with y = (l - hi) log2(e) / T in fp64, split into a whole
+// number and |f| <= 1/2; 2^f = 1 + f Q(f), Q of degree 7 by Remez exchange on the relative error (2^-39.8), which is exactly 1
+// at the maximum; one rounding to fp32, off by 2^-15 of half a step more than the nearest.
 struct Weight {
-  Soft<false> sf;
-  double zmax;
+  double hi, c, q[8], magic;
   int shift;
-  __device__ __forceinline__ Weight(float t, float hi, int shift) : sf(t), zmax(sf.z(hi)), shift(shift) {}
-  __device__ __forceinline__ float w(float l) const { return (float)sf.exp(sf.z(l) - zmax); }
+  __device__ __forceinline__ Weight(float t, float hi, int shift)
+      : hi(hi),
+        c(0x1.71547652b82fep+0 / (double)t),
+        q{0x1.63d13637ddc42p-20, 0x1.00dc4a532dcb6p-16, 0x1.4308ac85a9890p-13, 0x1.5d8745a728475p-10,
+          0x1.3b2ab7181b75cp-7,  0x1.c6b08dd6fd234p-5,  0x1.ebfbdff823cedp-3,  0x1.62e42fef84cf0p-1},
+        magic(0x1.8p52),
+        shift(shift) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("" : "+v"(q[i]));
+  }
+  __device__ __forceinline__ float w(float l) const {
+    const double y = fmax(((double)l - hi) * c, -2000.0);  // (-inf too)
+    const double k = y + magic;  // rint(y) in the low mantissa bits
+    const double f = y - (k - magic);
+    double p = q[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) p = __builtin_fma(p, f, q[i]);
+    p = __builtin_fma(p, f, 1.0);
+    return ldexpf((float)p, (int)(uint32_t)__builtin_bit_cast(uint64_t, k));
+  }
   // rint(w 2^shift), ties to even, from the bits of w in [0, 1]
   __device__ __forceinline__ int64_t r(float w) const {
     const uint32_t u = __builtin_bit_cast(uint32_t, w);
