@@ -27,7 +27,7 @@ namespace {
 constexpr int32_t kNoDist = 8, kBadParam = 256;  // the SQ_DEV_* values of the C headers
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kBins = kThreads;   // one a thread where they are scanned
-constexpr int kHeld = 4;          // gathered tokens a thread holds
+constexpr int kHeld = 2;          // gathered tokens a thread holds
 constexpr int kMost = kHeld * kThreads;
 constexpr int kFew = 512;         // tokens that are ranked against each other
 constexpr int kDirect = 96;       // gathered ones that are, without bins of theirs
@@ -149,27 +149,24 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 // `last`, `at` in (and everything before it in the order) against (l, j)
 __device__ __forceinline__ bool up_to(float l, int j, float last, int at) { return l > last || (l == last && j <= at); }
 
-// f(l, j) for the tokens from .. to, of which a wavefront (stride 64) or the workgroup takes every stride-th; kBatch loads
-// a thread in flight while the batch before is worked on.
-constexpr int kBatch = 4;
+// f(l, j) for the tokens from .. to, of which a wavefront (stride 64) or the workgroup takes every stride-th, kAhead loads
+// ahead of their use.  f's code stands there once: a workgroup runs through these kernels' code a few times only, and
+// fetching it is a part of their time.
+constexpr int kAhead = 6;
 template <class F>
 __device__ __forceinline__ void each_token(const float* row, int from, int to, int first, int stride, F f) {
   if (from >= to) return;
-  float x[kBatch], y[kBatch];
-  auto load = [&](int base, float (&v)[kBatch]) {
+  int j = from + first;
+  float x[kAhead];
 #pragma unroll
-    for (int e = 0; e < kBatch; ++e) v[e] = row[min(base + e * stride + first, to - 1)];
-  };
-  load(from, x);
-  for (int base = from; base < to; base += stride * kBatch) {  // uniform
-    if (base + stride * kBatch < to) load(base + stride * kBatch, y);
+  for (int e = 0; e < kAhead; ++e) x[e] = row[min(j + e * stride, to - 1)];
+#pragma unroll 1
+  for (; j < to; j += stride) {
+    const float now = x[0];
 #pragma unroll
-    for (int e = 0; e < kBatch; ++e) {
-      const int j = base + e * stride + first;
-      if (j < to) f(x[e], j);
-    }
-#pragma unroll
-    for (int e = 0; e < kBatch; ++e) x[e] = y[e];
+    for (int e = 0; e + 1 < kAhead; ++e) x[e] = x[e + 1];
+    x[kAhead - 1] = row[min(j + kAhead * stride, to - 1)];
+    f(now, j);
   }
 }
 // ... of this wavefront's run of a segment
@@ -182,6 +179,33 @@ __device__ __forceinline__ void each_of_run(const SampleArgs& a, const float* ro
 template <class F>
 __device__ __forceinline__ void each_of_row(const SampleArgs& a, const float* row, F f) {
   each_token(row, 0, a.v, threadIdx.x, kThreads, f);
+}
+
+// Exclusive prefix sum over the workgroup in thread order, and the workgroup's sum: as the acceptance's, but the wavefronts'
+// sums are scanned over the lanes, in a third of the code.
+__device__ __forceinline__ int64_t lane_of(int64_t v, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t scan(int64_t v, int64_t* sh, int64_t& total) {
+  static_assert(kWaves == 16, "a row of lanes");
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t x = wave_scan_i64(v);
+  if (lane == 63) sh[w] = x;
+  __syncthreads();
+  int64_t y = sh[lane & 15];
+  y += dpp_move<0x111>(y);  // row_shr:1
+  y += dpp_move<0x112>(y);
+  y += dpp_move<0x114>(y);
+  y += dpp_move<0x118>(y);
+  __syncthreads();
+  total = lane_of(y, 15);
+  return x - v + (w ? lane_of(y, w - 1) : 0);
+}
+__device__ __forceinline__ int64_t sum_of(int64_t v, int64_t* sh) {
+  int64_t total;
+  scan(v, sh, total);
+  return total;
 }
 
 // True in every thread of the row's last workgroup to arrive, after whose return it sees what all of them published.
@@ -244,7 +268,7 @@ __device__ __forceinline__ int locate_in(const float* row, int from, int to, int
   int64_t part = 0;
   for (int j = p0; j < p1; ++j) part += f(row[j], j);
   int64_t total;
-  int64_t at = base + block_exclusive_scan_i64<kWaves>(part, sh, total);
+  int64_t at = base + scan(part, sh, total);
   if (part > 0 && at <= t && t < at + part) {
     int j = p0;
     for (; j < p1 - 1; ++j) {
@@ -265,7 +289,7 @@ __device__ __forceinline__ int locate(const SampleArgs& a, const float* row, con
   const int n = a.segments * kWaves;  // at most a thread each
   const int64_t mine = (int)threadIdx.x < n ? runs[threadIdx.x] : 0;
   int64_t total;
-  const int64_t at = block_exclusive_scan_i64<kWaves>(mine, sh, total);
+  const int64_t at = scan(mine, sh, total);
   if (mine > 0 && at <= t && t < at + mine) {
     *shi = threadIdx.x;
     base = at;
@@ -299,7 +323,7 @@ __device__ __forceinline__ int64_t draw_at(uint32_t u24, int64_t z) {  // floor(
 template <class F>
 __device__ __forceinline__ void draw(const SampleArgs& a, int row, const int64_t* runs, F f, int64_t* sh, int* shi) {
   const uint32_t u = a.u24[row];
-  const int64_t z = block_sum_i64<kWaves>((int)threadIdx.x < a.segments * kWaves ? runs[threadIdx.x] : 0, sh);
+  const int64_t z = sum_of((int)threadIdx.x < a.segments * kWaves ? runs[threadIdx.x] : 0, sh);
   const int j = locate(a, a.logits + row * a.ld, runs, draw_at(u, z), f, sh, shi);
   if (threadIdx.x == 0) a.token[row] = j;
 }
@@ -324,7 +348,8 @@ __device__ __forceinline__ int64_t slices(int segments, F part) {
   return sum;
 }
 
-__global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc) {
+// (eight wavefronts a SIMD, two workgroups a CU: 27.6 us for 34.7 at 64 rows of 151936 logits)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8, 8))) void bins_kernel(SampleArgs a, Scratch sc) {
   __shared__ int64_t sums[kBins];
   __shared__ uint32_t counts[kBins];
   __shared__ int64_t sh[kWaves], runs[kMaxRuns];
@@ -409,8 +434,8 @@ __global__ __launch_bounds__(kThreads) void bins_kernel(SampleArgs a, Scratch sc
     });
   }
   int64_t all, tokens;
-  const int64_t m0 = block_exclusive_scan_i64<kWaves>(mass, sh, all);
-  const int64_t n0 = block_exclusive_scan_i64<kWaves>(n, sh, tokens);
+  const int64_t m0 = scan(mass, sh, all);
+  const int64_t n0 = scan(n, sh, tokens);
   if (tid == 0) {
     cut = {};
     cut.mode = kCut;
@@ -478,7 +503,7 @@ __device__ uint32_t radix_key(const SampleArgs& a, const float* row, int64_t tar
     __syncthreads();
     const int64_t x0 = hist[2 * threadIdx.x], x1 = hist[2 * threadIdx.x + 1];
     int64_t total;
-    const int64_t at = passed + block_exclusive_scan_i64<kWaves>(x0 + x1, sh, total);
+    const int64_t at = passed + scan(x0 + x1, sh, total);
     __shared__ int64_t found;
     if (at < target && target <= at + x0) {
       *shi = 2 * threadIdx.x;
@@ -522,7 +547,7 @@ __device__ __forceinline__ bool pick(const float (&l)[kHeld], const int (&j)[kHe
     __syncthreads();
     const int64_t h = hist[tid];
     int64_t total;
-    const int64_t at = base + block_exclusive_scan_i64<kWaves>(h, sh, total);
+    const int64_t at = base + scan(h, sh, total);
     if (at < target && target <= at + h) {
       p.bin = tid;
       p.sum = at;
@@ -645,7 +670,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
             b[e] = -1;  // dropped by top-k
         }
       }
-      part = block_sum_i64<kWaves>(part, sh);
+      part = sum_of(part, sh);
       const int64_t need = need_of(p.top_p, cut.before_k + part);
       // its bin, where it may be one of several: the sums of the gathered bins
       int at_bin = cut.g0;
@@ -659,7 +684,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
         __syncthreads();
         const int64_t h = list[tid];
         int64_t total;
-        const int64_t at = base + block_exclusive_scan_i64<kWaves>(h, sh, total);
+        const int64_t at = base + scan(h, sh, total);
         if (at < need && need <= at + h) {
           shi = tid;
           pk.sum = at;
@@ -705,7 +730,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
       };
       int64_t z = 0;
       each_of_row(a, logits, [&](float l, int j) { z += weight(l, j); });
-      z = block_sum_i64<kWaves>(z, sh);
+      z = sum_of(z, sh);
       const int64_t need = need_of(p.top_p, z);
       const uint32_t kp = radix_key(a, logits, need, weight, list, sh, &shi, passed);
       auto tie = [&](float l, int j) { return key_of(l) == kp ? weight(l, j) : 0; };
