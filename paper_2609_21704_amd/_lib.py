@@ -159,6 +159,8 @@ def _dtype_code(dt: torch.dtype) -> int:
 
 
 def _expect(t, dtype, shape, name):
+    if t.dtype is dtype and t.shape == shape:  # (torch.Size is a tuple)
+        return
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
     if tuple(t.shape) != tuple(shape):

@@ -282,6 +282,95 @@ __device__ __forceinline__ SeqWork seq_work(const PackedRows& pr, const AttnArgs
   return {(sr.n * G + TQ - 1) / TQ, steps_to(last_key(p0 + sr.n - 1, a.len_bound)), sr, p0};
 }
 
+// How few rows' work over pages is laid over workgroups where the sequences are many: the steps of all (sequence, kv head)
+// pairs one after the other, in shares of like length, one a workgroup, whatever the sequences' lengths.  A pair that a border
+// of two shares cuts is joined by shares_merge_kernel.  No border lies within kLeast steps of a pair's first or last, and none
+// in pairs of up to 2 kLeast (there it moves to the nearer end), so a part's loads are worth its start.  64 single tokens after
+// 500 to 24000 positions (28 heads on 4, 762 MB): 150 us with the merge, 5.1 TB/s where a streaming read reaches 6.4, for 336
+// with a workgroup a pair.  Four wavefronts a workgroup, two of them a CU, so that one's start and end lie beside the other's
+// loads: 144 us, 156 with eight, 139 with two, whose merge takes 3 more.  `grain`: log2 of the steps that count as one, for
+// lists that 32 bits would not hold.
+constexpr int kLeast = 4;
+constexpr int kMaxShares = 512;
+constexpr int kShareWaves = 4;
+
+struct Share {
+  int s, g, start, n;  // a pair: its first step in the list and its steps (one where it has no keys, for its answer)
+};
+
+template <class F>
+struct Shares {
+  int b, hkv, lane, grain, per;  // per: steps of a share
+  F work;
+  SeqWork w;  // of sequence base + lane
+  int n, incl, base, before, all;  // its steps, their sum up to here, the list's steps before `base` and altogether
+
+  __device__ __forceinline__ void load(int at) {
+    base = at;
+    w = base + lane < b ? work(base + lane) : SeqWork{};
+    n = w.tiles > 0 ? (w.steps > 1 ? (w.steps + (1 << grain) - 1) >> grain : 1) : 0;
+    incl = Planner<F>::scan(n);
+  }
+  __device__ __forceinline__ int here() const { return __builtin_amdgcn_readlane(incl, kWave - 1) * hkv; }
+  __device__ __forceinline__ Shares(int b, int hkv, int shares, int grain, F work)
+      : b(b), hkv(hkv), lane(threadIdx.x & 63), grain(grain), work(work), before(0), all(0) {
+#pragma unroll 1
+    for (int at = 0; at < b; at += kWave) {
+      load(at);
+      all += here();
+    }
+    if (b > kWave) load(0);
+    per = (all + shares - 1) / shares;
+    per = per < kLeast ? kLeast : per;
+  }
+  // where the border before share i would be, in the list (its end: the last step)
+  __device__ __forceinline__ int place(int i) const {
+    const int64_t at = (int64_t)i * per;
+    return at < all ? (int)at : all;
+  }
+  // the pair of step `at` (the list's end: a pair of no steps)
+  __device__ __forceinline__ Share find(int at) {
+    if (at >= all) return {0, 0, all, 0};
+    if (at < before) {
+      before = 0;
+      load(0);
+    }
+    while (at >= before + here()) {
+      before += here();
+      load(base + kWave);
+    }
+    const int l = __builtin_ctzll(__ballot(before + incl * hkv > at));
+    Share r;
+    r.s = base + l;
+    r.n = __builtin_amdgcn_readlane(n, l);
+    const int first = before + (__builtin_amdgcn_readlane(incl, l) - r.n) * hkv;
+    r.g = 0;  // (at most 127 steps of a few cycles, and no division)
+    r.start = first;
+    while (at >= r.start + r.n) {
+      r.start += r.n;
+      ++r.g;
+    }
+    return r;
+  }
+  // the border that would be at `at`, in pair p
+  __device__ __forceinline__ int border(int at, const Share& p) const {
+    const int in = at - p.start, left = p.n - in;
+    if (p.n == 0 || (p.n > 2 * kLeast && in >= kLeast && left >= kLeast)) return at;
+    return in <= left ? p.start : p.start + p.n;
+  }
+  // the sequence that find() has named
+  __device__ __forceinline__ void fill(Unit& u, int s) const {
+    const int l = s - base;
+    u.s = __builtin_amdgcn_readfirstlane(s);
+    u.tile = u.part = 0;
+    u.steps = __builtin_amdgcn_readlane(w.steps, l);
+    u.rows.first = __builtin_amdgcn_readlane(w.rows.first, l);
+    u.rows.n = __builtin_amdgcn_readlane(w.rows.n, l);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)w.p0, l);
+    u.p0 = (int64_t)__builtin_amdgcn_readlane((int)(w.p0 >> 32), l) << 32 | lo;
+  }
+};
+
 // ------------------------------------------------------------------ dequant
 // Sixteen bytes of codes to 16 halves of the low and 16 of the high nibbles: f16((c - z) s), the difference exact.
 template <bool HIGH, class Z, class S>
@@ -398,35 +487,26 @@ __device__ __forceinline__ uint32_t tame_scales(uint32_t w, int e, int left, boo
 // 1 us, the first loads 2, a step of 64 keys 0.7, the meeting in LDS 1, and a CU takes in fp16 entries at about 60 GB/s.
 constexpr int kFewWaves = 8;
 
-template <bool Q4, int NQT, int HALVES, bool Paged>
-__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2))) void few_attn_kernel(PackedRows pr,
-                                                                                                        AttnArgs a) {
-  constexpr int NW = kFewWaves / HALVES;  // wavefronts that share the keys of a half's queries
+// Steps st0 .. st1 of sequence u.s and kv head g; `whole`: they are all there are, and the rows are answered, else their sums
+// go to row `slot` of the parts.
+template <bool Q4, int NQT, int HALVES, bool Paged, int W>
+__device__ __forceinline__ void few_part(const AttnArgs& a, const Unit& u, int g, int st0, int st1, bool whole,
+                                         int64_t slot) {
+  constexpr int NW = W / HALVES;  // wavefronts that share the keys of a half's queries
   constexpr bool kAhead = Q4 || NQT == 1;
   constexpr bool kTwoTerms = !Q4;
-  __shared__ __align__(16) float ob[kFewWaves][16 * NQT][kHd + 4];
-  __shared__ float2 ml[kFewWaves][16 * NQT];
-  __shared__ __align__(16) uint16_t vsb[Q4 ? kFewWaves : 1][4][64];  // a step's scales and zeros of values, per wavefront
-  const int item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
+  __shared__ __align__(16) float ob[W][16 * NQT][kHd + 4];
+  __shared__ float2 ml[W][16 * NQT];
+  __shared__ __align__(16) uint16_t vsb[Q4 ? W : 1][4][64];  // a step's scales and zeros of values, per wavefront
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave8 = __builtin_amdgcn_readfirstlane(tid >> 6), wave = wave8 / HALVES;
   const int q0 = wave8 % HALVES * (16 * NQT);  // the wavefront's first query
   const int G = a.hq / a.hkv;
-  Unit u;
-  if (a.most) {
-    const Planner plan(pr.b, a.most, a.grain, [&](int i) { return seq_work(pr, a, G, 16 * NQT * HALVES, i); });
-    if (!plan.find(item, u)) return;
-  } else {  // an item a sequence
-    const SeqWork w = seq_work(pr, a, G, 16 * NQT * HALVES, item);
-    if (w.tiles == 0) return;
-    u = {item, 0, 0, 1 << 30, w.steps, w.rows, w.p0};
-  }
   const int64_t sg = (int64_t)u.s * a.hkv + g;
   const SeqRows sr = u.rows;
   const int nq = sr.n * G;
   const int64_t p0 = u.p0;
   const int64_t klast = last_key(p0 + sr.n - 1, a.len_bound);
-  const int st0 = u.part * u.span, st1 = st0 + u.span < u.steps ? st0 + u.span : u.steps;
 
   half8_t qf[NQT][4];
   int lpos[NQT];  // the position of this lane's query, clipped to [-1, 2^31)
@@ -508,6 +588,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
   const bool older = wave < NW / 2;
   int turn = 0;
   auto advance = [&](int st) {
+    if constexpr (W < 8) return st + NW;  // (the two are of different workgroups)
     const int gap = older ? (turn == 2 ? NW / 2 : NW) : (turn == 1 ? NW + NW / 2 : NW);
     turn = turn == (older ? 2 : 1) ? 0 : turn + 1;
     return st + gap;
@@ -707,7 +788,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     }
   }
   // the wavefronts' sums meet
-  const int nq_pad = 16 * NQT * HALVES, parts = u.steps > u.span ? (u.steps + u.span - 1) / u.span : 1;
+  constexpr int nq_pad = 16 * NQT * HALVES;
 #pragma unroll
   for (int t = 0; t < NQT; ++t) {
     const float lt = quad_sum(l[t]);
@@ -725,7 +806,7 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     for (int x = 0; x < 8; ++x) h[x] = bad ? __builtin_bit_cast(half_t, kNanF16) : (half_t)(r[x] / L);
     *reinterpret_cast<half8_t*>(a.out + ((int64_t)(sr.first + j) * a.hq + g * G + (qi - j * G)) * kHd + d0) = h;
   };
-  for (int qi = tid >> 4; qi < nq; qi += 4 * kFewWaves) {
+  for (int qi = tid >> 4; qi < nq; qi += 4 * W) {
     const int d0 = 8 * (tid & 15), half = qi / (16 * NQT), qx = qi & (16 * NQT - 1);
     float M = kNoMax, L = 0.f, r[8] = {};
 #pragma unroll
@@ -743,8 +824,8 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
         r[4 + i] += f * v[i];
       }
     }
-    if (parts > 1) {
-      const int64_t at = (int64_t)blockIdx.x * nq_pad + qi;
+    if (!whole) {
+      const int64_t at = slot * nq_pad + qi;
       float* po = a.part_o + at * kHd + d0;
       reinterpret_cast<float4_t*>(po)[0] = float4_t{r[0], r[1], r[2], r[3]};
       reinterpret_cast<float4_t*>(po)[1] = float4_t{r[4], r[5], r[6], r[7]};
@@ -752,6 +833,52 @@ __global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(
     } else {
       answer(qi, d0, r, L);
     }
+  }
+}
+
+template <bool Q4, int NQT, int HALVES, bool Paged>
+__global__ __launch_bounds__(64 * kFewWaves) __attribute__((amdgpu_waves_per_eu(2))) void few_attn_kernel(PackedRows pr,
+                                                                                                        AttnArgs a) {
+  const int G = a.hq / a.hkv, item = blockIdx.x / a.hkv, g = blockIdx.x - item * a.hkv;
+  auto work = [&](int i) { return seq_work(pr, a, G, 16 * NQT * HALVES, i); };
+  Unit u;
+  if (a.most) {
+    const Planner plan(pr.b, a.most, a.grain, work);
+    if (!plan.find(item, u)) return;
+  } else {  // an item a sequence
+    const SeqWork w = work(item);
+    if (w.tiles == 0) return;
+    u = {item, 0, 0, 1 << 30, w.steps, w.rows, w.p0};
+  }
+  const int st0 = u.part * u.span, st1 = st0 + u.span < u.steps ? st0 + u.span : u.steps;
+  few_part<Q4, NQT, HALVES, Paged, kFewWaves>(a, u, g, st0, st1, u.steps <= u.span, blockIdx.x);
+}
+
+// Share blockIdx.x of the steps of all sequences.
+template <bool Q4, int NQT, int HALVES, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void few_shares_kernel(PackedRows pr, AttnArgs a) {
+  Shares shares(pr.b, a.hkv, a.most, a.grain, [&](int i) { return seq_work(pr, a, a.hq / a.hkv, 16 * NQT * HALVES, i); });
+  int at = 0, end = 0;
+#pragma unroll 1
+  for (int k = 0; k < 2 || at < end; ++k) {  // (the borders by the same code as the pairs: its fetch counts)
+    const int want = k < 2 ? shares.place(blockIdx.x + k) : at;
+    const Share sh = shares.find(want);
+    if (k == 0) {
+      at = shares.border(want, sh);
+      continue;
+    }
+    if (k == 1) {
+      end = shares.border(want, sh);
+      continue;
+    }
+    Unit u;
+    shares.fill(u, sh.s);
+    const int stop = sh.start + sh.n < end ? sh.start + sh.n : end;
+    const int64_t st1 = (int64_t)(stop - sh.start) << a.grain;
+    few_part<Q4, NQT, HALVES, true, W>(a, u, sh.g, (at - sh.start) << a.grain, st1 < u.steps ? (int)st1 : u.steps,
+                                       stop - at == sh.n, 2 * (int64_t)blockIdx.x + (at == sh.start));
+    at = stop;
+    __syncthreads();  // the wavefronts' sums have been read
   }
 }
 
@@ -1158,10 +1285,9 @@ __global__ __launch_bounds__(64 * NW * KW) __attribute__((amdgpu_waves_per_eu(2,
 }
 
 // The parts of query qi joined, in their order: lane i the weights of parts i, 64 + i, .. (at most kMost a lane), then every
-// lane two dimensions, eight parts' sums in flight.  row0: the query's row of part 0's sums.
-template <int kMost>
-__device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr, int64_t p0, int qi, int parts,
-                                     int64_t row0, int64_t stride) {
+// lane two dimensions, eight parts' sums in flight.  row(p): the query's row of part p's sums.
+template <int kMost, class R>
+__device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr, int64_t p0, int qi, int parts, R row) {
   const int lane = threadIdx.x & 63;
   float2 ml[kMost];
   float M = kNoMax, L = 0.f;
@@ -1169,7 +1295,7 @@ __device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr
   for (int i = 0; i < kMost; ++i) {
     const int p = 64 * i + lane;
     ml[i] = make_float2(kNoMax, 0.f);
-    if (p < parts) ml[i] = a.part_ml[row0 + p * stride];
+    if (p < parts) ml[i] = a.part_ml[row(p)];
     M = fmaxf(M, ml[i].x);
   }
 #pragma unroll
@@ -1181,13 +1307,13 @@ __device__ __forceinline__ void join(const AttnArgs& a, int G, int g, SeqRows sr
   }
   L = wave_sum(L);
   float x = 0.f, y = 0.f;
-  const float* po = a.part_o + row0 * kHd + 2 * lane;
+  const float* po = a.part_o + 2 * lane;
   for (int p0i = 0; p0i < parts; p0i += 8) {
     float2 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int p = p0i + i < parts ? p0i + i : parts - 1;
-      v[i] = *reinterpret_cast<const float2*>(po + p * stride * kHd);
+      v[i] = *reinterpret_cast<const float2*>(po + row(p) * kHd);
     }
     float fw = ml[0].x;
 #pragma unroll
@@ -1229,10 +1355,32 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedRows pr, AttnAr
   const int qx = blockIdx.y * 4 + wave;
   if (qt * TQ + qx >= nq || (few && parts == 1) || first + parts > a.most) return;  // (the latter as in the plan)
   const int64_t row0 = ((int64_t)first * a.hkv + g) * TQ + qx;
+  auto row = [&](int p) { return row0 + p * stride; };
   if (parts <= kWave)
-    join<1>(a, G, g, sr, p0, qt * TQ + qx, parts, row0, stride);
+    join<1>(a, G, g, sr, p0, qt * TQ + qx, parts, row);
   else
-    join<kMaxParts / kWave>(a, G, g, sr, p0, qt * TQ + qx, parts, row0, stride);
+    join<kMaxParts / kWave>(a, G, g, sr, p0, qt * TQ + qx, parts, row);
+}
+
+// The pair that begins in share blockIdx.x and ends in a later one, four of its queries, one a wavefront.
+__global__ __launch_bounds__(256) void shares_merge_kernel(PackedRows pr, AttnArgs a, int TQ) {
+  const int G = a.hq / a.hkv, i = blockIdx.x;
+  Shares shares(pr.b, a.hkv, a.most, a.grain, [&](int s) { return seq_work(pr, a, G, TQ, s); });
+  const int end = shares.place(i + 1);
+  const Share sh = shares.find(end);
+  const int in = end - sh.start, left = sh.n - in;
+  if (in == 0 || shares.border(end, sh) != end) return;  // no pair is cut there
+  if (in - shares.per >= kLeast) return;  // the border before share i cuts this one too
+  const int qi = blockIdx.y * 4 + (threadIdx.x >> 6);
+  Unit u;
+  shares.fill(u, sh.s);
+  if (qi >= u.rows.n * G) return;
+  const int parts = 2 + (left - kLeast) / shares.per;  // the borders per, 2 per .. further on cut it, but near its end
+  auto row = [&](int p) { return (2 * (int64_t)(i + p) + (p == 0)) * TQ + qi; };
+  if (parts <= kWave)
+    join<1>(a, G, sh.g, u.rows, u.p0, qi, parts, row);
+  else
+    join<kMaxShares / kWave>(a, G, sh.g, u.rows, u.p0, qi, parts, row);
 }
 
 struct Plan {
@@ -1291,6 +1439,17 @@ void launch_few(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& 
     hipLaunchKernelGGL((few_attn_kernel<true, 2, 2, Paged>), grid, block, 0, stream, pr, a);
 }
 
+template <bool Q4>
+void launch_shares(const Plan& p, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)p.most), block(64 * kShareWaves);
+  if (p.tq == 16)
+    hipLaunchKernelGGL((few_shares_kernel<Q4, 1, 1, kShareWaves>), grid, block, 0, stream, pr, a);
+  else if (p.tq == 32)
+    hipLaunchKernelGGL((few_shares_kernel<Q4, 2, 1, kShareWaves>), grid, block, 0, stream, pr, a);
+  else if constexpr (Q4)
+    hipLaunchKernelGGL((few_shares_kernel<true, 2, 2, kShareWaves>), grid, block, 0, stream, pr, a);
+}
+
 template <bool Q4, bool Paged>
 void launch_prompt(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArgs& a, hipStream_t stream) {
   if (p.tq == 256)  // (never split: so many tiles fill the chip)
@@ -1306,12 +1465,25 @@ void launch_prompt(const Plan& p, dim3 grid, const PackedRows& pr, const AttnArg
 hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int hq, int hkv, const int32_t* pos_base,
                                    int pos_offset, int64_t len_bound, int64_t capacity, const KvCache& cache,
                                    uint16_t* out, hipStream_t stream) {
-  const bool q4 = cache.k4 != nullptr;
-  const Plan p = make_plan(pr, hq, hkv, len_bound, q4);
+  const bool q4 = cache.k4 != nullptr, paged = cache.table != nullptr;
+  Plan p = make_plan(pr, hq, hkv, len_bound, q4);
+  const int64_t steps = (len_bound + kTile - 1) / kTile;  // of one sequence, at most
+  // Pages: where the keys of a sequence would be taken whole, in shares of all sequences' keys.  The two, 28 heads on 4, fp16
+  // and 4-bit entries: 48 sequences of 2000 positions 40 and 49 us, 16 and 24; of 300 to 9000 positions 124 and 61, 44 and 32;
+  // 64 of 2000 49 and 62, 18 and 25, of 300 to 9000 133 and 83, 48 and 39.  Fewer sequences, in parts of one length each
+  // and in shares: 32 of 300 to 9000 42 and 47, 20 and 30, eight of them 15.3 and 18.1.
+  const bool shares = paged && p.few && 2 * (int64_t)pr.b * hkv > kMaxParts;
+  if (shares) {
+    p.grain = 0;
+    while (((steps >> p.grain) + 1) * pr.b * hkv >= int64_t(1) << 30) ++p.grain;
+    const int64_t most = (steps * pr.b * hkv + kLeast - 1) / kLeast, resident = cu_count() * 8 / kShareWaves;
+    p.most = (int)(most < resident ? most : resident);
+    p.most = p.most < kMaxShares ? p.most : kMaxShares;
+  }
   AttnArgs a{q, cache, pos_base, pos_offset, hq, hkv, len_bound, capacity, out, nullptr, nullptr, p.most, p.grain, false};
   const int units = p.most ? p.most : p.tiles;
   if (p.most) {
-    const size_t queries = (size_t)units * hkv * p.tq;
+    const size_t queries = (size_t)units * (shares ? 2 : hkv) * p.tq;
     void* ws = nullptr;
     const hipError_t e = workspace(queries * (kHd * sizeof(float) + sizeof(float2)), stream, &ws);
     if (e != hipSuccess) return e;
@@ -1327,9 +1499,10 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
   // 366; 40 heads on 8, four of up to 3000 72.3 for 75.6 and 128.4 for 126.5, eight 282 for 275 and 220 for 217.
   const int64_t seqs = pr.b < pr.rows ? pr.b : pr.rows;
   a.longest = !p.few && seqs > 1 && seqs * hkv <= 32 && (int64_t)units * hkv > (p.tq == 256 ? 256 : 512);
-  const bool paged = cache.table != nullptr;
   auto launch = [&](auto is_q4, auto is_paged) {
-    if (p.few)
+    if (shares)
+      launch_shares<is_q4.value>(p, pr, a, stream);
+    else if (p.few)
       launch_few<is_q4.value, is_paged.value>(p, grid, pr, a, stream);
     else
       launch_prompt<is_q4.value, is_paged.value>(p, grid, pr, a, stream);
@@ -1338,7 +1511,11 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
     q4 ? launch(std::true_type{}, std::true_type{}) : launch(std::false_type{}, std::true_type{});
   else
     q4 ? launch(std::true_type{}, std::false_type{}) : launch(std::false_type{}, std::false_type{});
-  if (p.most)
+  if (shares && (units == 1 || steps <= 2 * kLeast)) return hipGetLastError();  // no pair is cut
+  if (shares)
+    hipLaunchKernelGGL(shares_merge_kernel, dim3((unsigned)(units - 1), (unsigned)(p.tq / 4)), dim3(256), 0, stream, pr, a,
+                       p.tq);
+  else if (p.most)
     hipLaunchKernelGGL(packed_merge_kernel, dim3((unsigned)(p.tiles * hkv), (unsigned)(p.tq / 4)), dim3(256), 0, stream,
                        pr, a, p.tq, p.grain, p.few);
   return hipGetLastError();

@@ -44,16 +44,19 @@ __device__ __forceinline__ int block_scan(int v, int* sh, int& total) {
   return base + x - v;
 }
 
-// Calls f(id, rank) for the ids in [from, to) that `is` picks, of which rank - 1 lower ones were picked, and returns how
-// many there are; stops after the step in which there are `enough`.
+// Calls f(id, rank) for the ids in [from, to) with is(refs[id]), of which `rank` lower ones there are, and returns how many
+// were found; stops after the step in which there are `enough`.
 template <class P, class F>
-__device__ __forceinline__ int pick_ids(int from, int to, int enough, int* sh, P is, F f) {
+__device__ __forceinline__ int pick_ids(const int32_t* refs, int from, int to, int enough, int* sh, P is, F f) {
   int found = 0;
   for (int base = from; base < to && found < enough; base += kThreads * kIds) {  // uniform
     const int id0 = base + (int)threadIdx.x * kIds;
+    int x[kIds];
+#pragma unroll
+    for (int i = 0; i < kIds; ++i) x[i] = refs[id0 + i < to ? id0 + i : to - 1];
     uint32_t set = 0;
 #pragma unroll
-    for (int i = 0; i < kIds; ++i) set |= (id0 + i < to && is(id0 + i) ? 1u : 0u) << i;
+    for (int i = 0; i < kIds; ++i) set |= (id0 + i < to && is(x[i]) ? 1u : 0u) << i;
     int total;
     int rank = found + block_scan(__builtin_popcount(set), sh, total);
     while (set) {
@@ -71,7 +74,7 @@ __device__ __forceinline__ int64_t pages_for(int64_t n) { return n <= 0 ? 0 : (n
 
 // The lowest free ids, up to `most` of them, to list (device memory of the workgroup's own); how many there are.
 __device__ __forceinline__ int free_ids(const int32_t* refs, int pages, int most, int32_t* list, int* sh) {
-  const int found = pick_ids(0, pages, most, sh, [&](int id) { return refs[id] <= 0; },
+  const int found = pick_ids(refs, 0, pages, most, sh, [](int n) { return n <= 0; },
                              [&](int id, int rank) {
                                if (rank < most) list[rank] = id;
                              });
@@ -202,24 +205,39 @@ __global__ __launch_bounds__(kThreads) void pages_fork_kernel(PageState p, const
   sl[tid] = ok ? len : 0;
   sr[tid] = ok && part ? list[rank] : -1;
   __syncthreads();
-  for (int i = tid >> 6; i < n; i += kWaves) {
-    if (sl[i] == 0) continue;  // uniform
-    const int full = sl[i] / kPage;
-    const int32_t* from = p.table + (int64_t)sp[i] * p.width;
-    int32_t* to = p.table + (int64_t)sc[i] * p.width;
-    for (int e = lane; e < full; e += kWave) {
-      const int id = from[e];
-      to[e] = id;
-      if ((uint32_t)id < (uint32_t)p.pages)
-        atomicAdd(&p.refs[id], 1);
-      else
-        flag(status, kBadPage);
+  // a wavefront a pair, four of its pairs' loads in flight
+  constexpr int kPairs = 4;
+  for (int i0 = tid >> 6; i0 < n; i0 += kPairs * kWaves) {
+    int full[kPairs], most = 0;
+#pragma unroll
+    for (int x = 0; x < kPairs; ++x) {
+      const int i = i0 + x * kWaves;
+      full[x] = i < n ? sl[i] / kPage : 0;  // (sl 0: nothing)
+      most = full[x] > most ? full[x] : most;
     }
-    if (lane == 0 && sr[i] >= 0) {
-      to[full] = sr[i];
-      p.refs[sr[i]] = 1;
+    for (int e = lane; e < most; e += kWave) {
+      int id[kPairs];
+#pragma unroll
+      for (int x = 0; x < kPairs; ++x)
+        if (e < full[x]) id[x] = p.table[(int64_t)sp[i0 + x * kWaves] * p.width + e];
+#pragma unroll
+      for (int x = 0; x < kPairs; ++x) {
+        if (e >= full[x]) continue;
+        p.table[(int64_t)sc[i0 + x * kWaves] * p.width + e] = id[x];
+        if ((uint32_t)id[x] < (uint32_t)p.pages)
+          atomicAdd(&p.refs[id[x]], 1);
+        else
+          flag(status, kBadPage);
+      }
     }
-    if (lane == 0) p.held[sc[i]] = full + (sr[i] >= 0 ? 1 : 0);
+  }
+  if (ok) {  // a thread a pair
+    const int full = len / kPage;
+    if (part) {
+      p.table[(int64_t)ch * p.width + full] = sr[tid];
+      p.refs[sr[tid]] = 1;
+    }
+    p.held[ch] = full + (part ? 1 : 0);
   }
   if (ok && part) {  // (those that got a page are the first of those that needed one)
     src[rank] = p.table[(int64_t)pa * p.width + len / kPage];
@@ -234,14 +252,11 @@ __global__ __launch_bounds__(kThreads) void pages_compact_kernel(PageState p, in
                                                                  int32_t* __restrict__ used, int32_t* __restrict__ to) {
   __shared__ int sh[kWaves];
   const int all = p.pages + 1;  // (no scan ends early)
-  const int u = pick_ids(0, p.pages, all, sh, [&](int id) { return p.refs[id] > 0; }, [](int, int) {});
-  pick_ids(0, u, all, sh, [&](int id) { return p.refs[id] <= 0; }, [&](int id, int rank) { dst[rank] = id; });
-  const int n = pick_ids(u, p.pages, all, sh,
-                         [&](int id) {
-                           to[id] = id;
-                           return p.refs[id] > 0;
-                         },
-                         [&](int id, int rank) { src[rank] = id; });
+  auto held = [](int n) { return n > 0; };
+  const int u = pick_ids(p.refs, 0, p.pages, all, sh, held, [](int, int) {});
+  pick_ids(p.refs, 0, u, all, sh, [](int n) { return n <= 0; }, [&](int id, int rank) { dst[rank] = id; });
+  const int n = pick_ids(p.refs, u, p.pages, all, sh, held, [&](int id, int rank) { src[rank] = id; });
+  for (int i = u + threadIdx.x; i < p.pages; i += kThreads) to[i] = i;
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += kThreads) {  // as many free ids below u as used ones from u on
     const int a = src[i], b = dst[i];

@@ -157,6 +157,10 @@ ATTN = [([(1, 0)], 1, 1, 0),
         ([(1, 30 + 37 * i) for i in range(40)], 28, 4, 0),
         ([(1, 5000), (1, 3), (1, 900)], 8, 8, 0),
         ([(1, 20 * (i % 7) ** 3) for i in range(70)], 8, 4, 0),
+        ([(1, 30000)] + [(1, 10 + i) for i in range(34)], 8, 4, 0),
+        ([(2, (i * 797) % 3100) for i in range(150)], 14, 2, 0),
+        ([(i % 3, 70 * (i % 9)) for i in range(70)], 16, 4, 1),
+        ([(5, 90 * (i % 11)) for i in range(66)], 24, 4, 0),
         ([(2, 640 * i) for i in range(9)], 28, 4, 0),
         ([(9, 200), (9, 1900), (9, 0), (9, 64)], 28, 4, 1),
         ([(16, 100 * i) for i in range(20)], 8, 2, 0),
