@@ -177,7 +177,8 @@ __global__ __launch_bounds__(kThreads) void pages_fork_kernel(PageState p, const
                                                               int32_t* __restrict__ count, int32_t* __restrict__ list,
                                                               int32_t* __restrict__ status) {
   __shared__ int sh[kWaves];
-  __shared__ int sp[kThreads], sc[kThreads], sl[kThreads], sr[kThreads];  // parent, child, length (0: no fork), fresh page
+  __shared__ __align__(16) int sc[kThreads];  // child
+  __shared__ int sp[kThreads], sl[kThreads], sr[kThreads];  // parent, length (0: no fork), fresh page
   const int tid = threadIdx.x, lane = tid & 63;
   const bool mine = tid < n;
   const int pa = mine ? parent[tid] : -1, ch = mine ? child[tid] : -1, len = mine ? length[tid] : 0;
@@ -190,8 +191,11 @@ __global__ __launch_bounds__(kThreads) void pages_fork_kernel(PageState p, const
     const int hp = p.held[pa];
     ok = p.held[ch] == 0 && hp > 0 && hp <= p.width && len >= 1 && len <= (int64_t)hp * kPage;
   }
-  for (int j = 0; j < n; ++j)  // (uniform reads; n steps of a few cycles)
-    if (j < tid && sc[j] == ch) ok = false;
+  for (int j = 0; j < n; j += 4) {  // (the same words for all; past n they are -1)
+    const int4 c = *reinterpret_cast<const int4*>(&sc[j]);
+    if ((j < tid && c.x == ch) || (j + 1 < tid && c.y == ch) || (j + 2 < tid && c.z == ch) || (j + 3 < tid && c.w == ch))
+      ok = false;
+  }
   if (asked && !ok) flag(status, kBadFork);
   const bool part = ok && len % kPage != 0;
   int total;

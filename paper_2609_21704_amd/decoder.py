@@ -131,6 +131,95 @@ class KVCacheQ4:
         return self.k_codes[l], self.k_scales[l], self.v_codes[l], self.v_scales[l]
 
 
+class Pages:
+    """Which rows hold which pages of 64 positions (include/specquant_paged.h): the state that the pools of a decoder, the
+    parent's and the draft's, go by.  Rows take pages as they grow and may share them."""
+
+    def __init__(self, rows: int, width: int, pages: int, device):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.rows, self.width, self.pages = rows, width, pages
+        self.table = torch.full((rows, width), -1, **i32)
+        self.held = torch.zeros((rows,), **i32)
+        self.refs = torch.zeros((pages,), **i32)
+        moves = max(pages, rows)
+        self.src, self.dst = torch.zeros((moves,), **i32), torch.zeros((moves,), **i32)
+        self.count, self.used = torch.zeros((1,), **i32), torch.zeros((1,), **i32)
+
+    @property
+    def state(self):
+        return self.table, self.held, self.refs
+
+    def reserve(self, pos_base, ahead: int, status=None):
+        """Pages for the positions below pos_base[s] + ahead."""
+        sq.sq_pages_reserve(*self.state, pos_base, ahead, status=status)
+
+    def trim(self, keep, status=None):
+        """Give back the pages past position keep[s] (below 0: the row keeps its own)."""
+        sq.sq_pages_trim(*self.state, keep, status=status)
+
+    def _copy(self, pools, status):
+        for pool in pools:
+            for a in pool.arrays:
+                sq.sq_page_copy(a, self.src, self.dst, self.count, status=status)
+
+    def fork(self, parent, child, length, pools, status=None):
+        """Rows child[i], which hold no pages, share the first length[i] positions of rows parent[i]; a partly filled last
+        page is copied, in all pools."""
+        for i in range(0, parent.shape[0], 1024):
+            part = slice(i, i + 1024)
+            sq.sq_pages_fork(*self.state, parent[part], child[part], length[part], self.src, self.dst, self.count,
+                             status=status)
+            self._copy(pools, status)
+
+    def compact(self, pools, status=None) -> int:
+        """Move the pages in use to the lowest ids, in all pools; returns how many they are (and waits for that)."""
+        sq.sq_pages_compact(*self.state, self.src, self.dst, self.count, self.used, status=status)
+        self._copy(pools, status)
+        return int(self.used.item())
+
+
+class KVCachePaged:
+    """A pool of pages per layer, fp16 or ("q4") 4-bit, one allocation per array with the layers first; layer(l) are the
+    views that the paged calls take, before the table of `pages`."""
+
+    def __init__(self, cfg: Config, layers: int, pages: Pages, device, fmt: str = "f16"):
+        if fmt not in ("f16", "q4"):
+            raise ValueError("a cache is 'f16' or 'q4'")
+        self.pages, self.q4 = pages, fmt == "q4"
+        heads, u8, f16 = (layers, pages.pages, cfg.kv_heads), torch.uint8, torch.float16
+        shapes = (((sq.PAGE, HEAD_DIM // 2), u8), ((sq.PAGE, 4), f16), ((HEAD_DIM // 2, sq.PAGE), u8), ((4, sq.PAGE), f16))
+        if not self.q4:
+            shapes = (((sq.PAGE, HEAD_DIM), f16), ((HEAD_DIM, sq.PAGE), f16))
+        self.arrays = tuple(torch.zeros((*heads, *shape), dtype=dtype, device=device) for shape, dtype in shapes)
+
+    def layer(self, l: int):
+        return tuple(a[l] for a in self.arrays)
+
+    def rope_kv(self, l: int, qkv, bias, row_start, pos_base, hq: int, q_out, status, **rows):
+        call = sq.sq_paged_rope_kv_q4 if self.q4 else sq.sq_paged_rope_kv_f16
+        call(qkv, bias, row_start, pos_base, hq, *self.layer(l), self.pages.table, theta=THETA, q_out=q_out, status=status,
+             **rows)
+
+    def attention(self, l: int, q, row_start, pos_base, out, **rows):
+        call = sq.sq_paged_attention_q4 if self.q4 else sq.sq_paged_attention_f16
+        call(q, *self.layer(l), self.pages.table, row_start, pos_base, out=out, **rows)
+
+
+def filters_wanted(temperature: float, top_k: int, top_p: float, min_p: float) -> bool:
+    """Whether these settings filter anything (greedy tokens are not filtered)."""
+    if int(top_k) != top_k or not top_p >= 0 or not min_p >= 0:
+        raise ValueError("top_k must be an integer, top_p and min_p at least 0")
+    return temperature > 0 and (top_k > 0 or top_p < 1 or min_p > 0)
+
+
+def filter_rows(rows: int, temperature: float, top_k: int, top_p: float, min_p: float, device) -> dict:
+    """The sampling calls' settings (include/specquant_sample.h), the same for all rows."""
+    f32 = dict(dtype=torch.float32, device=device)
+    return dict(temperature=torch.full((rows,), temperature, **f32), top_p=torch.full((rows,), top_p, **f32),
+                min_p=torch.full((rows,), min_p, **f32),
+                top_k=torch.full((rows,), int(top_k), dtype=torch.int32, device=device))
+
+
 class _Buffers:
     """Activations of a pass of up to `rows` rows."""
 
@@ -160,9 +249,16 @@ class SpecDecoder:
 
     def __init__(self, weights: DecoderWeights, batch: int | None = None, k: int | None = None,
                  capacity: int = 1024, temperature: float = 1.0, history: int = 4096, keep_pq: bool = False,
-                 chains: int = 1, fuse: bool = True, draft_cache: str = "f16"):
+                 chains: int = 1, fuse: bool = True, draft_cache: str = "f16", pages: int | None = None, top_k: int = 0,
+                 top_p: float = 1.0, min_p: float = 0.0):
         """draft_cache "q4": the draft's cache in 4 bits.  Its drafts come from the coarser entries; what the rounds emit
-        follows the parent's distribution as before (one chain per sequence: entries are not adopted)."""
+        follows the parent's distribution as before (one chain per sequence: entries are not adopted).
+
+        pages: keep both caches in pools of that many pages of 64 positions, which the rows take as they grow, instead
+        of `capacity` positions a row (one chain per sequence).  Where they run out, `status` gets SQ_DEV_NO_PAGES.
+
+        top_k, top_p, min_p: draft and parent are filtered alike, so that the rounds emit the parent's filtered
+        distribution (T > 0)."""
         if draft_cache not in ("f16", "q4"):
             raise ValueError("draft_cache must be 'f16' or 'q4'")
         if draft_cache == "q4" and chains != 1:
@@ -181,9 +277,17 @@ class SpecDecoder:
             raise ValueError("draft step 0 runs 2 rows per chain; a pass takes at most 64 rows")
         if R * (k + 1) > 64:
             raise ValueError("the verification pass takes at most 64 rows")
-        self.dcache = (KVCacheQ4 if draft_cache == "q4" else KVCache)(cfg, L, R, capacity, dev)
-        self.pcache = KVCache(cfg, L, R, capacity, dev)
+        self._make_pages(pages, capacity)
+        if self.pages:
+            self.dcache = KVCachePaged(cfg, L, self.pages, dev, draft_cache)
+            self.pcache = KVCachePaged(cfg, L, self.pages, dev)
+        else:
+            self.dcache = (KVCacheQ4 if draft_cache == "q4" else KVCache)(cfg, L, R, capacity, dev)
+            self.pcache = KVCache(cfg, L, R, capacity, dev)
         self.capacity = capacity
+        self.filters = None  # of the draft's rows and of the parent's
+        if filters_wanted(self.T, top_k, top_p, min_p):
+            self.filters = [filter_rows(n, self.T, top_k, top_p, min_p, dev) for n in (R, R * (k + 1))]
         self.buf = _Buffers(cfg, 64, dev)  # the largest pass: 64 rows (verification, prefill chunks)
         i32, f32 = torch.int32, torch.float32
         self.pos_base = torch.zeros((R,), dtype=i32, device=dev)
@@ -209,6 +313,22 @@ class SpecDecoder:
             self.p_out = torch.empty((R, k + 1, V), dtype=f32, device=dev)
         self.graph = None
         self.fuse = fuse
+
+    def _make_pages(self, pages: int | None, capacity: int):
+        self.pages = None
+        if pages is None:
+            return
+        if capacity % sq.PAGE or pages < 1:
+            raise ValueError("paged caches take at least one page, and a capacity that is a multiple of 64")
+        if self.c != 1:
+            raise ValueError("paged caches take one chain per sequence")
+        self.pages = Pages(self.R, capacity // sq.PAGE, int(pages), self.device)
+
+    def _refill(self, lengths):
+        """Every row's pages given back, and those of the first lengths[s] positions taken."""
+        if self.pages:
+            self.pages.trim(torch.zeros((self.R,), dtype=torch.int32, device=self.device), self.status)
+            self.pages.reserve(torch.tensor(lengths, dtype=torch.int32, device=self.device), 0, self.status)
 
     # ------------------------------------------------------------- passes
     def _linear(self, draft: bool, key, x, y):
@@ -257,7 +377,17 @@ class SpecDecoder:
         delta = None  # a projection output not yet added into h
         for l in range(w.layers):
             self._norm_linear(draft, (l, "qkv"), h, w.in_norm[l], delta, x, qkv)
-            if isinstance(cache, KVCacheQ4):
+            if self.pages:
+                rows = dict(max_rows=rps, pos_offset=offset, len_bound=lb)
+                cache.rope_kv(l, qkv, w.qkv_bias[l], None, self.pos_base, cfg.q_heads, q, self.status, **rows)
+                if logits is None and l + 1 == w.layers and not self.attn_hook:
+                    return
+                if self.attn_hook:
+                    self.attn_hook(True, rps, offset)
+                cache.attention(l, q, None, self.pos_base, a, **rows)
+                if self.attn_hook:
+                    self.attn_hook(False, rps, offset)
+            elif isinstance(cache, KVCacheQ4):
                 rows = dict(max_rows=rps, pos_offset=offset, len_bound=lb)
                 sq.sq_packed_rope_kv_q4(qkv, w.qkv_bias[l], None, self.pos_base, cfg.q_heads, *cache.layer(l), theta=THETA,
                                         q_out=q, status=self.status, **rows)
@@ -318,7 +448,9 @@ class SpecDecoder:
         for l in range(w.layers):
             sq.sq_add_rmsnorm_f16(h, w.in_norm[l], EPS, x=x)
             w.stack.prefill_linear(draft, (l, "qkv"), x, qkv)
-            if packed is None and not q4:
+            if self.pages:
+                cache.rope_kv(l, qkv, w.qkv_bias[l], row_start, self.pos_base, cfg.q_heads, q, self.status, **rows)
+            elif packed is None and not q4:
                 sq.sq_prefill_rope_kv_f16(qkv, w.qkv_bias[l], self.pos_base, offset, n, cfg.q_heads, cache.k[l],
                                           cache.v[l], len_bound=lb, theta=THETA, q_out=q, status=self.status)
             else:
@@ -329,7 +461,9 @@ class SpecDecoder:
                 break
             if self.attn_hook:
                 self.attn_hook(True, n, offset)
-            if packed is None and not q4:
+            if self.pages:
+                cache.attention(l, q, row_start, self.pos_base, a, **rows)
+            elif packed is None and not q4:
                 sq.sq_prefill_attention_f16(q, cache.k[l], cache.v[l], self.pos_base, offset, n, len_bound=lb, out=a)
             else:
                 (sq.sq_packed_attention_q4 if q4 else sq.sq_packed_attention_f16)(
@@ -356,13 +490,18 @@ class SpecDecoder:
         if not self.takes_packed(models):
             raise ValueError("a projection of this model has no kernel for packed prompts: use prefill()")
         prompts = [list(p) for p in prompts for _ in range(self.c)]
+        self._fill_packed(prompts, models)
+
+    def _fill_packed(self, prompts, models):
+        """The passes of prefill_packed; a row without tokens is left alone."""
         i32 = torch.int32
+        self._refill([len(p) for p in prompts])
         for draft in models:
             done = [0] * self.R
             while True:
                 left, take = PREFILL_ROWS, []
                 for p, d in zip(prompts, done):
-                    take.append(min(left, len(p) - 1 - d))
+                    take.append(min(left, max(len(p) - 1, 0) - d))
                     left -= take[-1]
                 if sum(take) == 0:
                     break
@@ -375,8 +514,8 @@ class SpecDecoder:
                 self._prefill_pass(draft, torch.tensor(toks, dtype=i32, device=self.device), max(take), 0,
                                    packed=(torch.tensor(start, dtype=i32, device=self.device), max(done)))
         self.pos_base.copy_(torch.tensor([len(p) - 1 for p in prompts], dtype=i32))
-        self.pending.copy_(torch.tensor([p[-1] for p in prompts], dtype=i32))
-        self.prev.copy_(torch.tensor([p[-2] for p in prompts], dtype=i32))
+        self.pending.copy_(torch.tensor([p[-1] if p else 0 for p in prompts], dtype=i32))
+        self.prev.copy_(torch.tensor([p[-2] if p else 0 for p in prompts], dtype=i32))
         self.out_len.zero_()
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(True, False), lengths=None):
@@ -406,6 +545,7 @@ class SpecDecoder:
         last, before = host[rows, lens - 1].contiguous(), host[rows, lens - 2].contiguous()
         prompt = host.to(self.device)
         R = self.R
+        self._refill([Lp - 1] * R)  # (padding is written too)
         self.pos_base.zero_()
         for draft in models:
             # blocks of up to PREFILL_ROWS rows; a block of up to 64 goes through the streaming projections
@@ -419,6 +559,8 @@ class SpecDecoder:
                     rest = prompt[:, s + 1:s + n].t().contiguous() if n > 1 else None
                     self.forward(draft, first, rest, n, s, None, last_only=False, len_bound=s + n)
                 s += n
+        if self.pages:
+            self.pages.trim((lens - 1).to(device=self.device, dtype=torch.int32), self.status)
         self.pos_base.copy_((lens - 1).to(torch.int32))
         self.pending.copy_(last)
         self.prev.copy_(before)
@@ -431,14 +573,18 @@ class SpecDecoder:
             self.forward(True, self.prev, self.pending.view(1, R), 2, -1, self.draft_logits[0], last_only=True)
         else:
             self.forward(True, self.draft_tokens[i - 1], None, 1, i, self.draft_logits[i], last_only=True)
+        if self.filters:
+            sq.sq_filter_logits_f32(self.draft_logits[i], out=self.draft_logits[i], status=self.status, **self.filters[0])
         p_out = self.q_draft[i].view(R, 1, V) if self.keep_pq and self.T > 0 else None
         sq.sq_spec_accept(None, self.draft_logits[i].view(R, 1, V), None, self.u_draft[i].view(R, 1), self.T,
                           n_accepted=self.scratch_n, next_token=self.draft_tokens[i], p_out=p_out)
 
     def verify(self):
         R, k, V = self.R, self.k, self.cfg.vocab
-        self.forward(False, self.pending, self.draft_tokens, k + 1, 0, self.target_logits.view(R * (k + 1), V),
-                     last_only=False)
+        logits = self.target_logits.view(R * (k + 1), V)
+        self.forward(False, self.pending, self.draft_tokens, k + 1, 0, logits, last_only=False)
+        if self.filters:
+            sq.sq_filter_logits_f32(logits, out=logits, status=self.status, **self.filters[1])
 
     def accept_and_commit(self):
         keep = self.keep_pq and self.T > 0
@@ -466,6 +612,8 @@ class SpecDecoder:
                                 status=self.status)
 
     def run(self):
+        if self.pages:
+            self.pages.reserve(self.pos_base, self.k + 1, self.status)
         for i in range(self.k):
             self.draft_step(i)
         self.verify()
@@ -499,7 +647,11 @@ class DirectDecoder(SpecDecoder):
     route of high-complexity prompts, and the plain-decoding baseline."""
 
     def __init__(self, weights: DecoderWeights, batch: int | None = None, capacity: int = 1024,
-                 temperature: float = 1.0, history: int = 4096, fuse: bool = True):
+                 temperature: float = 1.0, history: int = 4096, fuse: bool = True, pages: int | None = None,
+                 top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, samples: int = 1):
+        """pages: as in SpecDecoder.  top_k, top_p, min_p: what the filters leave is drawn from (T > 0).  samples: rows come
+        in groups of that many, which continue one prompt each (prefill_packed takes batch / samples of them) and share
+        its pages."""
         self.w = weights
         self.fuse = fuse
         cfg = self.cfg = weights.cfg
@@ -510,7 +662,17 @@ class DirectDecoder(SpecDecoder):
         if B > 64:
             raise ValueError("a parent pass takes at most 64 rows")
         self.dcache = None
-        self.pcache = KVCache(cfg, weights.layers, B, capacity, dev)
+        self._make_pages(pages, capacity)
+        self.samples = int(samples)
+        if self.samples < 1 or B % self.samples or (self.samples > 1 and not self.pages):
+            raise ValueError("samples must divide the batch, and take paged caches")
+        if self.pages:
+            self.pcache = KVCachePaged(cfg, weights.layers, self.pages, dev)
+        else:
+            self.pcache = KVCache(cfg, weights.layers, B, capacity, dev)
+        self.filters = None
+        if filters_wanted(self.T, top_k, top_p, min_p):
+            self.filters = filter_rows(B, self.T, top_k, top_p, min_p, dev)
         self.capacity = capacity
         self.buf = _Buffers(cfg, 64, dev)
         i32 = torch.int32
@@ -529,22 +691,46 @@ class DirectDecoder(SpecDecoder):
         self.graph = None
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(False,), lengths=None):
+        if self.samples > 1:
+            raise ValueError("several samples of a prompt take prefill_packed()")
         super().prefill(prompt, chunk, models=models, lengths=lengths)
 
     def takes_packed(self, models=(False,)) -> bool:
         return super().takes_packed(models)
 
     def prefill_packed(self, prompts, models=(False,)):
-        super().prefill_packed(prompts, models=models)
+        """With samples > 1: one prompt per group of rows, which its first row computes and the others share."""
+        n = self.samples
+        if n == 1:
+            super().prefill_packed(prompts, models=models)
+            return
+        if len(prompts) * n != self.B or any(not 2 <= len(p) <= self.capacity for p in prompts):
+            raise ValueError("one prompt of 2 .. capacity tokens per group of samples")
+        if not self.takes_packed(models):
+            raise ValueError("a projection of this model has no kernel for packed prompts")
+        self._fill_packed([list(p) if i == 0 else [] for p in prompts for i in range(n)], models)
+        i32, dev = torch.int32, self.device
+        first = [g * n for g in range(len(prompts)) for _ in range(n - 1)]
+        child = [g * n + i for g in range(len(prompts)) for i in range(1, n)]
+        length = [len(prompts[g // n]) - 1 for g in first]
+        self.pages.fork(*(torch.tensor(x, dtype=i32, device=dev) for x in (first, child, length)), [self.pcache], self.status)
+        for t in (self.pos_base, self.pending, self.prev):
+            t.copy_(t.view(-1, n)[:, :1].expand(-1, n).reshape(-1))
 
     def set_uniforms(self, u: torch.Tensor, _unused=None):
         self.u.copy_(u.view(self.B, 1))
 
     def run(self):
         B, V = self.B, self.cfg.vocab
+        if self.pages:
+            self.pages.reserve(self.pos_base, 1, self.status)
         self.forward(False, self.pending, None, 1, 0, self.logits, last_only=False)
-        sq.sq_spec_accept(None, self.logits.view(B, 1, V), None, self.u, self.T, n_accepted=self.n_accepted,
-                          next_token=self.next_token)
+        if self.filters:
+            sq.sq_sample_f32(self.logits, self.u.view(B), token=self.next_token, status=self.status, **self.filters)
+            torch.clamp(self.next_token, max=0, out=self.n_accepted)  # (-1: no distribution)
+        else:
+            sq.sq_spec_accept(None, self.logits.view(B, 1, V), None, self.u, self.T, n_accepted=self.n_accepted,
+                              next_token=self.next_token)
         sq.sq_spec_commit(self.n_accepted, self.next_token, None, self.pending, self.prev, self.pos_base,
                           out_tokens=self.out_tokens, out_len=self.out_len, status=self.status)
 

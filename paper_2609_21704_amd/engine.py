@@ -27,8 +27,9 @@ import time
 import torch
 
 from . import synth
+from ._lib import PAGE
 from .configs import HEAD_DIM, Config
-from .decoder import DecoderWeights, DirectDecoder, SpecDecoder
+from .decoder import DecoderWeights, DirectDecoder, SpecDecoder, filters_wanted
 from .router import ROUTES, Router, features, hash_tokenize
 
 _U_DRAFT, _U_ACCEPT, _U_DIRECT = 140, 141, 142  # ids for synth.stream_seed
@@ -58,14 +59,17 @@ def cache_bytes(cfg: Config, layers: int, rows: int, capacity: int, fmt: str = "
 
 
 def placement(cfg: Config, free_bytes: int, batch: int, capacity: int, k: int, layers: int | None = None,
-              margin: float = 0.1, draft_cache: str = "f16") -> dict:
+              margin: float = 0.1, draft_cache: str = "f16", pages: int | None = None) -> dict:
     """Which variants are resident, given the device's free HBM: the parent
     and its direct-decoding cache first (required), then the INT4 draft with
     the caches of its decoder, then the FP8 draft with its own.  `margin` of
-    free_bytes stays unplanned (activations, workspace, allocator slack).
+    free_bytes stays unplanned (activations, workspace, allocator slack).  With `pages` each cache is a pool of that many
+    pages of 64 positions instead of batch rows of `capacity` positions.
     Returns {"resident": [...], "route_to": {route: served_by}, "bytes": {...}}."""
     L = cfg.layers if layers is None else layers
     w = weight_bytes(cfg, L)
+    if pages is not None:
+        batch, capacity = 1, pages * PAGE
     budget = int(free_bytes * (1.0 - margin))
     direct = w["f16"] + cache_bytes(cfg, L, batch, capacity)
     if direct > budget:
@@ -103,8 +107,10 @@ class Engine:
                  capacity: int = 1024, temperature: float = 0.0, router: Router | None = None,
                  chains: int = 1, free_bytes: int | None = None, seed: int | None = None,
                  parent: DecoderWeights | None = None, timed: bool = False, draft_cache: str = "f16",
-                 packed: bool = False):
-        """`draft_cache`: "q4" keeps the drafts' caches in 4 bits.  `packed`: the
+                 packed: bool = False, pages: int | None = None, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
+        """`pages`: the decoders keep their caches in pools of that many pages of 64 positions, taken as the sequences
+        grow.  `top_k`, `top_p`, `min_p`: tokens follow what these leave of the parent's distribution (temperature > 0).
+        `draft_cache`: "q4" keeps the drafts' caches in 4 bits.  `packed`: the
         prompts of a batch go through the models packed, without padding and
         without copies of a prompt for idle rows (`SpecDecoder.prefill_packed`, whose
         attention rounds its weights to one binary16); padded where a projection
@@ -124,8 +130,12 @@ class Engine:
             free_bytes = torch.cuda.mem_get_info(self.device)[0]
         if draft_cache == "q4" and chains != 1:
             raise ValueError("a 4-bit draft cache takes one chain per sequence")
-        self.draft_cache, self.packed = draft_cache, packed
-        self.plan = placement(cfg, free_bytes, batch * chains, capacity, self.k, L, draft_cache=draft_cache)
+        if pages is not None and (chains != 1 or pages < 1 or capacity % PAGE):
+            raise ValueError("paged caches take at least one page, one chain, and a capacity that is a multiple of 64")
+        self.draft_cache, self.packed, self.pages = draft_cache, packed, pages
+        filters_wanted(temperature, top_k, top_p, min_p)
+        self.filters = dict(top_k=top_k, top_p=top_p, min_p=min_p)
+        self.plan = placement(cfg, free_bytes, batch * chains, capacity, self.k, L, draft_cache=draft_cache, pages=pages)
         resident = self.plan["resident"]
         if parent is None:
             first = "int4" if "int4" in resident else ("fp8" if "fp8" in resident else "none")
@@ -149,11 +159,13 @@ class Engine:
             w = self.weights[variant]
             if variant == "f16":
                 self.decoders[variant] = DirectDecoder(w, batch=self.batch, capacity=self.capacity,
-                                                       temperature=self.T, history=self.capacity)
+                                                       temperature=self.T, history=self.capacity, pages=self.pages,
+                                                       **self.filters)
             else:
                 self.decoders[variant] = SpecDecoder(w, batch=self.batch, k=self.k, capacity=self.capacity,
                                                      temperature=self.T, chains=self.chains,
-                                                     history=self.capacity, draft_cache=self.draft_cache)
+                                                     history=self.capacity, draft_cache=self.draft_cache,
+                                                     pages=self.pages, **self.filters)
         return self.decoders[variant]
 
     def tokenize(self, prompt) -> list:
