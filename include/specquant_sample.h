@@ -9,7 +9,7 @@
  *
  * Per row, with logits l_j and the order O: l descending, then the lowest j first (-0 is 0):
  *   weights  w_j = exp((l_j - max l) / T) in fp64 to 2^-39, rounded to fp32; R_j = rint(w_j 2^s),
- *            s = 62 - ceil(log2 v) (sums of R are exact in int64)
+ *            s = min(51, 62 - ceil(log2 v)) (sums of R are exact in int64)
  *   top-k    the first k of O are kept (k <= 0, or k >= v: all)
  *   top-p    of the kept ones the shortest run from the start of O with sum R >= ceil(p Z), Z the sum of R over the
  *            kept ones, p Z and its ceil in fp64, at least the first token (p >= 1: all)

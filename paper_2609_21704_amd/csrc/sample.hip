@@ -46,7 +46,8 @@ struct SampleArgs {
   int32_t* token;  // null: filter
   float* out;
   int32_t* status;
-  int segments, run;  // of a row, of kWaves runs each; tokens of a run
+  int segments, run;  // of a row, of kWaves runs each; tokens of a run, a multiple of four
+  bool aligned;       // rows start on 16 bytes and are a multiple of them long
   int shift;          // log2 of the largest weight
 };
 
@@ -114,7 +115,12 @@ struct Weight {
 #pragma unroll
     for (int i = 0; i < 8; ++i) asm("" : "+v"(q[i]));
   }
-  __device__ __forceinline__ float w(float l) const {
+  // A weight as the fp32 of 2^f and its power of two.
+  struct Value {
+    float m;
+    int n;
+  };
+  __device__ __forceinline__ Value operator()(float l) const {
     const double y = fmax(((double)l - hi) * c, -2000.0);  // (-inf too)
     const double k = y + magic;  // rint(y) in the low mantissa bits
     const double f = y - (k - magic);
@@ -122,16 +128,18 @@ struct Weight {
 #pragma unroll
     for (int i = 1; i < 8; ++i) p = __builtin_fma(p, f, q[i]);
     p = __builtin_fma(p, f, 1.0);
-    return ldexpf((float)p, (int)(uint32_t)__builtin_bit_cast(uint64_t, k));
+    return {(float)p, (int)(uint32_t)__builtin_bit_cast(uint64_t, k)};
   }
-  // rint(w 2^shift), ties to even, from the bits of w in [0, 1]
-  __device__ __forceinline__ int64_t r(float w) const {
-    const uint32_t u = __builtin_bit_cast(uint32_t, w);
-    const int e = (int)(u >> 23) - 150 + shift;
-    const uint32_t m = u < 0x00800000u ? 0u : (u & 0x7FFFFFu) | 0x800000u;  // (below 2^-126: 0 on every grid)
-    if (e >= 0) return (int64_t)m << e;
-    const int k = -e < 26 ? -e : 26;
-    return (m + ((1u << (k - 1)) - 1) + ((m >> k) & 1)) >> k;
+  static __device__ __forceinline__ float fp32(Value v) { return ldexpf(v.m, v.n); }
+  // rint(w 2^shift), ties to even: what the sum with 2^52 holds in its mantissa (shift <= 51)
+  __device__ __forceinline__ int64_t grid(Value v) const {
+    const double x = ldexp((double)v.m, v.n + shift) + 0x1p52;
+    return __builtin_bit_cast(int64_t, x) - 0x4330000000000000;
+  }
+  // the same of a token that min_p keeps, 0 for the others
+  __device__ __forceinline__ int64_t kept(float l, float min_p) const {
+    const Value v = (*this)(l);
+    return fp32(v) >= min_p ? grid(v) : 0;
   }
 };
 
@@ -149,36 +157,55 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 // `last`, `at` in (and everything before it in the order) against (l, j)
 __device__ __forceinline__ bool up_to(float l, int j, float last, int at) { return l > last || (l == last && j <= at); }
 
-// f(l, j) for the tokens from .. to, of which a wavefront (stride 64) or the workgroup takes every stride-th, kAhead loads
-// ahead of their use.  f's code stands there once: a workgroup runs through these kernels' code a few times only, and
-// fetching it is a part of their time.
-constexpr int kAhead = 6;
+// f(l, j) for the tokens from .. to (from a multiple of four), four consecutive ones a load: of the fours a wavefront (stride
+// 64) or the workgroup takes every stride-th, the next two on their way while one is worked on (in registers of their own:
+// handed on from one to the next they would be waited for).
 template <class F>
-__device__ __forceinline__ void each_token(const float* row, int from, int to, int first, int stride, F f) {
+__device__ __forceinline__ void each_token(const SampleArgs& a, const float* row, int from, int to, int first, int stride,
+                                           F f) {
   if (from >= to) return;
-  int j = from + first;
-  float x[kAhead];
+  const int q1 = (to + 3) >> 2;
+  auto load = [&](int q) {
+    float4_t v;
+    if (a.aligned) {  // uniform; (rows are a multiple of four long, so the last load lies in its row)
+      v = reinterpret_cast<const float4_t*>(row)[min(q, q1 - 1)];
+    } else {
 #pragma unroll
-  for (int e = 0; e < kAhead; ++e) x[e] = row[min(j + e * stride, to - 1)];
+      for (int i = 0; i < 4; ++i) v[i] = row[min(4 * q + i, to - 1)];
+    }
+    return v;
+  };
+  auto use = [&](float4_t v, int q) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f(v[i], 4 * q + i);
+  };
+  int base = from >> 2;
+  float4_t x = load(base + first), y = load(base + stride + first);
 #pragma unroll 1
-  for (; j < to; j += stride) {
-    const float now = x[0];
+  for (; base + 2 * stride <= to >> 2; base += 2 * stride) {  // uniform: all lanes' fours are whole
+    use(x, base + first);
+    x = load(base + 2 * stride + first);
+    use(y, base + stride + first);
+    y = load(base + 3 * stride + first);
+  }
+#pragma unroll 1
+  for (int e = 0; e < 2; ++e) {  // the rest
+    const int j = 4 * (base + e * stride + first);
 #pragma unroll
-    for (int e = 0; e + 1 < kAhead; ++e) x[e] = x[e + 1];
-    x[kAhead - 1] = row[min(j + kAhead * stride, to - 1)];
-    f(now, j);
+    for (int i = 0; i < 4; ++i)
+      if (j + i < to) f(e ? y[i] : x[i], j + i);
   }
 }
 // ... of this wavefront's run of a segment
 template <class F>
 __device__ __forceinline__ void each_of_run(const SampleArgs& a, const float* row, int run, F f) {
   const int from = (int)min((int64_t)run * a.run, (int64_t)a.v), to = (int)min((int64_t)from + a.run, (int64_t)a.v);
-  each_token(row, from, to, threadIdx.x & 63, kWave, f);
+  each_token(a, row, from, to, threadIdx.x & 63, kWave, f);
 }
 // ... and of the whole row
 template <class F>
 __device__ __forceinline__ void each_of_row(const SampleArgs& a, const float* row, F f) {
-  each_token(row, 0, a.v, threadIdx.x, kThreads, f);
+  each_token(a, row, 0, a.v, threadIdx.x, kThreads, f);
 }
 
 // Exclusive prefix sum over the workgroup in thread order, and the workgroup's sum: as the acceptance's, but the wavefronts'
@@ -387,10 +414,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8, 8))
       }
       return;
     }
-    auto weight = [&](float l, int) -> int64_t {
-      const float w = wt.w(l);
-      return w >= p.min_p ? wt.r(w) : 0;
-    };
+    auto weight = [&](float l, int) { return wt.kept(l, p.min_p); };
     int64_t s = 0;
     each_of_run(a, logits, seg * kWaves + (tid >> 6), [&](float l, int j) { s += weight(l, j); });
     s = wave_sum_i64(s);
@@ -412,8 +436,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8, 8))
     const int b = bin_of(c.hi, scale, l);
     if (by_count) atomicAdd(&counts[b], 1u);
     if (by_mass) {
-      const int64_t r = wt.r(wt.w(l));
-      if (r) atomicAdd((unsigned long long*)&sums[b], (unsigned long long)r);
+      atomicAdd((unsigned long long*)&sums[b], (unsigned long long)wt.grid(wt(l)));
     }
   });
   __syncthreads();
@@ -597,10 +620,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
   each_of_run(a, logits, seg * kWaves + (tid >> 6), [&](float l, int j) {
     const int b = bin_of(cut.hi, cut.scale, l);
     if (b < cut.sure) {
-      if (a.token) {
-        const float w = wt.w(l);
-        s += w >= p.min_p ? wt.r(w) : 0;
-      }
+      if (a.token) s += wt.kept(l, p.min_p);
     } else if (b == cut.bk || (b >= cut.g0 && b <= cut.g1)) {
       const int at = atomicAdd(&found, 1);
       if (at < kMost) list[at] = (int64_t)j << 32 | __builtin_bit_cast(uint32_t, l);
@@ -639,7 +659,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
         l[e] = __builtin_bit_cast(float, (uint32_t)x);
         j[e] = (int)(x >> 32);
         b[e] = bin_of(cut.hi, cut.scale, l[e]);
-        r[e] = wt.r(wt.w(l[e]));
+        r[e] = wt.grid(wt(l[e]));
       }
     }
     // the place of a token in its bin, in kBins steps
@@ -705,7 +725,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < kHeld; ++e) {
-        if (tid + e * kThreads < n && up_to(l[e], j[e], last, last_at) && wt.w(l[e]) >= p.min_p)
+        if (tid + e * kThreads < n && up_to(l[e], j[e], last, last_at) && wt.fp32(wt(l[e])) >= p.min_p)
           atomicAdd((unsigned long long*)&runs[j[e] / a.run], (unsigned long long)r[e]);
       }
       __syncthreads();
@@ -726,7 +746,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
     if (by_mass) {
       auto weight = [&](float l, int j) -> int64_t {
         const uint32_t k = key_of(l);
-        return k < key || (k == key && j <= at) ? wt.r(wt.w(l)) : 0;
+        return k < key || (k == key && j <= at) ? wt.grid(wt(l)) : 0;
       };
       int64_t z = 0;
       each_of_row(a, logits, [&](float l, int j) { z += weight(l, j); });
@@ -751,8 +771,7 @@ __global__ __launch_bounds__(kThreads) void cut_kernel(SampleArgs a, Scratch sc)
   }
   auto weight = [&](float l, int j) -> int64_t {
     if (!(bin_of(cut.hi, cut.scale, l) < sure || up_to(l, j, last, last_at))) return 0;
-    const float w = wt.w(l);
-    return w >= p.min_p ? wt.r(w) : 0;
+    return wt.kept(l, p.min_p);
   };
   if (!settled) sum_runs(a, logits, runs, weight);
   draw(a, row, runs, weight, sh, &shi);
@@ -770,7 +789,7 @@ __global__ __launch_bounds__(kThreads) void filter_kernel(SampleArgs a, Scratch 
     bool keep = true;
     if (cut.mode == kCut) keep = greedy ? j == cut.last_at
                                         : bin_of(cut.hi, cut.scale, l) < cut.sure || up_to(l, j, cut.last, cut.last_at);
-    if ((cut.mode == kCut || cut.mode == kAll) && !greedy && keep && p.min_p > 0.f) keep = wt.w(l) >= p.min_p;
+    if ((cut.mode == kCut || cut.mode == kAll) && !greedy && keep && p.min_p > 0.f) keep = wt.fp32(wt(l)) >= p.min_p;
     out[j] = cut.mode == kNan ? __builtin_nanf("") : (keep ? l : -INFINITY);
   });
 }
@@ -785,14 +804,20 @@ hipError_t launch_sample(const float* logits, int m, int v, int64_t ld, const fl
                          const float* top_p, const float* min_p, const uint32_t* u24, int32_t* token, float* out,
                          int32_t* status, hipStream_t stream) {
   const int rows = m < kRowsAtOnce ? m : kRowsAtOnce;
-  SampleArgs a{logits, v, ld, temperature, top_p, min_p, top_k, u24, token, out, status, 1, v, 62};
+  SampleArgs a{logits, v, ld, temperature, top_p, min_p, top_k, u24, token, out, status, 1, v, false, 51};
+  a.aligned = (uintptr_t)logits % 16 == 0 && ld % 4 == 0;
   while (a.shift > 0 && (int64_t(1) << (62 - a.shift)) < v) --a.shift;
-  // segments: two workgroups a CU over all rows, none shorter than pays
-  int segments = (2 * cu_count() + rows - 1) / rows;
-  const int most = (v + kMinSegment - 1) / kMinSegment;
-  segments = segments > kMaxSegments ? kMaxSegments : segments;
-  a.segments = segments > most ? most : segments;
-  a.run = (v + a.segments * kWaves - 1) / (a.segments * kWaves);
+  // Segments: as many workgroups as run at once over all rows (two a CU, one of cut_kernel, whose registers allow no more:
+  // at 64 rows of 151936 logits 27 us for 34 with two), none shorter than pays.
+  auto cut_up = [&](SampleArgs& b, int at_once) {
+    int n = at_once / rows;
+    const int most = (v + kMinSegment - 1) / kMinSegment;
+    n = n > kMaxSegments ? kMaxSegments : n;
+    n = n > most ? most : n;
+    b.segments = n < 1 ? 1 : n;
+    b.run = ((v + b.segments * kWaves - 1) / (b.segments * kWaves) + 3) / 4 * 4;
+  };
+  cut_up(a, 2 * cu_count());
   const size_t rs = (size_t)rows * a.segments;
   const size_t bytes[] = {rs * sizeof(Cell),        rs * kBins * 8,             rs * kWaves * 8,  rs * kBins * 4,
                           (size_t)rows * kMost * 8, (size_t)rows * sizeof(Cut), (size_t)rows * 16};
@@ -826,10 +851,12 @@ hipError_t launch_sample(const float* logits, int m, int v, int64_t ld, const fl
     if (b.u24) b.u24 += r0;
     if (b.token) b.token += r0;
     if (b.out) b.out += r0 * ld;
+    SampleArgs c = b;
+    cut_up(c, cu_count());
     const dim3 grid((unsigned)(n * a.segments)), block(kThreads);
     hipLaunchKernelGGL(range_kernel, grid, block, 0, stream, b, sc);
     hipLaunchKernelGGL(bins_kernel, grid, block, 0, stream, b, sc);
-    if (top_k || top_p) hipLaunchKernelGGL(cut_kernel, grid, block, 0, stream, b, sc);
+    if (top_k || top_p) hipLaunchKernelGGL(cut_kernel, dim3((unsigned)(n * c.segments)), block, 0, stream, c, sc);
     if (out) hipLaunchKernelGGL(filter_kernel, grid, block, 0, stream, b, sc);
   }
   return hipGetLastError();

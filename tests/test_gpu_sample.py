@@ -26,7 +26,7 @@ def kept(x, temp, k, p, mp):
         return keep.astype(np.int64), keep
     z = x / np.float64(np.float32(temp))
     w = np.exp(z - z.max()).astype(np.float32)
-    r = np.rint(w.astype(np.float64) * 2.0 ** (62 - (v - 1).bit_length())).astype(np.int64)
+    r = np.rint(w.astype(np.float64) * 2.0 ** min(51, 62 - (v - 1).bit_length())).astype(np.int64)
     order = np.lexsort((np.arange(v), -x))
     if 0 < k < v:
         order = order[:k]
