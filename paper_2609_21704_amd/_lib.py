@@ -909,7 +909,7 @@ def sq_page_copy(pool, src, dst, count, status=None):
     layers, pages = pool.shape[:2]
     n = min(src.shape[0], dst.shape[0], 1 << 20)
     _launch("sq_page_copy", (pool, src, dst, count, status), pool.data_ptr(), layers, pages,
-            pool[0, 0].numel() * pool.element_size(), _ints(src, n, "src"), _ints(dst, n, "dst"), _ints(count, 1, "count"),
+            pool.numel() // max(1, layers * pages) * pool.element_size(), _ints(src, n, "src"), _ints(dst, n, "dst"), _ints(count, 1, "count"),
             n, _status_word(status))
 
 

@@ -191,8 +191,15 @@ def test_a_pool_that_runs_out():
     dims, model = parent_model(w)
     for i, n in ((0, 20), (1, 4)):
         check_greedy(dims, model, prompts[i], d.out_tokens[i, :n].tolist(), f"sequence {i}")
-    with pytest.raises(RuntimeError, match="status|no token"):
-        Engine(cfg, DEV, layers=3, batch=2, capacity=256, pages=2, parent=w).generate(prompts, 20, routes=["f16"] * 2)
+    eng = Engine(cfg, DEV, layers=3, batch=2, capacity=256, pages=2, parent=w)
+    with pytest.raises(RuntimeError, match="no token .*status flags"):
+        eng.generate(prompts, 20, routes=["f16"] * 2)
+    assert len(eng.generate(prompts, 3, routes=["f16"] * 2)[1].tokens) == 3  # the next requests fit
+    # rows that have their tokens may run out while the others go on
+    eng = Engine(cfg, DEV, layers=3, batch=2, capacity=256, pages=4, parent=w, k=3)
+    got = [r.tokens for r in eng.generate(prompts, 40, routes=["int4"] * 2)]
+    for i, p in enumerate(prompts):
+        check_greedy(dims, model, p, got[i], f"request {i}")
 
 
 def test_refusals():
