@@ -191,7 +191,8 @@ __global__ __launch_bounds__(kThreads) void pages_fork_kernel(PageState p, const
     const int hp = p.held[pa];
     ok = p.held[ch] == 0 && hp > 0 && hp <= p.width && len >= 1 && len <= (int64_t)hp * kPage;
   }
-  for (int j = 0; j < n; j += 4) {  // (the same words for all; past n they are -1)
+  const int before = __any(ok) ? n : 0;  // (wavefronts without a pair need not look)
+  for (int j = 0; j < before; j += 4) {  // (the same words for all; past n they are -1)
     const int4 c = *reinterpret_cast<const int4*>(&sc[j]);
     if ((j < tid && c.x == ch) || (j + 1 < tid && c.y == ch) || (j + 2 < tid && c.z == ch) || (j + 3 < tid && c.w == ch))
       ok = false;
