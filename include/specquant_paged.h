@@ -77,8 +77,9 @@ sq_status sq_page_copy(void* pool, int32_t layers, int64_t pages, int64_t page_b
  *   k_codes [pages][hkv][64][64], v_codes [pages][hkv][64][64] u8, k_scales [pages][hkv][64][4], v_scales
  *   [pages][hkv][4][64] fp16 (one block of 64 positions each of the 4-bit cache's layout)
  * with table [b][width] in the place of the capacity; 1 <= len_bound <= 64 width, width and pages as above.
- * Results are the bits of those calls over a cache with the same entries where the keys are split alike (single tokens
- * and small blocks of more than half as many sequences as CUs per kv head are split here, where they differ in length).
+ * Results are the bits of those calls over a cache with the same entries and capacity, but for the attention of few rows
+ * (at most 32 queries of a kv head, 4-bit 64) of more than 128 / hkv sequences: there those calls take a sequence's keys
+ * whole, and these cut all sequences' keys into equal shares, whose sums take at most 34 MiB of the library workspace.
  * A position whose table entry is outside [0, pages) has no entry: a row there is treated as one at a bad position
  * (nothing written, NaN in q_out, k_out and v_out) and sets SQ_DEV_BAD_PAGE; a row that reads one gets NaN in out.
  * Writing into a page that several rows hold changes it for all of them. */
