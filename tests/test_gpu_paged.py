@@ -223,6 +223,75 @@ def test_attention(seqs, hq, hkv, shared, q4):
     assert torch.equal(again[inside], out[inside])
 
 
+@pytest.mark.parametrize("seqs,hq,hkv", [([(1, 700), (1, 0), (1, 5000)], 28, 4), ([(2, 300)] * 5, 8, 8),
+                                         ([(1, 30 * i) for i in range(40)], 28, 4), ([(9, 1000), (9, 77)], 28, 4),
+                                         ([(40, 4000)], 28, 4), ([(300, 0), (129, 64), (0, 3)], 12, 2)])
+@pytest.mark.parametrize("q4", [False, True])
+def test_the_bits_of_contiguous_caches(seqs, hq, hkv, q4):
+    """The attention over a contiguous cache with the same entries, wherever the sequences' keys are split as there."""
+    lens, past = [n for n, _ in seqs], [p for _, p in seqs]
+    table, pages = tables([n + p for n, p in seqs], 31)
+    pool, _ = pool_of(table, pages, lens, past, hkv, q4, 32)
+    ids = table.clamp(min=0).long()  # (entries of no page are never read)
+    if q4:
+        whole = [pool[0][ids].permute(0, 2, 1, 3, 4).flatten(2, 3), pool[1][ids].permute(0, 2, 1, 3, 4).flatten(2, 3),
+                 pool[2][ids].transpose(1, 2), pool[3][ids].transpose(1, 2)]
+    else:
+        whole = [pool[0][ids].permute(0, 2, 1, 3, 4).flatten(2, 3), pool[1][ids].permute(0, 2, 3, 1, 4).flatten(3, 4)]
+    rows = sum(lens)
+    q = normal((rows, hq, 128), 33, rows)
+    args = dict(max_rows=max(lens), len_bound=max(n + p for n, p in seqs))
+    got = calls(q4)[2](q, *pool, table, starts(lens), ints(past), **args)
+    want = calls(q4)[3](q, *[x.contiguous() for x in whole], starts(lens), ints(past), **args)
+    if 2 * len(seqs) * hkv > 256 and max(lens) * (hq // hkv) <= (64 if q4 else 32):  # cut into equal shares instead
+        assert float((got.double() - want.double()).abs().max()) <= 2.0 ** -9 * float(want.abs().max())
+    else:
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 9, 130])
+@pytest.mark.parametrize("q4", [False, True])
+def test_offsets_past_32_bits(rows, q4):
+    """Pages whose bytes lie beyond 4 GiB of a pool's array: as the same pages at its start."""
+    hq, hkv, past = 16, 8, [500, 63]
+    paged_rope, _, paged, _ = calls(q4)
+    pages = 140000 if q4 else 40000
+    small, n = tables([p + rows for p in past], 41, spare=0, extra=0)
+    pool = nan_pool(n, hkv, q4)
+    far = [torch.empty((pages, *x.shape[1:]), dtype=x.dtype, device=DEV) for x in pool]
+    assert far[0].numel() * far[0].element_size() > 1 << 32
+    shift = pages - n
+    for x, y in zip(pool, far):
+        y[shift:] = x  # (what no position writes)
+    big = torch.where(small >= 0, small + shift, small)
+    # all positions written, then the last ones once more with their queries
+    ends = [p + rows for p in past]
+    qkv = normal((sum(ends), (hq + 2 * hkv) * 128), 42, rows).float()
+    new = normal((2 * rows, (hq + 2 * hkv) * 128), 43, rows).float()
+    outs = []
+    for cache, table in ((pool, small), (far, big)):
+        paged_rope(qkv, None, starts(ends), ints([0, 0]), hq, *cache, table, max_rows=max(ends))
+        q = paged_rope(new, None, None, ints(past), hq, *cache, table, max_rows=rows)
+        outs.append(paged(q, *cache, table, None, ints(past), max_rows=rows))
+    assert torch.equal(outs[0], outs[1]) and bool(torch.isfinite(outs[0]).all())
+    used = sorted({i for row in small.tolist() for i in row if i >= 0})
+    for x, y in zip(pool, far):
+        assert torch.equal(bits(x[used]), bits(y[shift:][used]))
+
+
+def test_a_list_of_steps_past_32_bits():
+    """So many and such wide rows that the bound of their steps counts several as one."""
+    hq, hkv, b, width = 8, 4, 300, 1 << 20
+    past = [(i * 37) % 1500 for i in range(b)]
+    small, pages = tables([p + 1 for p in past], 51, extra=0)
+    pool, (k, v) = pool_of(small, pages, [1] * b, past, hkv, False, 52)
+    table = torch.full((b, width), -1, dtype=I32, device=DEV)
+    table[:, :small.shape[1]] = small
+    q = normal((b, hq, 128), 53)
+    out = sq.sq_paged_attention_f16(q, *pool, table, None, ints(past), max_rows=1)
+    check_attention(out, exact(q, k, v, [1] * b, past, list(range(b))), v, hq, True)
+
+
 @pytest.mark.parametrize("rows,hq,hkv", [(1, 28, 4), (2, 28, 4), (9, 28, 4), (9, 8, 8), (100, 12, 2)])
 @pytest.mark.parametrize("q4", [False, True])
 def test_pages_outside_the_pool(rows, hq, hkv, q4):

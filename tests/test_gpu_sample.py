@@ -120,6 +120,22 @@ def test_ties(v):
     check(x, SETTINGS * len(rows))
 
 
+def test_large():
+    """A vocabulary of millions, and rows that lie more than 2^31 logits apart."""
+    g = torch.Generator().manual_seed(21)
+    v = (1 << 22) + 3
+    check(torch.randn(3, v, generator=g) * 2, [(0.9, 1000, 0.9, 0.0), (1.0, 0, 0.99, 0.0), (1.3, 0, 1.0, 0.01)], draws=2)
+    x, far = torch.randn(4, 999, generator=g), torch.empty(4, 1 << 30, device=DEV)
+    far[:, :999] = x.to(DEV)
+    settings = [(0.8, 50, 0.95, 0.0), (1.0, 0, 1.0, 0.0), (0.0, 0, 1.0, 0.0), (1.0, 20, 1.0, 0.1)]
+    u = torch.randint(0, 1 << 24, (4,), generator=g, dtype=torch.int32)
+    got = sq.sq_sample_f32(far, u.to(DEV), vocab=999, **device(settings)).tolist()
+    assert got == [token(x[i].numpy(), int(u[i]), *s) for i, s in enumerate(settings)]
+    sq.sq_filter_logits_f32(far, vocab=999, out=far, **device(settings))
+    want = sq.sq_filter_logits_f32(x.to(DEV), **device(settings))
+    assert torch.equal(far[:, :999], want)
+
+
 def test_far_apart():
     """Logits at the ends of fp32, and temperatures that take their quotients there."""
     v = 3000
