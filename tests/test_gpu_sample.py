@@ -120,6 +120,24 @@ def test_ties(v):
     check(x, SETTINGS * len(rows))
 
 
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 95, 96, 97, 130, 511, 512, 513])
+@pytest.mark.parametrize("step", [0.0, 2.0 ** -22])
+def test_crowded(n, step):
+    """Cuts at the ends of and inside a group of n tokens that no bins tell apart, up to more than are ranked."""
+    g = torch.Generator().manual_seed(n)
+    v = 3000
+    x = torch.randn(v, generator=g) * 4
+    order = torch.randperm(v, generator=g)[:n]
+    x[order] = 2.0 + step * torch.randint(0, 9, (n,), generator=g)
+    above = int((x > 3.0).sum())
+    cuts = sorted({above + i for i in (1, n // 3 + 1, n - 1, n, n + 1)} | {max(above, 1)})
+    full = torch.softmax(x.double(), 0)
+    mass, group = float(full[x > 3.0].sum()), float(full[order].sum())
+    settings = [(1.0, k, 1.0, 0.0) for k in cuts if k > 0] + [(1.0, 0, mass + p * group, 0.0) for p in (0.01, 0.5, 0.99)] \
+        + [(1.0, above + n // 2 + 1, p, 0.0) for p in (0.5, 0.9, 0.999)]
+    check(x.repeat(len(settings), 1), settings)
+
+
 def test_large():
     """A vocabulary of millions, and rows that lie more than 2^31 logits apart."""
     g = torch.Generator().manual_seed(21)
