@@ -330,6 +330,12 @@ class SpecDecoder:
             self.pages.trim(torch.zeros((self.R,), dtype=torch.int32, device=self.device), self.status)
             self.pages.reserve(torch.tensor(lengths, dtype=torch.int32, device=self.device), 0, self.status)
 
+    def _silence(self):
+        """Rows that found no pages for their prompt (pos_base entries of it) lose their position: pages that become free
+        later do not hold it, so such a row takes none and emits nothing."""
+        if self.pages:
+            self.pos_base.masked_fill_(self.pages.held * sq.PAGE < self.pos_base, -1)
+
     # ------------------------------------------------------------- passes
     def _linear(self, draft: bool, key, x, y):
         st = self.w.stack
@@ -517,6 +523,7 @@ class SpecDecoder:
         self.pending.copy_(torch.tensor([p[-1] if p else 0 for p in prompts], dtype=i32))
         self.prev.copy_(torch.tensor([p[-2] if p else 0 for p in prompts], dtype=i32))
         self.out_len.zero_()
+        self._silence()
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(True, False), lengths=None):
         """Feed prompt [B][Lp] (int32) but its last token to both models
@@ -529,7 +536,8 @@ class SpecDecoder:
         padding.  Every row is fed Lp - 1 tokens; a short row's entries from
         its last prompt position on are rewritten before any row attends to
         them, as a rolled-back draft block's are, so the padding is never
-        read."""
+        read.  Over pages every row takes those of its own length; padding past
+        them is not written."""
         B, Lp = prompt.shape
         if B != self.B or Lp < 2 or Lp > self.capacity:
             raise ValueError("prompt must be [batch][2 .. capacity]")
@@ -544,9 +552,26 @@ class SpecDecoder:
         rows = torch.arange(self.R)
         last, before = host[rows, lens - 1].contiguous(), host[rows, lens - 2].contiguous()
         prompt = host.to(self.device)
-        R = self.R
-        self._refill([Lp - 1] * R)  # (padding is written too)
+        self._refill((lens - 1).tolist())
         self.pos_base.zero_()
+        status = self.status
+        if self.pages:
+            self.status = torch.zeros_like(status)
+        try:
+            self._prefill_padded(prompt, chunk, models)
+        finally:
+            found, self.status = self.status, status
+        if self.pages:  # padding has no pages past its row's own, and a row that lacks some of these has SQ_DEV_NO_PAGES
+            status.bitwise_or_(found & ~sq.DEV_BAD_PAGE)
+        self.pos_base.copy_((lens - 1).to(torch.int32))
+        self.pending.copy_(last)
+        self.prev.copy_(before)
+        self.out_len.zero_()
+        self._silence()
+
+    def _prefill_padded(self, prompt, chunk, models):
+        """The passes of prefill(), over prompt [R][Lp] from position 0 on."""
+        R, Lp = prompt.shape
         for draft in models:
             # blocks of up to PREFILL_ROWS rows; a block of up to 64 goes through the streaming projections
             c = max(1, min(chunk or PREFILL_ROWS, PREFILL_ROWS // R))
@@ -559,12 +584,6 @@ class SpecDecoder:
                     rest = prompt[:, s + 1:s + n].t().contiguous() if n > 1 else None
                     self.forward(draft, first, rest, n, s, None, last_only=False, len_bound=s + n)
                 s += n
-        if self.pages:
-            self.pages.trim((lens - 1).to(device=self.device, dtype=torch.int32), self.status)
-        self.pos_base.copy_((lens - 1).to(torch.int32))
-        self.pending.copy_(last)
-        self.prev.copy_(before)
-        self.out_len.zero_()
 
     # -------------------------------------------------------------- round
     def draft_step(self, i: int):
@@ -716,6 +735,7 @@ class DirectDecoder(SpecDecoder):
         self.pages.fork(*(torch.tensor(x, dtype=i32, device=dev) for x in (first, child, length)), [self.pcache], self.status)
         for t in (self.pos_base, self.pending, self.prev):
             t.copy_(t.view(-1, n)[:, :1].expand(-1, n).reshape(-1))
+        self._silence()
 
     def set_uniforms(self, u: torch.Tensor, _unused=None):
         self.u.copy_(u.view(self.B, 1))

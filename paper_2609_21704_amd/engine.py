@@ -226,6 +226,9 @@ class Engine:
             t0 = self._clock()
             dec.prefill(prompt, lengths=[len(t) for t in rows])
         t1 = self._clock()
+        if self.pages is not None and int(dec.pos_base[:n].min()) < 0:
+            raise RuntimeError(f"the batch's prompts find no pages in a pool of {self.pages} (device status flags "
+                               f"{self._flags(dec)})")
         per_round = 1 if variant == "f16" else self.k + 1
         r = 0
         while True:
