@@ -243,6 +243,11 @@ sq_status sq_spec_accept_noalloc(const float* draft_logits, const float* target_
 #define SQ_DEV_NO_DIST 8   /* a round with n_accepted < 0: that sequence kept its
                               state                                                 */
 
+/* pos_base[s] of a sequence that takes no part: sq_spec_commit leaves its state
+ * as it is and raises nothing, the calls over pages (specquant_paged.h) give it
+ * no rows.  Elsewhere it is a position outside the bounds. */
+#define SQ_POS_IDLE INT32_MIN
+
 /* Token embedding of a block: h[s][j] = table[tok(s, j)] widened to fp32, with
  * tok(s, 0) = first[s] and tok(s, 1 + i) = rest[i][s] (rest position-major
  * [kd][b], as draft_tokens of sq_spec_accept): the pending token followed by
@@ -367,7 +372,8 @@ sq_status sq_silu_mul_f16(const float* gu, int64_t m, int64_t inter, uint16_t* t
  *     (entries at or past out_capacity are not stored: SQ_DEV_OVERFLOW);
  *   out_len[s] += n + 1;  prev[s] = n > 0 ? draft_tokens[n - 1][s] : pending[s];
  *   pending[s] = next_token[s];  pos_base[s] += n + 1.
- * A sequence with n outside [0, kd] keeps its state (SQ_DEV_NO_DIST).
+ * A sequence with n outside [0, kd] keeps its state (SQ_DEV_NO_DIST), one with
+ * pos_base[s] = SQ_POS_IDLE too, whatever its n.
  * draft_tokens [kd][b] (NULL when kd == 0); pending, prev, pos_base, out_len [b]
  * in/out; out_tokens [b][out_capacity] out, NULL to keep no history (then
  * out_len may be NULL). 1 <= b < 2^24, 0 <= kd <= 64. */

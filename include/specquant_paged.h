@@ -82,7 +82,9 @@ sq_status sq_page_copy(void* pool, int32_t layers, int64_t pages, int64_t page_b
  * whole, and these cut all sequences' keys into equal shares, whose sums take at most 34 MiB of the library workspace.
  * A position whose table entry is outside [0, pages) has no entry: a row there is treated as one at a bad position
  * (nothing written, NaN in q_out, k_out and v_out) and sets SQ_DEV_BAD_PAGE; a row that reads one gets NaN in out.
- * Writing into a page that several rows hold changes it for all of them. */
+ * Writing into a page that several rows hold changes it for all of them.
+ * A sequence with pos_base[s] = SQ_POS_IDLE has no rows, whatever row_start gives it: they are left as they were, and no
+ * bit is set.  So rows of a batch may be idle without pages. */
 sq_status sq_paged_rope_kv_f16(const float* qkv, const uint16_t* bias, const int32_t* row_start, int32_t b,
                                int64_t rows, int64_t max_rows, int32_t hq, int32_t hkv, const int32_t* pos_base,
                                int32_t pos_offset, int64_t len_bound, const int32_t* table, int64_t width,

@@ -116,6 +116,7 @@ EXPORTED = ("sq_abi_version", "sq_status_str", "sq_quantize_int4_g128", "sq_quan
 
 # device status bits (SQ_DEV_* of include/specquant.h)
 DEV_BAD_TOKEN, DEV_BAD_POS, DEV_OVERFLOW, DEV_NO_DIST = 1, 2, 4, 8
+POS_IDLE = -(1 << 31)  # a position that takes a sequence out of the calls over pages and of sq_spec_commit
 DEV_BAD_ROWS = 16  # of include/specquant_packed.h
 DEV_NO_PAGES, DEV_BAD_PAGE, DEV_BAD_FORK = 32, 64, 128  # of include/specquant_paged.h
 DEV_BAD_PARAM = 256  # of include/specquant_sample.h

@@ -6,6 +6,7 @@
 #include "sq_internal.hpp"
 
 static_assert(sq::kPage == SQ_PAGE, "one page size");
+static_assert(sq::kPosIdle == SQ_POS_IDLE, "one mark of idle sequences");
 
 namespace {
 

@@ -983,7 +983,7 @@ __global__ __launch_bounds__(256) void commit_kernel(const int32_t* __restrict__
                                                      int64_t out_capacity, int32_t* __restrict__ out_len,
                                                      int32_t* __restrict__ status) {
   const int bi = blockIdx.x * blockDim.x + threadIdx.x;
-  if (bi >= b) return;
+  if (bi >= b || pos_base[bi] == kPosIdle) return;
   const int n = n_accepted[bi];
   if (n < 0 || n > kd) {  // the round had no distribution for this sequence
     flag(status, kNoDist);

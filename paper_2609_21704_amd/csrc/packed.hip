@@ -27,13 +27,15 @@ struct RowTile {
   int shift;         // pos0 % 16
 };
 
+template <bool Paged>
 __device__ __forceinline__ bool row_tile(const PackedRows& pr, const int32_t* pos_base, int pos_offset, int item,
                                          RowTile& rt) {
   int s, t;
   if (!find_tile(pr.b, item,
                  [&](int i) {
-                   const int n = seq_rows(pr, i).n;
-                   const int sh = (int)(((int64_t)pos_base[i] + pos_offset) & (kTileRows - 1));
+                   const int32_t base = pos_base[i];
+                   const int n = seq_rows(pr, i, base, Paged).n;
+                   const int sh = (int)(((int64_t)base + pos_offset) & (kTileRows - 1));
                    return n > 0 ? (n + sh + kTileRows - 1) / kTileRows : 0;
                  },
                  s, t))
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(256) void packed_rope_kernel(PackedRows pr, RopeArg
     }
   }
   RowTile rt;
-  if (!row_tile(pr, a.pos_base, a.pos_offset, tile_of_block(), rt)) return;  // uniform
+  if (!row_tile<Paged>(pr, a.pos_base, a.pos_offset, tile_of_block(), rt)) return;  // uniform
   const int nh = a.hq + 2 * a.hkv, turned = a.hq + a.hkv, share = blockIdx.y, shares = gridDim.y;
   const int per = (turned + shares - 1) / shares, head0 = share * per;
   const int head1 = head0 + per < turned ? head0 + per : turned;
@@ -314,7 +316,7 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedRows pr, const i
   __shared__ __align__(16) uint8_t vb[64][kTileRows];
   const int tid = threadIdx.x, t = tid & 15, unit = tid >> 4;
   RowTile rt;
-  if (!row_tile(pr, pos_base, pos_offset, tile_of_block(), rt)) return;  // uniform
+  if (!row_tile<Paged>(pr, pos_base, pos_offset, tile_of_block(), rt)) return;  // uniform
   const int64_t base = rt.pos0 - rt.shift;
   bool page_good = true;
   if constexpr (Paged) page_good = tile_page_ok(c, rt.s, base, len_bound);

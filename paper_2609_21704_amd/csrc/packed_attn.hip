@@ -277,8 +277,9 @@ __device__ __forceinline__ int steps_to(int klast) { return klast < 0 ? 0 : klas
 
 // Tiles of TQ queries of a sequence, and its steps.
 __device__ __forceinline__ SeqWork seq_work(const PackedRows& pr, const AttnArgs& a, int G, int TQ, int s) {
-  const int64_t p0 = (int64_t)a.pos_base[s] + a.pos_offset;
-  const SeqRows sr = seq_rows(pr, s);
+  const int32_t base = a.pos_base[s];
+  const int64_t p0 = (int64_t)base + a.pos_offset;
+  const SeqRows sr = seq_rows(pr, s, base, a.c.table != nullptr);
   return {(sr.n * G + TQ - 1) / TQ, steps_to(last_key(p0 + sr.n - 1, a.len_bound)), sr, p0};
 }
 

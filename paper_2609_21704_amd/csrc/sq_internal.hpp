@@ -219,6 +219,7 @@ struct KvCache {
   const int32_t* table = nullptr;
   int width = 0, pages = 0;
 };
+constexpr int32_t kPosIdle = INT32_MIN;  // pos_base of a sequence that takes no part
 constexpr int kPage = 64;  // positions of a page: a step of the attention kernels, a block of 4-bit values
 hipError_t launch_packed_rope_kv(const float* qkv, const uint16_t* bias, const PackedRows& pr, int hq, int hkv,
                                  const int32_t* pos_base, int pos_offset, int64_t len_bound, int64_t capacity,

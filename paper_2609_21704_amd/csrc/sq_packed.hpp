@@ -20,6 +20,13 @@ __device__ __forceinline__ SeqRows seq_rows(const PackedRows& p, int s) {
   return {a, n < p.max_rows ? n : p.max_rows};
 }
 
+// ... in the calls over pages (`paged`), where a sequence without a position has none.
+__device__ __forceinline__ SeqRows seq_rows(const PackedRows& p, int s, int32_t pos_base, bool paged) {
+  SeqRows r = seq_rows(p, s);
+  if (paged && pos_base == kPosIdle) r.n = 0;
+  return r;
+}
+
 // Item `item` of the list (sequence 0: tile 0, 1, ..; sequence 1: ..), with tiles(s) tiles in sequence s, found by
 // every wavefront for itself: 64 sequences a step, one scan of their counts.  False past the end of the list.
 template <class F>

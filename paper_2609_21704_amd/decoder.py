@@ -330,11 +330,13 @@ class SpecDecoder:
             self.pages.trim(torch.zeros((self.R,), dtype=torch.int32, device=self.device), self.status)
             self.pages.reserve(torch.tensor(lengths, dtype=torch.int32, device=self.device), 0, self.status)
 
-    def _silence(self):
-        """Rows that found no pages for their prompt (pos_base entries of it) lose their position: pages that become free
-        later do not hold it, so such a row takes none and emits nothing."""
+    def _settle(self):
+        """The end of a prefill over pages.  Rows that found no pages for their prompt (pos_base entries of it) go idle:
+        pages that become free later do not hold it, so such a row takes none and emits nothing.  The attention leaves
+        the rows of idle sequences as they are, so they start finite, as their logits then are."""
         if self.pages:
-            self.pos_base.masked_fill_(self.pages.held * sq.PAGE < self.pos_base, -1)
+            self.pos_base.masked_fill_(self.pages.held * sq.PAGE < self.pos_base, sq.POS_IDLE)
+            self.buf.a.zero_()
 
     # ------------------------------------------------------------- passes
     def _linear(self, draft: bool, key, x, y):
@@ -490,8 +492,10 @@ class SpecDecoder:
         """prefill() of prompts given as one list of token ids per sequence (2 .. capacity of them), their tokens packed
         one after the other: no padding is computed, and prompts longer than a pass (PREFILL_ROWS rows over all
         sequences) continue in the next.  The attention rounds its weights to one binary16 (prefill() to two), which is
-        up to 5 % on top of the rounding of its outputs."""
-        if len(prompts) != self.B or any(not 2 <= len(p) <= self.capacity for p in prompts):
+        up to 5 % on top of the rounding of its outputs.  Over pages a prompt may be empty: its row is idle, holds no pages
+        and emits nothing."""
+        least = 0 if self.pages else 2
+        if len(prompts) != self.B or any(not least <= len(p) <= self.capacity or len(p) == 1 for p in prompts):
             raise ValueError("one prompt of 2 .. capacity tokens per sequence")
         if not self.takes_packed(models):
             raise ValueError("a projection of this model has no kernel for packed prompts: use prefill()")
@@ -519,11 +523,11 @@ class SpecDecoder:
                 done = [d + n for d, n in zip(done, take)]
                 self._prefill_pass(draft, torch.tensor(toks, dtype=i32, device=self.device), max(take), 0,
                                    packed=(torch.tensor(start, dtype=i32, device=self.device), max(done)))
-        self.pos_base.copy_(torch.tensor([len(p) - 1 for p in prompts], dtype=i32))
+        self.pos_base.copy_(torch.tensor([len(p) - 1 if p else sq.POS_IDLE for p in prompts], dtype=i32))
         self.pending.copy_(torch.tensor([p[-1] if p else 0 for p in prompts], dtype=i32))
         self.prev.copy_(torch.tensor([p[-2] if p else 0 for p in prompts], dtype=i32))
         self.out_len.zero_()
-        self._silence()
+        self._settle()
 
     def prefill(self, prompt: torch.Tensor, chunk: int | None = None, models=(True, False), lengths=None):
         """Feed prompt [B][Lp] (int32) but its last token to both models
@@ -537,7 +541,8 @@ class SpecDecoder:
         its last prompt position on are rewritten before any row attends to
         them, as a rolled-back draft block's are, so the padding is never
         read.  Over pages every row takes those of its own length; padding past
-        them is not written."""
+        them is not written, and a row of length 0 is idle: it holds no pages
+        and emits nothing."""
         B, Lp = prompt.shape
         if B != self.B or Lp < 2 or Lp > self.capacity:
             raise ValueError("prompt must be [batch][2 .. capacity]")
@@ -545,15 +550,17 @@ class SpecDecoder:
             lens = torch.full((B,), Lp, dtype=torch.int64)
         else:
             lens = torch.as_tensor(lengths, dtype=torch.int64).cpu()
-            if lens.shape != (B,) or int(lens.min()) < 2 or int(lens.max()) > Lp:
+            short = lens[lens > 0] if self.pages else lens
+            if lens.shape != (B,) or bool((lens < 0).any()) or bool((short < 2).any()) or int(lens.max()) > Lp:
                 raise ValueError("lengths must be [batch] in 2 .. prompt length")
         host = prompt.to(device="cpu", dtype=torch.int32).repeat_interleave(self.c, dim=0)
         lens = lens.repeat_interleave(self.c)
         rows = torch.arange(self.R)
-        last, before = host[rows, lens - 1].contiguous(), host[rows, lens - 2].contiguous()
+        idle = lens == 0
+        last, before = (host[rows, (lens - i).clamp(min=0)].masked_fill(idle, 0) for i in (1, 2))
         prompt = host.to(self.device)
         self._refill((lens - 1).tolist())
-        self.pos_base.zero_()
+        self.pos_base.copy_(torch.where(idle, sq.POS_IDLE, 0))
         status = self.status
         if self.pages:
             self.status = torch.zeros_like(status)
@@ -563,11 +570,11 @@ class SpecDecoder:
             found, self.status = self.status, status
         if self.pages:  # padding has no pages past its row's own, and a row that lacks some of these has SQ_DEV_NO_PAGES
             status.bitwise_or_(found & ~sq.DEV_BAD_PAGE)
-        self.pos_base.copy_((lens - 1).to(torch.int32))
+        self.pos_base.copy_(torch.where(idle, sq.POS_IDLE, lens - 1))
         self.pending.copy_(last)
         self.prev.copy_(before)
         self.out_len.zero_()
-        self._silence()
+        self._settle()
 
     def _prefill_padded(self, prompt, chunk, models):
         """The passes of prefill(), over prompt [R][Lp] from position 0 on."""
@@ -735,7 +742,7 @@ class DirectDecoder(SpecDecoder):
         self.pages.fork(*(torch.tensor(x, dtype=i32, device=dev) for x in (first, child, length)), [self.pcache], self.status)
         for t in (self.pos_base, self.pending, self.prev):
             t.copy_(t.view(-1, n)[:, :1].expand(-1, n).reshape(-1))
-        self._silence()
+        self._settle()
 
     def set_uniforms(self, u: torch.Tensor, _unused=None):
         self.u.copy_(u.view(self.B, 1))

@@ -214,11 +214,13 @@ class Engine:
     def _run_batch(self, variant: str, toks: list, max_new: int) -> list:
         dec = self.decoder(variant)
         n = len(toks)
+        # idle rows have no prompt over pages, which they would take from the others; elsewhere they are fed two tokens of the
+        # first one, or repeat it
         if self.packed and dec.takes_packed():
             t0 = self._clock()
-            dec.prefill_packed(toks + [toks[0][:2]] * (self.batch - n))  # idle rows: two tokens of the first prompt
+            dec.prefill_packed(toks + [[] if self.pages else toks[0][:2]] * (self.batch - n))
         else:
-            rows = toks + [toks[0]] * (self.batch - n)  # idle rows repeat the first prompt
+            rows = toks + [[] if self.pages else toks[0]] * (self.batch - n)
             Lp = max(len(t) for t in rows)
             prompt = torch.zeros((self.batch, Lp), dtype=torch.int32)
             for i, t in enumerate(rows):

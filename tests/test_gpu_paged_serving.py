@@ -1,8 +1,9 @@
 """GPU tests of what shares a pool of pages with what: padded prompts take the pages of their own lengths, sequences whose
-prompts found none emit nothing, whatever becomes free later."""
+prompts found none emit nothing, whatever becomes free later, and idle rows of a batch hold none."""
 import pytest
 import torch
 
+import paper_2609_21704_amd as sq
 from paper_2609_21704_amd import _lib
 from paper_2609_21704_amd import decoder as dec
 from paper_2609_21704_amd import synth
@@ -100,3 +101,126 @@ def test_padding_past_the_pages_raises_no_status(chunk):
     tokens[1, 7] = cfg.vocab
     d.prefill(tokens, lengths=[10, 200], chunk=chunk)
     assert d.status.item() == _lib.DEV_BAD_TOKEN
+
+
+# ----------------------------------------------------------------- idle rows
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("route", ["f16", "int4", "fp8"])
+def test_one_request_in_a_wide_batch(route, packed):
+    """A pool for one request serves one request, whatever the batch could hold; then two, and one again."""
+    cfg = config(8)
+    eng = Engine(cfg, DEV, layers=3, k=3, batch=8, capacity=256, temperature=0.0, pages=3, packed=packed)
+    prompts = ragged_prompts(cfg, [120, 9, 64, 130], 26)
+    got = []
+    for part, max_new in (([0], 30), ([1, 2], 12), ([3], 30)):
+        got += [r.tokens for r in eng.generate([prompts[i] for i in part], max_new, routes=[route] * len(part))]
+        d = eng.decoders[route]
+        assert d.pages.held[len(part):].tolist() == [0] * (8 - len(part)) and d.status.item() == 0
+    dims, model = parent_model(eng.weights["f16"])
+    for i, p in enumerate(prompts):
+        check_greedy(dims, model, p, got[i], f"{route} {i}")
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("kind", ["direct", "spec", "filtered"])
+def test_idle_rows_keep_their_state(kind, packed):
+    """An idle row between others: its state stays, no status is raised, and it changes no token of theirs, eager or in a
+    graph."""
+    cfg = config(4)
+    w = dec.DecoderWeights(cfg, DEV)
+    prompts = ragged_prompts(cfg, [70, 5, 64, 33], 27)
+    prompts[1] = []
+    args = dict(capacity=256, temperature=0.0 if kind == "spec" else 1.0, pages=12,
+                **(dict(top_k=8, top_p=0.9) if kind == "filtered" else {}))
+    outs = []
+    for graph in (False, True):
+        d = dec.DirectDecoder(w, **args) if kind == "direct" else dec.SpecDecoder(w, **args)
+        for a in (d.buf.a, d.buf.q):
+            a.fill_(float("nan"))
+        for _ in range(2):  # (a second prompt after the first one's rounds)
+            if packed:
+                d.prefill_packed(prompts)
+            else:
+                d.prefill(padded(prompts), lengths=[len(p) for p in prompts])
+            state = [int(t[1]) for t in (d.pos_base, d.pending, d.prev, d.out_len)]
+            assert state == [_lib.POS_IDLE, 0, 0, 0]
+            for r in range(6):
+                if kind == "direct":
+                    d.set_uniforms(synth.uniform_u24((4, 1), 600 + r, DEV))
+                else:
+                    d.set_uniforms(synth.uniform_u24((3, 4), 600 + r, DEV), synth.uniform_u24((4, 4), 650 + r, DEV))
+                if not graph:
+                    d.run()
+                elif d.graph is None:
+                    d.capture()
+                else:
+                    d.replay()
+                torch.cuda.synchronize()
+            assert [int(t[1]) for t in (d.pos_base, d.pending, d.prev, d.out_len)] == state
+            assert int(d.pages.held[1]) == 0 and d.status.item() == 0
+            outs.append([d.out_tokens[s, :int(d.out_len[s])].tolist() for s in (0, 2, 3)])
+    assert all(o == outs[0] for o in outs) and min(map(len, outs[0])) >= 6
+    if kind == "spec":
+        dims, model = parent_model(w)
+        for s, o in zip((0, 2, 3), outs[0]):
+            check_greedy(dims, model, prompts[s], o, f"sequence {s}")
+
+
+@pytest.mark.parametrize("rows,hq,hkv", [(1, 28, 4), (9, 28, 4), (70, 8, 2)])
+@pytest.mark.parametrize("q4", [False, True])
+def test_calls_leave_idle_sequences_alone(rows, hq, hkv, q4):
+    """Rows, pages and status as they were; the other sequences' results those of the call without the idle ones."""
+    from test_gpu_paged import bits, calls, ints, normal, pool_of, starts, tables
+
+    paged_rope, _, paged, _ = calls(q4)
+    past = [130, 7, 64, 300, 20]
+    idle, b = (1, 4), 5
+    table, pages = tables([p + rows for p in past], 61)
+    pool, _ = pool_of(table, pages, [rows] * b, past, hkv, q4, 62)
+    pos = ints([_lib.POS_IDLE if s in idle else p for s, p in enumerate(past)])
+    live = [s * rows + j for s in range(b) if s not in idle for j in range(rows)]
+    rest = [s * rows + j for s in idle for j in range(rows)]
+    kept = [s for s in range(b) if s not in idle]
+    qkv, q = normal((b * rows, (hq + 2 * hkv) * 128), 63, rows).float(), normal((b * rows, hq, 128), 64, rows)
+    for start in (None, starts([rows] * b)):
+        for offset in (0, -3):
+            args = dict(max_rows=rows, pos_offset=offset)
+            status = torch.zeros(1, dtype=torch.int32, device=DEV)
+            caches = [x.clone() for x in pool], [x.clone() for x in pool]
+            q_out, out = (torch.full((b * rows, hq, 128), 9.0, dtype=torch.float16, device=DEV) for _ in range(2))
+            paged_rope(qkv, None, start, pos, hq, *caches[0], table, q_out=q_out, status=status, **args)
+            paged(q, *pool, table, start, pos, out=out, **args)
+            # the same rows of the others alone
+            few = dict(max_rows=rows, pos_offset=offset)
+            want_q = paged_rope(qkv[live].contiguous(), None, None, pos[kept].contiguous(), hq, *caches[1],
+                                table[kept].contiguous(), **few)
+            want = paged(q[live].contiguous(), *pool, table[kept].contiguous(), None, pos[kept].contiguous(), **few)
+            assert int(status) == 0
+            assert torch.equal(q_out[live], want_q) and bool((q_out[rest] == 9).all()) and bool((out[rest] == 9).all())
+            # (keys may be split at other places where there are more sequences)
+            assert float((out[live].double() - want.double()).abs().max()) <= 2.0 ** -9 * float(want.abs().max())
+            for x, y in zip(*caches):
+                assert torch.equal(bits(x), bits(y))
+            if q4:
+                ko, vo = (torch.full((b * rows, hkv, 128), 9.0, dtype=torch.float16, device=DEV) for _ in range(2))
+                sq.sq_paged_kv_read_q4(*pool, table, start, pos, b * rows, k_out=ko, v_out=vo, **args)
+                assert bool((ko[rest] == 9).all()) and bool((vo[rest] == 9).all())
+    # all of them idle
+    none, out = ints([_lib.POS_IDLE] * b), torch.full((b * rows, hq, 128), 9.0, dtype=torch.float16, device=DEV)
+    before, status = [x.clone() for x in pool], torch.zeros(1, dtype=torch.int32, device=DEV)
+    paged_rope(qkv, None, None, none, hq, *pool, table, q_out=out, status=status, max_rows=rows)
+    paged(q, *pool, table, None, none, out=out, max_rows=rows)
+    assert int(status) == 0 and bool((out == 9).all()) and all(torch.equal(bits(x), bits(y)) for x, y in zip(pool, before))
+
+
+def test_commit_leaves_idle_sequences():
+    def ints(v):
+        return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+    pos, pending, prev = ints([5, _lib.POS_IDLE, _lib.POS_IDLE, 8]), ints([1, 2, 3, 4]), ints([5, 6, 7, 8])
+    out, n_out, status = torch.zeros((4, 6), dtype=torch.int32, device=DEV), ints([0, 1, 1, 0]), ints([0])
+    sq.sq_spec_commit(ints([1, 1, -1, 0]), ints([20, 21, -1, 23]), ints([[30, 31, -1, 33]]), pending, prev, pos,
+                      out_tokens=out, out_len=n_out, status=status)
+    assert pos.tolist() == [7, _lib.POS_IDLE, _lib.POS_IDLE, 9] and pending.tolist() == [20, 2, 3, 23]
+    assert prev.tolist() == [30, 6, 7, 4] and n_out.tolist() == [2, 1, 1, 1] and int(status) == 0
+    assert out[0, :2].tolist() == [30, 20] and not out[1:3].any() and out[3, :1].tolist() == [23]
