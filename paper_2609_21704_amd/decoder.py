@@ -37,7 +37,7 @@ import torch
 from . import _lib as sq
 from . import synth
 from .configs import HEAD_DIM, Config
-from .rounds import Stack, round_uniforms  # noqa: F401  (round_uniforms: per-round uniforms, same layout)
+from .rounds import Stack, captured, round_uniforms  # noqa: F401  (round_uniforms: per-round uniforms, same layout)
 
 EPS = 1e-6
 THETA = 1e6
@@ -654,13 +654,8 @@ class SpecDecoder:
         advances the sequences by one round), so that the library workspace
         has its final size before capture."""
         self.run()
-        torch.cuda.synchronize()
-        g = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(g):
-            self.run()
-        torch.cuda.synchronize()
-        self.graph = g
-        return g
+        self.graph = captured(self.run)
+        return self.graph
 
     def replay(self):
         self.graph.replay()

@@ -14,6 +14,7 @@ bonus row k is the parent LM head's output for the last verified position.
 """
 from __future__ import annotations
 
+import gc
 from dataclasses import dataclass
 
 import torch
@@ -24,6 +25,24 @@ from .configs import Config
 
 # tensor ids for synth.stream_seed(config seed, kind, ...)
 _W, _XD, _XV, _XLMD, _XLMV, _EPS, _UD, _UA, _DL, _BONUS, _XDIRECT = range(11)
+
+
+def captured(step):
+    """step() as a HIP graph.  Python's garbage collector stays off meanwhile: a dead cycle of objects with a graph among
+    them (a decoder whose user holds it and is held by it, one in the frames of an exception) may be found at any
+    allocation, and a graph that is destroyed while another is captured ends the process."""
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    on = gc.isenabled()
+    gc.disable()
+    try:
+        with torch.cuda.graph(g):
+            step()
+    finally:
+        if on:
+            gc.enable()
+    torch.cuda.synchronize()
+    return g
 
 
 class Stack:
@@ -230,13 +249,8 @@ class Round:
         """Capture one round as a HIP graph (run once eagerly first so the
         library's workspace exists before capture)."""
         self.run()
-        torch.cuda.synchronize()
-        g = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(g):
-            self.run()
-        torch.cuda.synchronize()
-        self.graph = g
-        return g
+        self.graph = captured(self.run)
+        return self.graph
 
     def set_uniforms(self, u_draft: torch.Tensor, u_accept: torch.Tensor):
         self.buf.u_draft.copy_(u_draft)
@@ -288,13 +302,8 @@ class DirectDecode:
 
     def capture(self):
         self.run()
-        torch.cuda.synchronize()
-        g = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(g):
-            self.run()
-        torch.cuda.synchronize()
-        self.graph = g
-        return g
+        self.graph = captured(self.run)
+        return self.graph
 
     def replay(self):
         self.graph.replay()
