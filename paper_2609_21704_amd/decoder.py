@@ -338,6 +338,17 @@ class SpecDecoder:
             self.pos_base.masked_fill_(self.pages.held * sq.PAGE < self.pos_base, sq.POS_IDLE)
             self.buf.a.zero_()
 
+    def retire(self, rows):
+        """These sequences (row numbers, over pages) end: they give their pages back and are idle until the next prefill;
+        their tokens stay."""
+        if not self.pages:
+            raise ValueError("sequences end before their batch over pages only")
+        ended = torch.zeros((self.R,), dtype=torch.bool)
+        ended[list(rows)] = True
+        ended = ended.to(self.device)
+        self.pos_base.masked_fill_(ended, sq.POS_IDLE)
+        self.pages.trim(ended.to(torch.int32) - 1, self.status)
+
     # ------------------------------------------------------------- passes
     def _linear(self, draft: bool, key, x, y):
         st = self.w.stack

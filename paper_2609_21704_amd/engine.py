@@ -27,7 +27,7 @@ import time
 import torch
 
 from . import synth
-from ._lib import DEV_BAD_PAGE, DEV_NO_DIST, DEV_NO_PAGES, PAGE
+from ._lib import PAGE
 from .configs import HEAD_DIM, Config
 from .decoder import DecoderWeights, DirectDecoder, SpecDecoder, filters_wanted
 from .router import ROUTES, Router, features, hash_tokenize
@@ -109,7 +109,8 @@ class Engine:
                  parent: DecoderWeights | None = None, timed: bool = False, draft_cache: str = "f16",
                  packed: bool = False, pages: int | None = None, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
         """`pages`: the decoders keep their caches in pools of that many pages of 64 positions, taken as the sequences
-        grow.  `top_k`, `top_p`, `min_p`: tokens follow what these leave of the parent's distribution (temperature > 0).
+        grow and given back once they have their tokens; a batch with a sequence that lacks one before that fails.
+        `top_k`, `top_p`, `min_p`: tokens follow what these leave of the parent's distribution (temperature > 0).
         `draft_cache`: "q4" keeps the drafts' caches in 4 bits.  `packed`: the
         prompts of a batch go through the models packed, without padding and
         without copies of a prompt for idle rows (`SpecDecoder.prefill_packed`, whose
@@ -232,7 +233,7 @@ class Engine:
             raise RuntimeError(f"the batch's prompts find no pages in a pool of {self.pages} (device status flags "
                                f"{self._flags(dec)})")
         per_round = 1 if variant == "f16" else self.k + 1
-        r = 0
+        r = ended = 0
         while True:
             dec.set_uniforms(*self._uniforms(variant, r))
             if dec.graph is None:
@@ -241,8 +242,13 @@ class Engine:
                 dec.replay()
             r += 1
             # every round emits at least one token per sequence: check only once enough rounds may have run
-            if r * per_round >= max_new and int(dec.out_len[:n].min().item()) >= max_new:
-                break
+            if r * per_round >= max_new:
+                done = [s for s, x in enumerate(dec.out_len[:n].tolist()) if x >= max_new]
+                if len(done) == n:
+                    break
+                if self.pages is not None and len(done) > ended:  # nothing that they would still need may fail the others
+                    ended = len(done)
+                    dec.retire(done)
             if r > max_new:
                 raise RuntimeError(f"a round emitted no token (device status flags {self._flags(dec)})")
         t2 = self._clock()
@@ -250,9 +256,6 @@ class Engine:
             self.seconds[(variant, "prefill")] += t1 - t0
             self.seconds[(variant, "rounds")] += t2 - t1
         flags = self._flags(dec)
-        if self.pages is not None:
-            # a row that found no page once it had its tokens; what it lacked them for it did not emit
-            flags &= ~(DEV_NO_PAGES | DEV_BAD_PAGE | DEV_NO_DIST)
         if flags:
             raise RuntimeError(f"device status flags {flags} raised")
         self._batches += 1

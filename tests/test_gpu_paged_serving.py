@@ -1,5 +1,5 @@
 """GPU tests of what shares a pool of pages with what: padded prompts take the pages of their own lengths, sequences whose
-prompts found none emit nothing, whatever becomes free later, and idle rows of a batch hold none."""
+prompts found none emit nothing, whatever becomes free later, idle rows of a batch hold none, and sequences that have their tokens give theirs back."""
 import pytest
 import torch
 
@@ -224,3 +224,82 @@ def test_commit_leaves_idle_sequences():
     assert pos.tolist() == [7, _lib.POS_IDLE, _lib.POS_IDLE, 9] and pending.tolist() == [20, 2, 3, 23]
     assert prev.tolist() == [30, 6, 7, 4] and n_out.tolist() == [2, 1, 1, 1] and int(status) == 0
     assert out[0, :2].tolist() == [30, 20] and not out[1:3].any() and out[3, :1].tolist() == [23]
+
+
+# --------------------------------------------------- sequences with their tokens
+class Uneven(Engine):
+    """Uniforms with which the first sequence accepts every draft that has a weight, and the others next to none."""
+
+    def _uniforms(self, variant, r):
+        u_draft, u = super()._uniforms(variant, r)
+        if u is not None:
+            u[0, :-1], u[1:, :-1] = 0, (1 << 24) - 1
+        return u_draft, u
+
+
+@pytest.mark.parametrize("draft_cache", ["f16", "q4"])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("route", ["int4", "fp8"])
+def test_a_sequence_ahead_of_its_batch(route, packed, draft_cache):
+    """A pool that holds every sequence until it has its tokens, but not what the first one would take until the last has
+    its own: the tokens are those over a pool without end."""
+    cfg, max_new = config(3), 40
+    w = dec.DecoderWeights(cfg, DEV)
+    prompts = ragged_prompts(cfg, [20, 18, 21], 28)
+    got = []
+    for pages in (3, 40):
+        eng = Uneven(cfg, DEV, layers=3, k=3, batch=3, capacity=256, temperature=1.0, pages=pages, packed=packed,
+                     draft_cache=draft_cache, parent=w, seed=9)
+        for _ in range(2):
+            got.append([r.tokens for r in eng.generate(prompts, max_new, routes=[route] * 3)])
+            d = eng.decoders[route]
+            assert int(d.pos_base[0]) == _lib.POS_IDLE and int(d.pages.held[0]) == 0
+    assert got[0] == got[2] and got[1] == got[3] and all(len(t) == max_new for o in got for t in o)
+    # the first one left to run finds no page for its further tokens before the last one has its own
+    eng = Uneven(cfg, DEV, layers=3, k=3, batch=3, capacity=256, temperature=1.0, pages=3, packed=packed,
+                 draft_cache=draft_cache, parent=w, seed=9)
+    d = eng.decoder(route)
+    if packed:
+        d.prefill_packed(prompts)
+    else:
+        d.prefill(padded(prompts), lengths=[20, 18, 21])
+    for r in range(max_new):
+        d.set_uniforms(*eng._uniforms(route, r))
+        d.run()
+        if int(d.out_len.min()) >= max_new:
+            break
+    assert d.status.item() & _lib.DEV_NO_PAGES and d.status.item() & _lib.DEV_BAD_TOKEN
+
+
+def test_what_ended_sequences_held_is_for_the_others():
+    """Two sequences end, a third one grows over their pages."""
+    cfg = config(3)
+    w = dec.DecoderWeights(cfg, DEV)
+    prompts = ragged_prompts(cfg, [60, 64, 40], 29)
+    d = dec.SpecDecoder(w, capacity=256, temperature=0.0, pages=4)
+    d.prefill_packed(prompts)
+    d.run()
+    first = [d.out_tokens[s, :int(d.out_len[s])].tolist() for s in (0, 1)]
+    d.retire([0, 1])
+    assert d.pages.held.tolist() == [0, 0, 1] and int(d.pages.refs.sum()) == 1
+    while int(d.out_len[2]) < 150:
+        d.run()
+    assert d.status.item() == 0 and d.pages.held.tolist()[:2] == [0, 0] and int(d.pages.held[2]) >= 3
+    assert d.out_len[:2].tolist() == [len(t) for t in first]
+    dims, model = parent_model(w)
+    for s in range(3):
+        check_greedy(dims, model, prompts[s], d.out_tokens[s, :int(d.out_len[s])].tolist(), f"sequence {s}")
+    with pytest.raises(ValueError, match="over pages only"):
+        dec.SpecDecoder(w, capacity=128).retire([0])
+
+
+@pytest.mark.parametrize("route", ["f16", "int4"])
+def test_a_sequence_that_lacks_a_page_before_its_tokens_fails_its_batch(route):
+    cfg = config(2)
+    eng = Engine(cfg, DEV, layers=3, k=3, batch=2, capacity=256, temperature=0.0, pages=3)
+    prompts = ragged_prompts(cfg, [60, 62], 30)
+    with pytest.raises(RuntimeError, match="status flags"):
+        eng.generate(prompts, 80, routes=[route] * 2)  # two sequences of 3 pages each
+    got = eng.generate(prompts[:1], 80, routes=[route])[0].tokens
+    dims, model = parent_model(eng.weights["f16"])
+    check_greedy(dims, model, prompts[0], got, route)
