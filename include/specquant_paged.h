@@ -34,8 +34,10 @@ extern "C" {
 #define SQ_DEV_BAD_FORK 128 /* a fork that names no possible pair of rows: it was left out */
 
 /* Room for the positions below pos_base[s] + ahead: row s gets the pages it lacks, in the order of the rows, as long as
- * free pages last (the first row that does not get all of its pages gets none, like every later one that needs any:
- * SQ_DEV_NO_PAGES).  pos_base[s] < 0: the row is left alone.  Nothing is taken back.  Pages come as they were left.
+ * free pages last.  The first row for which too few are left gets none, like every later one that needs any.  A row that
+ * needs more than its table's width gets none either, and keeps none from the others.  Each sets SQ_DEV_NO_PAGES.
+ * pos_base[s] < 0: the row is left alone.  Nothing is taken back.  Pages come as they were left: positions for which a row
+ * found no page while they were computed hold nothing of it later.
  * pos_base [b]; 0 <= ahead <= 2^20.  Workspace: 4 bytes a page. */
 sq_status sq_pages_reserve(int32_t* table, int32_t* held, int32_t* refs, int32_t b, int64_t width, int64_t pages,
                            const int32_t* pos_base, int32_t ahead, int32_t* status, hipStream_t stream);
