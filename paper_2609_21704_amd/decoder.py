@@ -349,6 +349,15 @@ class SpecDecoder:
         self.pos_base.masked_fill_(ended, sq.POS_IDLE)
         self.pages.trim(ended.to(torch.int32) - 1, self.status)
 
+    def rewind(self, rows, tokens: int):
+        """These sequences (row numbers) have ended with `tokens` tokens, and go on over the entries of their own caches from
+        position 1 on, to no end: contiguous caches have no idle rows, and past its end a row would raise SQ_DEV_BAD_POS."""
+        ended = torch.zeros((self.B,), dtype=torch.bool)
+        ended[list(rows)] = True
+        ended = ended.to(self.device)
+        self.pos_base.masked_fill_(ended.repeat_interleave(self.c), 1)
+        self.out_len.masked_fill_(ended, tokens)
+
     # ------------------------------------------------------------- passes
     def _linear(self, draft: bool, key, x, y):
         st = self.w.stack

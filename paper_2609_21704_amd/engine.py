@@ -218,8 +218,9 @@ class Engine:
         # idle rows have no prompt over pages, which they would take from the others; elsewhere they are fed two tokens of the
         # first one, or repeat it
         if self.packed and dec.takes_packed():
+            rows = toks + [[] if self.pages else toks[0][:2]] * (self.batch - n)
             t0 = self._clock()
-            dec.prefill_packed(toks + [[] if self.pages else toks[0][:2]] * (self.batch - n))
+            dec.prefill_packed(rows)
         else:
             rows = toks + [[] if self.pages else toks[0]] * (self.batch - n)
             Lp = max(len(t) for t in rows)
@@ -243,12 +244,20 @@ class Engine:
             r += 1
             # every round emits at least one token per sequence: check only once enough rounds may have run
             if r * per_round >= max_new:
-                done = [s for s, x in enumerate(dec.out_len[:n].tolist()) if x >= max_new]
-                if len(done) == n:
+                lens = dec.out_len.tolist()
+                done = [s for s, x in enumerate(lens) if x >= max_new]
+                live = n - sum(s < n for s in done)
+                if live == 0:
                     break
-                if self.pages is not None and len(done) > ended:  # nothing that they would still need may fail the others
-                    ended = len(done)
-                    dec.retire(done)
+                # nothing that the others would still need may fail those
+                if self.pages is not None:
+                    if n - live > ended:
+                        ended = n - live
+                        dec.retire(done)
+                else:  # those whose next round would leave their caches, idle rows among them
+                    done = [s for s in done if len(rows[s]) + lens[s] + per_round - 1 > self.capacity]
+                    if done:
+                        dec.rewind(done, max_new)
             if r > max_new:
                 raise RuntimeError(f"a round emitted no token (device status flags {self._flags(dec)})")
         t2 = self._clock()
