@@ -1472,7 +1472,8 @@ hipError_t launch_packed_attention(const uint16_t* q, const PackedRows& pr, int 
   // Pages: where the keys of a sequence would be taken whole, in shares of all sequences' keys.  The two, 28 heads on 4, fp16
   // and 4-bit entries: 48 sequences of 2000 positions 40 and 49 us, 16 and 24; of 300 to 9000 positions 124 and 61, 44 and 32;
   // 64 of 2000 49 and 62, 18 and 25, of 300 to 9000 133 and 83, 48 and 39.  Fewer sequences, in parts of one length each
-  // and in shares: 32 of 300 to 9000 42 and 47, 20 and 30, eight of them 15.3 and 18.1.
+  // and in shares: 32 of 300 to 9000 42 and 47, 20 and 30, eight of them 15.3 and 18.1.  (So many sequences of one length
+  // lose by shares a fifth to a half, and those of different lengths gain up to half; the lengths are on the device.)
   const bool shares = paged && p.few && 2 * (int64_t)pr.b * hkv > kMaxParts;
   if (shares) {
     p.grain = 0;

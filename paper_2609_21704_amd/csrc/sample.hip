@@ -8,8 +8,9 @@
 //                     workgroup finds the cuts among the gathered tokens (1024 bins of the bin, then ranks) and draws
 //   4. filter_kernel  writes the kept logits
 // A row without top-k and top-p is drawn from by step 2.  Where the bins of the cuts hold too many tokens (ties, rows
-// whose logits lie close together but for a few), the last workgroup finds the cuts by a radix selection over the row
-// (11 bits of the logit's key a pass).
+// whose logits lie close together but for a few, rows with fewer finite logits than top-k keeps, whose cut goes through the
+// -inf ones), the last workgroup finds the cuts by a radix selection over the row (11 bits of the logit's key a pass): 5
+// finite logits of 151936 under top-k 50 take 475 us a row and 502 for 64 rows, ordinary rows 23 and 42.
 // Weights are whole numbers, so their sums do not depend on any order.  Rows are cut into segments so that a call fills
 // the chip from one row on, and a segment into runs, one a wavefront, whose sums say where a draw has to look.  Last
 // workgroups are found by counting arrivals (counters that step 1 clears).
