@@ -303,3 +303,33 @@ def test_a_sequence_that_lacks_a_page_before_its_tokens_fails_its_batch(route):
     got = eng.generate(prompts[:1], 80, routes=[route])[0].tokens
     dims, model = parent_model(eng.weights["f16"])
     check_greedy(dims, model, prompts[0], got, route)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_padded_prompts_of_a_4_bit_draft(packed):
+    cfg, max_new = config(3), 20
+    eng = Engine(cfg, DEV, layers=3, k=3, batch=3, capacity=256, temperature=0.0, pages=7, packed=packed, draft_cache="q4")
+    prompts = ragged_prompts(cfg, [200, 10, 66], 31)
+    got = [r.tokens for r in eng.generate(prompts, max_new, routes=["int4"] * 3)]
+    dims, model = parent_model(eng.weights["f16"])
+    for i, p in enumerate(prompts):
+        check_greedy(dims, model, p, got[i], f"request {i}")
+
+
+def test_lengths_that_are_refused():
+    """One token is no prompt, over pages or not; none is one over pages only."""
+    cfg = config(2)
+    w = dec.DecoderWeights(cfg, DEV)
+    prompts = ragged_prompts(cfg, [9, 5], 32)
+    for pages in (None, 4):
+        d = dec.SpecDecoder(w, capacity=128, pages=pages)
+        for lengths in ([9, 1], [9, -1], [9, 10], [9]) + (() if pages else ([9, 0],)):
+            with pytest.raises(ValueError, match="lengths"):
+                d.prefill(padded(prompts), lengths=lengths)
+        for bad in (prompts[1][:1],) + (() if pages else ([],)):
+            with pytest.raises(ValueError, match="one prompt of 2"):
+                d.prefill_packed([prompts[0], bad])
+    d.prefill(padded(prompts), lengths=[9, 0])
+    assert d.pages.held.tolist() == [1, 0] and int(d.pos_base[1]) == _lib.POS_IDLE and d.status.item() == 0
+    with pytest.raises(ValueError, match="group of samples"):
+        dec.DirectDecoder(w, capacity=128, pages=4, samples=2).prefill_packed([[]])
